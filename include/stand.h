@@ -360,6 +360,134 @@ int stand_copy_bytes(void *d_dst, const void *d_src, uint64_t bytes, void *strea
  * alignment. */
 int stand_read_rows(const void *d_src, uint64_t row_bytes, uint64_t rows, uint32_t *d_sink, void *stream);
 
+/* ---- around a verification: the target model's attention, its cache, its logits --------------------------------------
+ *
+ * What a serving loop does between two steps beside stand_step, on data that only the GPU has (which nodes were drafted,
+ * which were accepted), so that the host never waits for a length:
+ *
+ *   stand_cache_pages      lengths move on by what was accepted; pages are taken and given back; slots of the next tokens
+ *   stand_tree_attention   in every layer: the tree's nodes attend to the cache and to their ancestors in the tree
+ *   stand_count_tokens,
+ *   stand_shape_logits     penalties, biases and a grammar's masks on the tree's logits, before stand_verify / stand_step
+ *   stand_cache_commit     keys and values of the accepted path go to their slots, all layers at once
+ *
+ * The calls take tree, batch, vocabulary, type of the logits and device from the handle, read nothing else of it and change
+ * nothing in it; they allocate nothing, keep nothing, and may be captured into a graph.  The caller's current device is
+ * the same after a call.  Up to 65 535 trajectories (STAND_ELIMIT above).
+ *
+ * Trees: the root's keys and values are those of the last committed token, which is not in the cache yet: a cache of n
+ * tokens holds the positions 0 .. n-1 and node u stands at position n + depth(u) (stand_tree_packing's d_pos).  The rows of
+ * a tree stay in the caller's buffers until stand_cache_commit; rejected nodes never reach the cache. */
+
+#define STAND_F16 2         /* binary16: caches only, not logits */
+#define STAND_MAX_PAGE 4096 /* tokens of a page, a power of two */
+
+/* A paged cache: element e of head g at place s of page p in layer l is d_k[l * layer_stride + p * page_stride + s * slot_stride
+ * + g * head_stride + e], d_v likewise.  Strides are in elements, not negative and multiples of 8; pointers are 16-byte aligned.
+ * A slot is p * page_size + s. */
+typedef struct {
+    void *d_k, *d_v;
+    int32_t dtype;      /* STAND_BF16 or STAND_F16, also that of the rows given with it */
+    int32_t layers, pages;
+    int32_t page_size;  /* a power of two <= STAND_MAX_PAGE */
+    int32_t kv_heads;   /* <= 4096 */
+    int32_t head_dim;   /* 64 or 128 */
+    int64_t layer_stride, page_stride, slot_stride, head_stride;
+} stand_cache;
+
+/* Queries, keys, values and outputs of the tree's nodes in one layer: strides of batch, node and head in elements, not
+ * negative and multiples of 8 (slices of a fused projection are fine); a head's elements are contiguous; pointers are
+ * 16-byte aligned.  The outputs overlap none of the inputs. */
+typedef struct {
+    const void *d_q, *d_k, *d_v; /* [B][N][q_heads | kv_heads | kv_heads][head_dim] */
+    void *d_out;                 /* [B][N][q_heads][head_dim] */
+    int32_t q_heads;             /* a multiple of kv_heads; query head i reads head i / (q_heads / kv_heads) */
+    float scale;                 /* of the scores, > 0 (usually head_dim ^ -0.5) */
+    int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
+} stand_tree_rows;
+
+/* Attention of a drafted tree.  For every node u with d_draft_tok[b][u] >= 0 and every query head:
+ *     out = sum_t p_t value_t,   p = softmax over t of (scale * query . key_t)
+ * where t runs over the first d_len[b] cached tokens of trajectory b and over the nodes on the path root -> u (u included):
+ * the mask of stand_tree_packing beside the cache.  Nodes that were not drafted get zeros; what stands in their rows, in
+ * rows off a node's path and behind a length is never used, whatever it is (a NaN included).  d_draft_tok [B][N] is what
+ * stand_draft / stand_step gave.  Token t of trajectory b is in page d_table[b][t / page_size], d_table: [B][table_width].
+ * A length below 0 counts as 0, one above table_width * page_size (at most 2^31 - 1) as that; a page outside the cache is never
+ * read (what is read instead is not specified).  A tree of one node is the ordinary attention of single tokens.
+ *   Products are summed in fp32, the weights p are rounded to the cache's type for the product with the values (relative error
+ * 2^-9 in bf16, 2^-12 in fp16 each, at most half a step) and summed as rounded; the result is rounded once.
+ *   d_work: 16-byte aligned device memory of stand_tree_attention_work bytes, used from the call's start to its end on the
+ * stream; no content is expected or kept.  Calls that may overlap (other streams, other graphs) need one each. */
+int stand_tree_attention(stand_handle *h, const stand_cache *cache, int32_t layer, const int32_t *d_len, const int32_t *d_table,
+                         int32_t table_width, const int32_t *d_draft_tok, const stand_tree_rows *rows, void *d_work,
+                         uint64_t work_bytes, void *stream);
+/* Bytes of d_work (0 for arguments that stand_tree_attention refuses). */
+uint64_t stand_tree_attention_work(const stand_handle *h, const stand_cache *cache, int32_t q_heads);
+
+/* Keys and values of `rows` rows of each trajectory in all layers of a cache: [layers][B][rows][kv_heads][head_dim] by the
+ * strides, as in stand_cache. */
+typedef struct {
+    const void *d_k, *d_v;
+    int32_t rows;
+    int64_t layer_stride, batch_stride, row_stride, head_stride;
+} stand_cache_rows;
+
+/* Rows into the cache: for all layers, trajectories b and j < d_count[b], row d_row[b][j] of trajectory b goes to slot
+ * d_slots[b][j] (stand_cache_pages).  After a verification d_row is d_out_node and d_count is d_out_len (width = depth + 1); a
+ * prompt's rows go in as they stand with d_row NULL (row j).  d_count NULL: `width` each.  A negative slot or row (or one past
+ * the end) is left out.  d_slots, d_row: [B][width].  The slots of a call differ from each other (where they do not, what
+ * ends up there is not specified); the rows do not overlap the cache. */
+int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots, int32_t width,
+                       const int32_t *d_row, const int32_t *d_count, void *stream);
+
+/* The pages of a cache.  Free pages stand in a ring: entries mark[0] .. mark[1] - 1, modulo `pages`; a new cache has every page
+ * in the ring, mark = {0, pages}, and all lengths and held counts 0.  d_table rows are valid up to d_held[b] entries. */
+typedef struct {
+    int32_t *d_table;       /* [B][width] */
+    int32_t *d_ring;        /* [pages] */
+    int32_t *d_length;      /* [B] tokens in the cache */
+    int32_t *d_held;        /* [B] pages of the trajectory */
+    int64_t *d_mark;        /* [2] {taken, given}, only grow */
+    int32_t width, pages, page_size; /* width * page_size < 2^31 */
+} stand_pages;
+
+/* Moves lengths on and sees that there is room for the next tokens.  For each trajectory
+ *     length <- min(max(length + d_add[b], 0), held * page_size);   need = ceil((length + d_room[b]) / page_size) pages;
+ * with need > held the missing pages are taken from the ring, with need < held the last ones go back to it.  d_room[b] < 0
+ * gives everything back (length 0).  d_add NULL: 0; after a step it is d_out_len.  d_room NULL: depth + 1 of the tree, what a
+ * verification can accept.  Demands are served in the order of the trajectories from the pages that were free before the call:
+ * one is served if it and all before it (those that would not fit the table's width aside) fit into them; d_missing[b] is the
+ * number of pages that a trajectory asked for and did not get (it keeps what it held), else 0.  Pages given back in a call are
+ * free from the next one on.  d_slots [B][slot_width]: slot of the token at position length + j for j < d_room[b], -1 behind that
+ * and where there is no page.  (d_slots may be NULL with slot_width 0.)
+ *   `out` receives lengths, held counts and marks, and names the table and the ring of `p`; its three arrays may be those of
+ * `p`.  Where they are others, the call can be repeated from `p` with the same result. */
+int stand_cache_pages(stand_handle *h, const stand_pages *p, const int32_t *d_add, const int32_t *d_room, int64_t *d_slots,
+                      int32_t slot_width, int32_t *d_missing, const stand_pages *out, void *stream);
+
+/* Penalties, biases and masks on the logits [B][N][V] of a drafted tree; d_out may be d_logits, otherwise they do not overlap.
+ * For a drafted node u and token v, in this order and in fp32, rounded once to the type of the logits:
+ *   c = times v was generated in trajectory b, its occurrences on the path root -> u after the root included
+ *   c > 0 or v in the prompt:  x <- x > 0 ? x / repetition : x * repetition
+ *   x <- x - frequency * c;   c > 0:  x <- x - presence;   x <- x + bias of v
+ *   d_allow[b][u] has no bit for v:  x <- -inf, whatever x was.  A row without any bit for a token is not masked (a node that
+ *   the grammar does not reach: its parent's mask keeps it from being accepted), so that its maximum stays finite.
+ * Rows of nodes that were not drafted are copied.
+ *   d_count    [B][V] kept by stand_count_tokens, or NULL (nothing generated, no prompt; the path's tokens count all the same)
+ *   d_penalty  [B][3]: repetition (> 0; 1: none), presence, frequency (0: none); or NULL
+ *   d_bias_id  [B][bias_width], d_bias [B][bias_width]: ids outside [0, V) are left out, of entries with the same id the last
+ *              counts; biases are finite or -inf; bias_width 0: none
+ *   d_allow    [B][N][(V + 31) / 32]: bit v % 32 of word v / 32; bits past V do not matter; or NULL */
+int stand_shape_logits(stand_handle *h, const void *d_logits, void *d_out, const int32_t *d_draft_tok, const int32_t *d_count,
+                       const float *d_penalty, const int32_t *d_bias_id, const float *d_bias, int32_t bias_width,
+                       const uint32_t *d_allow, void *stream);
+
+/* Tokens into the counts d_count [B][V] (zeros at first): the first d_len[b] (NULL: width) of d_tok [B][width]; ids outside [0, V)
+ * are left out.  prompt == 0: generated tokens, added (after a step: d_out_tok, d_out_len); otherwise the prompt's.  A count
+ * holds the times generated in bits 0 .. 29 and the prompt's mark in bit 30. */
+int stand_count_tokens(stand_handle *h, int32_t *d_count, const int32_t *d_tok, const int32_t *d_len, int32_t width, int32_t prompt,
+                       void *stream);
+
 const char *stand_strerror(int code);
 int stand_last_hip_error(const stand_handle *h);
 

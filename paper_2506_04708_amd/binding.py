@@ -13,7 +13,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libstand.so")
 
-STAND_BF16, STAND_F32 = 0, 1
+STAND_BF16, STAND_F32, STAND_F16 = 0, 1, 2
 DRAFT_GUMBEL_TOPK, DRAFT_MULTINOMIAL, DRAFT_DETERMINISTIC = 0, 1, 2
 MERGE_MEAN, MERGE_REPLACE = 0, 1
 STEP_AUTO, STEP_SERIAL, STEP_FUSED = 0, 1, 2
@@ -28,6 +28,8 @@ EXPORTED = [
     "stand_tree_packing", "stand_verify_static", "stand_static_scratch_need",
     "stand_set_step_plan", "stand_set_wait_limit", "stand_step_timeline", "stand_step_is_one_launch",
     "stand_get_record_slots",
+    "stand_tree_attention", "stand_tree_attention_work", "stand_cache_commit", "stand_cache_pages", "stand_shape_logits",
+    "stand_count_tokens",
 ]
 
 
@@ -47,6 +49,36 @@ class Stats(C.Structure):
         ("inserts", C.c_uint64), ("merges", C.c_uint64), ("drops", C.c_uint64),
         ("near_threshold", C.c_uint64), ("tokens_emitted", C.c_uint64), ("accept_tests", C.c_uint64),
         ("filter_mismatch", C.c_uint64), ("wait_expired", C.c_uint64), ("late_paths", C.c_uint64),
+    ]
+
+
+class CacheDesc(C.Structure):
+    _fields_ = [
+        ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("dtype", C.c_int32), ("layers", C.c_int32), ("pages", C.c_int32),
+        ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("layer_stride", C.c_int64),
+        ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
+    ]
+
+
+class TreeRows(C.Structure):
+    _fields_ = [
+        ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_out", C.c_void_p), ("q_heads", C.c_int32),
+        ("scale", C.c_float), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
+        ("out_stride", C.c_int64 * 3),
+    ]
+
+
+class CacheRows(C.Structure):
+    _fields_ = [
+        ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("rows", C.c_int32), ("layer_stride", C.c_int64),
+        ("batch_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64),
+    ]
+
+
+class PagesDesc(C.Structure):
+    _fields_ = [
+        ("d_table", C.c_void_p), ("d_ring", C.c_void_p), ("d_length", C.c_void_p), ("d_held", C.c_void_p),
+        ("d_mark", C.c_void_p), ("width", C.c_int32), ("pages", C.c_int32), ("page_size", C.c_int32),
     ]
 
 
@@ -88,6 +120,13 @@ def load_library():
     lib.stand_get_record_slots.argtypes = [vp, vp]
     lib.stand_tree_packing.argtypes = [vp, vp, vp, vp]
     lib.stand_reset_node_counts.argtypes = [vp]
+    lib.stand_tree_attention.argtypes = [vp, vp, C.c_int32, vp, vp, C.c_int32, vp, vp, vp, C.c_uint64, vp]
+    lib.stand_tree_attention_work.argtypes = [vp, vp, C.c_int32]
+    lib.stand_tree_attention_work.restype = C.c_uint64
+    lib.stand_cache_commit.argtypes = [vp, vp, vp, vp, C.c_int32, vp, vp, vp]
+    lib.stand_cache_pages.argtypes = [vp, vp, vp, vp, vp, C.c_int32, vp, vp, vp]
+    lib.stand_shape_logits.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, C.c_int32, vp, vp]
+    lib.stand_count_tokens.argtypes = [vp, vp, vp, vp, C.c_int32, C.c_int32, vp]
     lib.stand_strerror.restype = C.c_char_p
     lib.stand_strerror.argtypes = [C.c_int]
     lib.stand_last_hip_error.argtypes = [vp]
@@ -179,6 +218,53 @@ try:
         return _raw_stream(_device())
 except AttributeError:   # (a torch without them)
     _stream_ptr_up = _stream_ptr
+
+
+def _stream_of(device):
+    return torch.cuda.current_stream(device).cuda_stream
+
+
+try:
+    _stream_of = _raw_stream
+except NameError:
+    pass
+
+
+_HALF = {torch.bfloat16: STAND_BF16, torch.float16: STAND_F16}
+
+
+class PagedCache:
+    """Keys and values of a paged cache: tensors indexed [layer, page, place, head, element], any strides but for the last."""
+
+    def __init__(self, k, v):
+        assert k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device
+        assert k.is_cuda and k.dtype in _HALF and k.stride(4) == 1
+        self.k, self.v = k, v
+        self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), _HALF[k.dtype], *k.shape, *k.stride()[:4])
+        self.ref = C.addressof(self.desc)
+
+
+class Pages:
+    """Block tables, lengths and the ring of free pages of a cache (stand_pages)."""
+
+    def __init__(self, page_size, table, ring, length, held, mark):
+        assert table.dim() == 2 and length.shape == held.shape == table.shape[:1] and mark.shape == (2,) and ring.dim() == 1
+        assert all(t.device == table.device for t in (ring, length, held, mark))
+        self.page_size, self.table, self.ring, self.length, self.held, self.mark = page_size, table, ring, length, held, mark
+        self.desc = PagesDesc(*[_dptr(t, torch.int32) for t in (table, ring, length, held)], _dptr(mark, torch.int64),
+                              table.shape[1], ring.shape[0], page_size)
+        self.ref = C.addressof(self.desc)
+
+    @classmethod
+    def new(cls, batch, pages, page_size, width, device="cuda"):
+        """Nothing in the cache, all pages free."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return cls(page_size, torch.full((batch, width), -1, **i32), torch.arange(pages, **i32), torch.zeros(batch, **i32),
+                   torch.zeros(batch, **i32), torch.tensor([0, pages], dtype=torch.int64, device=device))
+
+    def beside(self):
+        """Other lengths, held counts and marks beside the same table and ring."""
+        return Pages(self.page_size, self.table, self.ring, *(torch.empty_like(t) for t in (self.length, self.held, self.mark)))
 
 
 class Stand:
@@ -327,6 +413,82 @@ class Stand:
         pos = torch.empty((self.B, self.N), dtype=torch.int64, device=self.device)
         _check(self._lib.stand_tree_packing(self.h, _dptr(mask), _dptr(pos), _stream_ptr_up()), self.h)
         return mask, pos
+
+    def _here(self, *tensors):
+        for t in tensors:
+            assert t is None or t.device == self.device, "tensor on %s, handle on %s" % (t.device, self.device)
+
+    def _stream(self):
+        # the caller's stream on the handle's device, whichever device is the current one
+        return _stream_of(self.device.index)
+
+    def tree_attention(self, cache, layer, length, table, draft_tok, q, k, v, scale=None, out=None):
+        """Attention of the drafted nodes over the cache's first length[b] tokens and their own ancestors: q [B, N, heads, d],
+        k, v [B, N, kv heads, d] (slices of a fused projection are fine) -> out, like q."""
+        B, N, H, d = q.shape
+        G = cache.k.shape[3]
+        if out is None:
+            out = torch.empty((B, N, H, d), dtype=q.dtype, device=q.device)
+        assert (B, N) == (self.B, self.N) and k.shape == v.shape == (B, N, G, d) and out.shape == q.shape and d == cache.k.shape[4]
+        assert q.dtype == k.dtype == v.dtype == out.dtype == cache.k.dtype
+        assert q.stride(3) == k.stride(3) == v.stride(3) == out.stride(3) == 1
+        assert length.shape == (B,) and table.dim() == 2 and table.shape[0] == B and draft_tok.shape == (B, N)
+        self._here(cache.k, length, table, draft_tok, q, k, v, out)
+        s3 = C.c_int64 * 3
+        rows = TreeRows(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), H, d ** -0.5 if scale is None else scale,
+                        s3(*q.stride()[:3]), s3(*k.stride()[:3]), s3(*v.stride()[:3]), s3(*out.stride()[:3]))
+        need = self._lib.stand_tree_attention_work(self.h, cache.ref, H)
+        # (torch's allocator hands this memory on in the order of the stream, and keeps a captured graph's apart)
+        work = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
+        _check(self._lib.stand_tree_attention(self.h, cache.ref, layer, _dptr(length, torch.int32), _dptr(table, torch.int32), table.shape[1],
+                                              _dptr(draft_tok, torch.int32), C.addressof(rows), work.data_ptr(), need, self._stream()), self.h)
+        return out
+
+    def cache_commit(self, cache, k, v, slots, row=None, count=None):
+        """Rows k, v [layers, B, rows, kv heads, d] into the cache: row[b][j] (None: j) to slots[b][j], j < count[b] (None: all)."""
+        L, _, _, G, d = cache.k.shape
+        assert k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype == cache.k.dtype and k.stride(4) == 1
+        assert k.dim() == 5 and (k.shape[0], k.shape[1], k.shape[3], k.shape[4]) == (L, self.B, G, d)
+        assert slots.dim() == 2 and slots.shape[0] == self.B and (row is None or row.shape == slots.shape) and (count is None or count.shape == (self.B,))
+        self._here(cache.k, k, v, slots, row, count)
+        rows = CacheRows(k.data_ptr(), v.data_ptr(), k.shape[2], *k.stride()[:4])
+        _check(self._lib.stand_cache_commit(self.h, cache.ref, C.addressof(rows), _dptr(slots, torch.int64), slots.shape[1],
+                                            _dptr(row, torch.int32), _dptr(count, torch.int32), self._stream()), self.h)
+
+    def cache_pages(self, pages, add=None, room=None, slots=None, missing=None, out=None):
+        """Moves lengths on by add, takes and gives back pages for room more tokens (None: a whole path); slots [B, any] and
+        missing [B] are written.  out: Pages that receives the new state (None: in place)."""
+        if missing is None:
+            missing = torch.empty(self.B, dtype=torch.int32, device=self.device)
+        out = pages if out is None else out
+        assert pages.table.shape[0] == self.B and missing.shape == (self.B,) and (slots is None or (slots.dim() == 2 and slots.shape[0] == self.B))
+        assert (add is None or add.shape == (self.B,)) and (room is None or room.shape == (self.B,))
+        self._here(pages.table, out.table, add, room, slots, missing)
+        _check(self._lib.stand_cache_pages(self.h, pages.ref, _dptr(add, torch.int32), _dptr(room, torch.int32), _dptr(slots, torch.int64),
+                                           0 if slots is None else slots.shape[1], _dptr(missing, torch.int32), out.ref, self._stream()), self.h)
+        return missing
+
+    def shape_logits(self, logits, out, draft_tok, count=None, penalty=None, bias_id=None, bias=None, allow=None):
+        """Penalties [B, 3] (repetition, presence, frequency), biases [B, M] and a grammar's bits [B, N, (V + 31) // 32] (int32) on
+        the logits of a drafted tree; out may be logits (None: it is)."""
+        out = logits if out is None else out
+        M = 0 if bias_id is None else bias_id.shape[1]
+        assert draft_tok.shape == (self.B, self.N) and (count is None or count.shape == (self.B, self.V))
+        assert penalty is None or penalty.shape == (self.B, 3)
+        assert (bias_id is None) == (bias is None) and (bias is None or bias.shape == bias_id.shape == (self.B, M))
+        assert allow is None or allow.shape == (self.B, self.N, (self.V + 31) // 32)
+        self._here(logits, out, draft_tok, count, penalty, bias_id, bias, allow)
+        _check(self._lib.stand_shape_logits(self.h, self._logits_ptr(logits), self._logits_ptr(out), _dptr(draft_tok, torch.int32),
+                                            _dptr(count, torch.int32), _dptr(penalty, torch.float32), _dptr(bias_id, torch.int32),
+                                            _dptr(bias, torch.float32), M, _dptr(allow, torch.int32), self._stream()), self.h)
+        return out
+
+    def count_tokens(self, count, tok, length=None, prompt=False):
+        """Tokens tok [B, any] (the first length[b] of them) into count [B, V]: generated ones, or the prompt's."""
+        assert count.shape == (self.B, self.V) and tok.dim() == 2 and tok.shape[0] == self.B and (length is None or length.shape == (self.B,))
+        self._here(count, tok, length)
+        _check(self._lib.stand_count_tokens(self.h, _dptr(count, torch.int32), _dptr(tok, torch.int32), _dptr(length, torch.int32),
+                                            tok.shape[1], int(prompt), self._stream()), self.h)
 
     def record_slots(self, rows_per_trajectory, orders):
         """Slot of every merge record of the last update, [B, R, orders] (-1: no such record, or dropped)."""

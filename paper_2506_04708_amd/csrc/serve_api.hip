@@ -1,0 +1,201 @@
+// serve_api.hip -- host side of the operators around a verification (include/stand.h): argument checks and launches.
+// Nothing here allocates, waits or keeps state between calls; everything a call needs comes with it.
+#include "../../include/stand.h"
+#include "cache_ops.hpp"
+#include "serve_view.hpp"
+#include "shape_logits.hpp"
+#include "tree_attn.hpp"
+
+#include <cmath>
+
+using namespace stand;
+
+namespace {
+
+// The handle's device is current inside a call and the caller's is again after it.
+struct DeviceScope {
+    int before = -1;
+    hipError_t e;
+    explicit DeviceScope(int device)
+    {
+        e = hipGetDevice(&before);
+        if (e == hipSuccess && before != device) e = hipSetDevice(device);
+        else before = -1;
+    }
+    ~DeviceScope()
+    {
+        if (before >= 0) (void)hipSetDevice(before);
+    }
+};
+
+int launched(const ServeView &v)
+{
+    const hipError_t e = hipGetLastError();
+    if (e == hipSuccess) return STAND_OK;
+    *v.last_hip = (int)e;
+    return STAND_EHIP;
+}
+
+int bad_device(const ServeView &v, hipError_t e)
+{
+    *v.last_hip = (int)e;
+    return STAND_EHIP;
+}
+
+bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
+bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s < ((int64_t)1 << 48); }
+int log2_of(int64_t x)
+{
+    int s = 0;
+    while (((int64_t)1 << s) < x) ++s;
+    return s;
+}
+bool power_of_two(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
+bool page_size_ok(int32_t p) { return power_of_two(p) && p <= STAND_MAX_PAGE; }
+
+bool cache_ok(const stand_cache *c)
+{
+    return c && c->d_k && c->d_v && aligned16(c->d_k) && aligned16(c->d_v) && (c->dtype == STAND_BF16 || c->dtype == STAND_F16) &&
+           c->layers >= 1 && c->pages >= 1 && page_size_ok(c->page_size) && c->kv_heads >= 1 && c->kv_heads <= 4096 &&
+           (c->head_dim == 64 || c->head_dim == 128) && stride_ok(c->layer_stride) && stride_ok(c->page_stride) &&
+           stride_ok(c->slot_stride) && stride_ok(c->head_stride);
+}
+
+bool strides_ok(const int64_t *s) { return stride_ok(s[0]) && stride_ok(s[1]) && stride_ok(s[2]); }
+
+}  // namespace
+
+extern "C" uint64_t stand_tree_attention_work(const stand_handle *h, const stand_cache *cache, int32_t q_heads)
+{
+    if (!h || !cache_ok(cache) || q_heads < 1 || q_heads % cache->kv_heads) return 0;
+    return 16;
+}
+
+extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, int32_t layer, const int32_t *d_len,
+                                    const int32_t *d_table, int32_t table_width, const int32_t *d_draft_tok,
+                                    const stand_tree_rows *rows, void *d_work, uint64_t work_bytes, void *stream)
+{
+    if (!h || !cache_ok(cache) || !rows || !d_len || !d_table || !d_draft_tok || !d_work) return STAND_EINVAL;
+    if (layer < 0 || layer >= cache->layers || table_width < 1) return STAND_EINVAL;
+    if (!rows->d_q || !rows->d_k || !rows->d_v || !rows->d_out) return STAND_EINVAL;
+    if (!aligned16(rows->d_q) || !aligned16(rows->d_k) || !aligned16(rows->d_v) || !aligned16(rows->d_out) || !aligned16(d_work))
+        return STAND_EINVAL;
+    if (!strides_ok(rows->q_stride) || !strides_ok(rows->k_stride) || !strides_ok(rows->v_stride) || !strides_ok(rows->out_stride))
+        return STAND_EINVAL;
+    if (rows->q_heads < 1 || rows->q_heads % cache->kv_heads) return STAND_EINVAL;
+    if (!(rows->scale > 0.0f) || !std::isfinite(rows->scale)) return STAND_EINVAL;
+    if (work_bytes < stand_tree_attention_work(h, cache, rows->q_heads)) return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    if ((int64_t)table_width * cache->page_size > INT32_MAX) return STAND_EINVAL;
+    if (v.B > 65535) return STAND_ELIMIT;
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    TreeAttnArgs a;
+    a.q = (const uint16_t *)rows->d_q; a.k_new = (const uint16_t *)rows->d_k; a.v_new = (const uint16_t *)rows->d_v;
+    a.out = (uint16_t *)rows->d_out;
+    a.k_pool = (const uint16_t *)cache->d_k + layer * cache->layer_stride;
+    a.v_pool = (const uint16_t *)cache->d_v + layer * cache->layer_stride;
+    a.len = d_len; a.table = d_table; a.draft_tok = d_draft_tok; a.anc = v.anc; a.anc_words = v.anc_words;
+    for (int i = 0; i < 3; ++i) {
+        a.qs[i] = rows->q_stride[i]; a.ks[i] = rows->k_stride[i]; a.vs[i] = rows->v_stride[i]; a.os[i] = rows->out_stride[i];
+    }
+    a.pool_page = cache->page_stride; a.pool_slot = cache->slot_stride; a.pool_head = cache->head_stride;
+    a.scale = rows->scale; a.B = v.B; a.N = v.N; a.q_heads = rows->q_heads; a.kv_heads = cache->kv_heads;
+    a.width = table_width; a.pages = cache->pages; a.page_shift = log2_of(cache->page_size); a.f16 = cache->dtype == STAND_F16;
+    const dim3 grid((unsigned)a.q_heads, (unsigned)v.N, (unsigned)v.B);
+    if (cache->head_dim == 64) tree_attn_kernel<64><<<grid, dim3(256), 0, (hipStream_t)stream>>>(a);
+    else tree_attn_kernel<128><<<grid, dim3(256), 0, (hipStream_t)stream>>>(a);
+    return launched(v);
+}
+
+extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots,
+                                  int32_t width, const int32_t *d_row, const int32_t *d_count, void *stream)
+{
+    if (!h || !cache_ok(cache) || !rows || !rows->d_k || !rows->d_v || !d_slots || width < 1 || rows->rows < 1) return STAND_EINVAL;
+    if (!aligned16(rows->d_k) || !aligned16(rows->d_v)) return STAND_EINVAL;
+    if (!stride_ok(rows->layer_stride) || !stride_ok(rows->batch_stride) || !stride_ok(rows->row_stride) || !stride_ok(rows->head_stride))
+        return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    CommitArgs a;
+    a.words = cache->head_dim / 8;
+    a.heads = cache->kv_heads;
+    // a workgroup copies at least four words a thread, where there are as many
+    const int row_words = a.heads * a.words;
+    a.per_group = (1024 + row_words - 1) / row_words;
+    const int64_t groups = (width + (int64_t)a.per_group - 1) / a.per_group;
+    if (v.B > 65535 || cache->layers > 65535 || groups * 256 > UINT32_MAX) return STAND_ELIMIT;
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    a.k_rows = (const uint4 *)rows->d_k; a.v_rows = (const uint4 *)rows->d_v;
+    a.k_pool = (uint4 *)cache->d_k; a.v_pool = (uint4 *)cache->d_v;
+    a.slots = d_slots; a.row = d_row; a.count = d_count;
+    a.src_layer = rows->layer_stride / 8; a.src_batch = rows->batch_stride / 8; a.src_row = rows->row_stride / 8; a.src_head = rows->head_stride / 8;
+    a.pool_layer = cache->layer_stride / 8; a.pool_page = cache->page_stride / 8; a.pool_slot = cache->slot_stride / 8;
+    a.pool_head = cache->head_stride / 8;
+    a.page_shift = log2_of(cache->page_size);
+    a.slot_count = (long long)cache->pages << a.page_shift;
+    a.B = v.B; a.rows = rows->rows; a.width = width;
+    cache_commit_kernel<<<dim3((unsigned)groups, (unsigned)v.B, (unsigned)cache->layers), dim3(256), 0, (hipStream_t)stream>>>(a);
+    return launched(v);
+}
+
+extern "C" int stand_cache_pages(stand_handle *h, const stand_pages *p, const int32_t *d_add, const int32_t *d_room, int64_t *d_slots,
+                                 int32_t slot_width, int32_t *d_missing, const stand_pages *out, void *stream)
+{
+    if (!h || !p || !out || !p->d_table || !p->d_ring || !p->d_length || !p->d_held || !p->d_mark || !d_missing) return STAND_EINVAL;
+    if (!out->d_length || !out->d_held || !out->d_mark) return STAND_EINVAL;
+    if (out->d_table != p->d_table || out->d_ring != p->d_ring || out->width != p->width || out->pages != p->pages || out->page_size != p->page_size)
+        return STAND_EINVAL;
+    if (p->width < 1 || p->pages < 1 || !page_size_ok(p->page_size) || slot_width < 0 || (slot_width > 0 && !d_slots)) return STAND_EINVAL;
+    if ((int64_t)p->width * p->page_size > INT32_MAX) return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    PagesArgs a;
+    a.table = p->d_table; a.ring = p->d_ring; a.length = p->d_length; a.held = p->d_held; a.add = d_add; a.room = d_room;
+    a.mark = (const long long *)p->d_mark;
+    a.length_out = out->d_length; a.held_out = out->d_held; a.missing = d_missing; a.mark_out = (long long *)out->d_mark;
+    a.slots = (long long *)d_slots;
+    a.B = v.B; a.width = p->width; a.pages = p->pages; a.page_shift = log2_of(p->page_size); a.slot_width = slot_width;
+    a.default_room = v.D + 1;
+    cache_pages_kernel<<<dim3(1), dim3(kPagesThreads), 0, (hipStream_t)stream>>>(a);
+    return launched(v);
+}
+
+extern "C" int stand_shape_logits(stand_handle *h, const void *d_logits, void *d_out, const int32_t *d_draft_tok, const int32_t *d_count,
+                                  const float *d_penalty, const int32_t *d_bias_id, const float *d_bias, int32_t bias_width,
+                                  const uint32_t *d_allow, void *stream)
+{
+    if (!h || !d_logits || !d_out || !d_draft_tok || bias_width < 0 || (bias_width > 0 && (!d_bias_id || !d_bias))) return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    const bool f32 = v.logits_dtype == STAND_F32;
+    if (((uintptr_t)d_logits | (uintptr_t)d_out) & (f32 ? 3u : 1u)) return STAND_EINVAL;
+    ShapeArgs a;
+    a.x = d_logits; a.out = d_out; a.draft_tok = d_draft_tok; a.count = d_count; a.penalty = d_penalty; a.bias_id = d_bias_id; a.bias = d_bias;
+    a.allow = d_allow; a.anc = v.anc; a.anc_words = v.anc_words; a.N = v.N; a.V = v.V; a.M = bias_width; a.words = (v.V + 31) / 32;
+    const int64_t spans = ((int64_t)v.V + kShapeSpan - 1) / kShapeSpan;
+    // nodes that share a workgroup's counts: as many as leave 2048 workgroups, at most 16
+    a.nodes_per_group = 16;
+    while (a.nodes_per_group > 1 && spans * v.B * ((v.N + a.nodes_per_group - 1) / a.nodes_per_group) < 2048) a.nodes_per_group /= 2;
+    a.node_groups = (v.N + a.nodes_per_group - 1) / a.nodes_per_group;
+    if (v.B > 65535 || spans * a.node_groups * kShapeThreads > UINT32_MAX) return STAND_ELIMIT;
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    const dim3 grid((unsigned)(spans * a.node_groups), (unsigned)v.B);
+    if (f32) shape_logits_kernel<kDtF32><<<grid, dim3(kShapeThreads), 0, (hipStream_t)stream>>>(a);
+    else shape_logits_kernel<kDtBf16><<<grid, dim3(kShapeThreads), 0, (hipStream_t)stream>>>(a);
+    return launched(v);
+}
+
+extern "C" int stand_count_tokens(stand_handle *h, int32_t *d_count, const int32_t *d_tok, const int32_t *d_len, int32_t width,
+                                  int32_t prompt, void *stream)
+{
+    if (!h || !d_count || !d_tok || width < 1) return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    const int64_t groups = ((int64_t)width + 255) / 256;
+    if (v.B > 65535) return STAND_ELIMIT;
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    count_tokens_kernel<<<dim3((unsigned)groups, (unsigned)v.B), dim3(256), 0, (hipStream_t)stream>>>(d_count, d_tok, d_len, v.V, width, prompt);
+    return launched(v);
+}

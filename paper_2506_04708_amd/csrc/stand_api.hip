@@ -3,6 +3,7 @@
 // kernels.hpp.  No CPU fallback exists: every step of the path runs in the HIP kernels.
 #include "../../include/stand.h"
 #include "kernels.hpp"
+#include "serve_view.hpp"
 
 #include <algorithm>
 #include <cmath>
@@ -1382,3 +1383,8 @@ extern "C" const char *stand_strerror(int code)
 }
 
 extern "C" int stand_last_hip_error(const stand_handle *h) { return h ? h->last_hip : 0; }
+
+stand::ServeView stand::serve_view(stand_handle *h)
+{
+    return ServeView{h->B, h->N, h->D, h->V, h->cfg.logits_dtype, h->cfg.device, h->anc, h->anc_words, &h->last_hip};
+}
