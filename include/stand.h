@@ -373,7 +373,7 @@ int stand_read_rows(const void *d_src, uint64_t row_bytes, uint64_t rows, uint32
  *
  * The calls take tree, batch, vocabulary, type of the logits and device from the handle, read nothing else of it and change
  * nothing in it; they allocate nothing, keep nothing, and may be captured into a graph.  The caller's current device is
- * the same after a call.  Up to 65 535 trajectories (STAND_ELIMIT above).
+ * the same after a call.  Up to 65 535 trajectories, 4096 for the attention (STAND_ELIMIT above).
  *
  * Trees: the root's keys and values are those of the last committed token, which is not in the cache yet: a cache of n
  * tokens holds the positions 0 .. n-1 and node u stands at position n + depth(u) (stand_tree_packing's d_pos).  The rows of
@@ -381,6 +381,7 @@ int stand_read_rows(const void *d_src, uint64_t row_bytes, uint64_t rows, uint32
 
 #define STAND_F16 2         /* binary16: caches only, not logits */
 #define STAND_MAX_PAGE 4096 /* tokens of a page, a power of two */
+#define STAND_MAX_CACHED (1 << 30) /* tokens that a row of a block table covers */
 
 /* A paged cache: element e of head g at place s of page p in layer l is d_k[l * layer_stride + p * page_stride + s * slot_stride
  * + g * head_stride + e], d_v likewise.  Strides are in elements, not negative and multiples of 8; pointers are 16-byte aligned.
@@ -412,7 +413,7 @@ typedef struct {
  * the mask of stand_tree_packing beside the cache.  Nodes that were not drafted get zeros; what stands in their rows, in
  * rows off a node's path and behind a length is never used, whatever it is (a NaN included).  d_draft_tok [B][N] is what
  * stand_draft / stand_step gave.  Token t of trajectory b is in page d_table[b][t / page_size], d_table: [B][table_width].
- * A length below 0 counts as 0, one above table_width * page_size (at most 2^31 - 1) as that; a page outside the cache is never
+ * A length below 0 counts as 0, one above table_width * page_size (at most STAND_MAX_CACHED) as that; a page outside the cache is never
  * read (what is read instead is not specified).  A tree of one node is the ordinary attention of single tokens.
  *   Products are summed in fp32, the weights p are rounded to the cache's type for the product with the values (relative error
  * 2^-9 in bf16, 2^-12 in fp16 each, at most half a step) and summed as rounded; the result is rounded once.
@@ -448,7 +449,7 @@ typedef struct {
     int32_t *d_length;      /* [B] tokens in the cache */
     int32_t *d_held;        /* [B] pages of the trajectory */
     int64_t *d_mark;        /* [2] {taken, given}, only grow */
-    int32_t width, pages, page_size; /* width * page_size < 2^31 */
+    int32_t width, pages, page_size; /* width * page_size <= STAND_MAX_CACHED */
 } stand_pages;
 
 /* Moves lengths on and sees that there is room for the next tokens.  For each trajectory

@@ -1,0 +1,43 @@
+// attn_plan.hpp -- how stand_tree_attention's work is cut, the same on the host, in its two kernels and in tests.
+//
+// A unit is one stage of keys for one tile of query rows and one key/value head.  The units of all trajectories stand in one
+// row; W workgroups take equal shares of it, so that trajectories of any lengths keep the whole chip busy.  A share that ends
+// inside an item (a trajectory's tile of rows of one head) leaves a part of its sums, which a second kernel joins.
+#pragma once
+#include <stdint.h>
+
+#if defined(__HIPCC__)
+#define STAND_BOTH __host__ __device__ __forceinline__
+#else
+#define STAND_BOTH inline
+#endif
+
+namespace stand {
+
+constexpr int kAttnMaxBatch = 4096;   // trajectories of a call: their unit sums are made in LDS
+constexpr int kAttnMinUnits = 2;      // a share is no smaller: a part costs about as much as a unit to write and join
+
+STAND_BOTH long long clamp_length(long long len, long long most) { return len < 0 ? 0 : (len > most ? most : len); }
+STAND_BOTH int clamp_page(int page, int pages) { return page < 0 ? 0 : (page >= pages ? pages - 1 : page); }
+
+// Units of one item: its cached keys, then the tree's nodes.
+STAND_BOTH long long item_units(long long len, long long most, int nodes_of_tree, int keys)
+{
+    return (clamp_length(len, most) + keys - 1) / keys + (nodes_of_tree + keys - 1) / keys;
+}
+// Items of a trajectory with `drafted` nodes: per_kv query heads share a key/value head, a tile has `tile_rows` rows.
+STAND_BOTH int tree_items(int drafted, int per_kv, int kv_heads, int tile_rows)
+{
+    return (drafted * per_kv + tile_rows - 1) / tile_rows * kv_heads;
+}
+// Workgroups that get a share, of `groups` launched.
+STAND_BOTH long long attn_groups(long long total, int groups)
+{
+    const long long w = (total + kAttnMinUnits - 1) / kAttnMinUnits;
+    return w < groups ? w : groups;
+}
+STAND_BOTH long long group_start(long long w, long long total, long long W) { return w * total / W; }
+// The workgroup whose share holds a unit: the last one that starts at or before it.
+STAND_BOTH long long group_of(long long unit, long long total, long long W) { return ((unit + 1) * W - 1) / total; }
+
+}  // namespace stand

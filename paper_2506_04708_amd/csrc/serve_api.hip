@@ -6,6 +6,7 @@
 #include "shape_logits.hpp"
 #include "tree_attn.hpp"
 
+#include <algorithm>
 #include <cmath>
 
 using namespace stand;
@@ -65,10 +66,66 @@ bool strides_ok(const int64_t *s) { return stride_ok(s[0]) && stride_ok(s[1]) &&
 
 }  // namespace
 
+namespace {
+
+// The form of the attention kernel a call takes, by the rows that share a key/value head.
+enum AttnForm { kAttn32, kAttn64, kAttn128, kAttn256 };
+AttnForm attn_form(int64_t rows) { return rows <= 32 ? kAttn32 : rows <= 64 ? kAttn64 : rows <= 128 ? kAttn128 : kAttn256; }
+
+template <int D, bool F16, typename Call>
+auto with_attn_shape(AttnForm f, Call call)
+{
+    switch (f) {
+    case kAttn32: return call(AttnShape<D, F16, 1, 4, 1>{});
+    case kAttn64: return call(AttnShape<D, F16, 2, 2, 1>{});
+    case kAttn128: return call(AttnShape<D, F16, 4, 2, 1>{});
+    default: return call(AttnShape<D, F16, 8, 1, 2>{});
+    }
+}
+template <typename Call>
+auto with_attn_shape(int head_dim, bool f16, AttnForm f, Call call)
+{
+    if (head_dim == 64) return f16 ? with_attn_shape<64, true>(f, call) : with_attn_shape<64, false>(f, call);
+    return f16 ? with_attn_shape<128, true>(f, call) : with_attn_shape<128, false>(f, call);
+}
+
+// Workgroups launched: as many as the device holds at once, a multiple of its eight XCDs.
+template <typename S>
+int attn_launch_groups(int cus)
+{
+    const int per_cu = std::max(1, std::min(160 * 1024 / S::BYTES, 8 / S::WAVES));
+    return std::max(8, cus * per_cu / 8 * 8);
+}
+template <typename S>
+uint64_t attn_part_bytes(int cus)
+{
+    return (uint64_t)2 * attn_launch_groups<S>(cus) * S::TM * (S::D + 2) * 4;
+}
+uint64_t attn_prefix_bytes(int B) { return (8 * ((uint64_t)B + 1) + 255) / 256 * 256; }
+
+template <typename S>
+hipError_t attn_launch(TreeAttnArgs &a, int cus, hipStream_t s)
+{
+    static_assert(S::BYTES <= 160 * 1024, "LDS of a compute unit");
+    a.groups = attn_launch_groups<S>(cus);
+    // (above 64 KiB dynamic LDS has to be asked for, once per device; the call is cheap and says so of any later one)
+    const hipError_t e = hipFuncSetAttribute((const void *)tree_attn_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
+    if (e != hipSuccess) return e;
+    tree_attn_kernel<S><<<dim3((unsigned)a.groups), dim3(S::THREADS), S::BYTES, s>>>(a);
+    const int heads = a.kv_heads * a.per_kv, rows = a.B * a.N;
+    const int along = std::max(1, std::min((heads + 3) / 4, 2048 / rows));
+    tree_attn_join_kernel<S::D, S::TM, S::KT, S::F16><<<dim3((unsigned)rows, (unsigned)along), dim3(256), 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace
+
 extern "C" uint64_t stand_tree_attention_work(const stand_handle *h, const stand_cache *cache, int32_t q_heads)
 {
     if (!h || !cache_ok(cache) || q_heads < 1 || q_heads % cache->kv_heads) return 0;
-    return 16;
+    const ServeView v = serve_view(const_cast<stand_handle *>(h));
+    const AttnForm f = attn_form((int64_t)v.N * (q_heads / cache->kv_heads));
+    return attn_prefix_bytes(v.B) + with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, f, [&](auto s) { return attn_part_bytes<decltype(s)>(v.cus); });
 }
 
 extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, int32_t layer, const int32_t *d_len,
@@ -86,8 +143,8 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     if (!(rows->scale > 0.0f) || !std::isfinite(rows->scale)) return STAND_EINVAL;
     if (work_bytes < stand_tree_attention_work(h, cache, rows->q_heads)) return STAND_EINVAL;
     const ServeView v = serve_view(h);
-    if ((int64_t)table_width * cache->page_size > INT32_MAX) return STAND_EINVAL;
-    if (v.B > 65535) return STAND_ELIMIT;
+    if ((int64_t)table_width * cache->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
+    if (v.B > kAttnMaxBatch || rows->q_heads > 65535) return STAND_ELIMIT;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
     TreeAttnArgs a;
@@ -95,17 +152,20 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     a.out = (uint16_t *)rows->d_out;
     a.k_pool = (const uint16_t *)cache->d_k + layer * cache->layer_stride;
     a.v_pool = (const uint16_t *)cache->d_v + layer * cache->layer_stride;
-    a.len = d_len; a.table = d_table; a.draft_tok = d_draft_tok; a.anc = v.anc; a.anc_words = v.anc_words;
+    a.len = d_len; a.table = d_table; a.draft_tok = d_draft_tok;
+    a.anc = (const uint32_t *)v.anc; a.anc_words = 2 * v.anc_words;      // (little endian: words of 32 nodes)
+    a.prefix = (long long *)d_work; a.part = (float *)((char *)d_work + attn_prefix_bytes(v.B));
     for (int i = 0; i < 3; ++i) {
         a.qs[i] = rows->q_stride[i]; a.ks[i] = rows->k_stride[i]; a.vs[i] = rows->v_stride[i]; a.os[i] = rows->out_stride[i];
     }
     a.pool_page = cache->page_stride; a.pool_slot = cache->slot_stride; a.pool_head = cache->head_stride;
-    a.scale = rows->scale; a.B = v.B; a.N = v.N; a.q_heads = rows->q_heads; a.kv_heads = cache->kv_heads;
-    a.width = table_width; a.pages = cache->pages; a.page_shift = log2_of(cache->page_size); a.f16 = cache->dtype == STAND_F16;
-    const dim3 grid((unsigned)a.q_heads, (unsigned)v.N, (unsigned)v.B);
-    if (cache->head_dim == 64) tree_attn_kernel<64><<<grid, dim3(256), 0, (hipStream_t)stream>>>(a);
-    else tree_attn_kernel<128><<<grid, dim3(256), 0, (hipStream_t)stream>>>(a);
-    return launched(v);
+    a.scale = rows->scale; a.B = v.B; a.N = v.N; a.kv_heads = cache->kv_heads; a.per_kv = rows->q_heads / cache->kv_heads;
+    a.width = table_width; a.pages = cache->pages; a.page_shift = log2_of(cache->page_size);
+    const hipError_t e = with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, attn_form((int64_t)v.N * a.per_kv),
+                                         [&](auto s) { return attn_launch<decltype(s)>(a, v.cus, (hipStream_t)stream); });
+    if (e == hipSuccess) return STAND_OK;
+    *v.last_hip = (int)e;
+    return STAND_EHIP;
 }
 
 extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots,
@@ -147,7 +207,7 @@ extern "C" int stand_cache_pages(stand_handle *h, const stand_pages *p, const in
     if (out->d_table != p->d_table || out->d_ring != p->d_ring || out->width != p->width || out->pages != p->pages || out->page_size != p->page_size)
         return STAND_EINVAL;
     if (p->width < 1 || p->pages < 1 || !page_size_ok(p->page_size) || slot_width < 0 || (slot_width > 0 && !d_slots)) return STAND_EINVAL;
-    if ((int64_t)p->width * p->page_size > INT32_MAX) return STAND_EINVAL;
+    if ((int64_t)p->width * p->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
     const ServeView v = serve_view(h);
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);

@@ -7,7 +7,7 @@ struct stand_handle;
 namespace stand {
 
 struct ServeView {
-    int B, N, D, V, logits_dtype, device;
+    int B, N, D, V, logits_dtype, device, cus;
     const unsigned long long *anc;  // device, [N][anc_words]: ancestor-or-self bit sets of the tree
     int anc_words;
     int *last_hip;                  // where a HIP error of a call is kept

@@ -1386,5 +1386,5 @@ extern "C" int stand_last_hip_error(const stand_handle *h) { return h ? h->last_
 
 stand::ServeView stand::serve_view(stand_handle *h)
 {
-    return ServeView{h->B, h->N, h->D, h->V, h->cfg.logits_dtype, h->cfg.device, h->anc, h->anc_words, &h->last_hip};
+    return ServeView{h->B, h->N, h->D, h->V, h->cfg.logits_dtype, h->cfg.device, h->cus, h->anc, h->anc_words, &h->last_hip};
 }
