@@ -15,6 +15,7 @@
 namespace stand {
 
 constexpr int kAttnMaxBatch = 4096;   // trajectories of a call: their unit sums are made in LDS
+constexpr int kAttnMaxGroups = 2048;  // workgroups of a launch: their records are summed up in LDS
 constexpr int kAttnMinUnits = 2;      // a share is no smaller: a part costs about as much as a unit to write and join
 
 STAND_BOTH long long clamp_length(long long len, long long most) { return len < 0 ? 0 : (len > most ? most : len); }

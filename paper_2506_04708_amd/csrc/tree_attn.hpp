@@ -8,12 +8,17 @@
 
 namespace stand {
 
+// What the workgroup leaves whose share begins inside an item that the one before it began: who has the parts.
+struct JoinRecord { int first, last, rows, unused; };
+
 struct TreeAttnArgs {
     const uint16_t *q, *k_new, *v_new, *k_pool, *v_pool;
     uint16_t *out;
     const int32_t *len, *table, *draft_tok;
     const uint32_t *anc;                             // [N][anc_words] bit sets in 32-bit words
-    long long *prefix;                               // workspace: [B + 1] units before each trajectory
+    long long *total;                                // workspace: units of the call
+    JoinRecord *join;                                // workspace: [groups], then the rows' places in out, [groups][rows of a tile]
+    long long *place;
     float *part;                                     // workspace: [2 * groups][rows of a tile][D + 2]
     long long qs[3], ks[3], vs[3], os[3];            // batch, node, head strides in elements
     long long pool_page, pool_slot, pool_head;
@@ -30,6 +35,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) short4v lds_short4v;
+typedef __attribute__((address_space(3))) uint4v lds_uint4v;
 typedef __attribute__((address_space(3))) char lds_char;
 
 extern __shared__ __attribute__((aligned(16))) char attn_lds[];
@@ -105,14 +111,16 @@ struct AttnShape {
     static constexpr int ROW = 2 * D;                  // bytes of a key
     static constexpr int CPR = D / 8;                  // 16-byte chunks of a key
     static constexpr int KPI = 64 / CPR;               // keys of one copy instruction
-    static constexpr int KW = KT / WAVES;              // keys that a wave loads per stage
+    static constexpr int LOADERS = WAVES >= 8 ? 8 : WAVES;  // waves that load
+    static constexpr int KW = KT / LOADERS;            // keys that each of them loads per stage
     static constexpr int COPIES = 2 * KW / KPI;
     static constexpr int STAGE = 2 * KT * ROW;
-    static constexpr int IDS = NBUF * STAGE;           // LDS: stages | page ids [4][WAVES][64] | node list | scratch
-    static constexpr int LIST = IDS + 4 * WAVES * 256;
+    static constexpr int IDS = NBUF * STAGE;           // LDS: stages | page ids [4][LOADERS][64] | node list | scratch
+    static constexpr int LIST = IDS + 4 * LOADERS * 256;
     static constexpr int MISC = LIST + 2048;
     static constexpr int BYTES = MISC + 256;
-    static_assert(KW % KPI == 0 && (KPI <= KW), "a copy instruction brings whole keys of one wave");
+    static_assert(KW % KPI == 0 && KW >= KPI && KW <= 64, "a copy instruction brings whole keys of one wave");
+    static_assert(!ALONE || LOADERS == WAVES, "every wave loads for itself");
     static_assert((WK - 1) * TM * (D + 2) * 4 <= NBUF * STAGE, "parts of the key waves are joined in the stages' memory");
     static_assert(8 * (kAttnMaxBatch + 1) <= NBUF * STAGE, "unit sums are made in the stages' memory");
     // 16-byte chunk c of key k stands at chunk c ^ swizzle(k): reads of one chunk of 16 keys (K) and of four chunks of four
@@ -169,8 +177,12 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
     long long *sums = (long long *)attn_lds;
     unit_sums<TM, KT, S::THREADS>(a, sums);
     const long long total = sums[a.B];
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= a.B; b += S::THREADS) a.prefix[b] = sums[b];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.total = total;
+    // rows of nodes that were not drafted
+    for (int r = blockIdx.x; r < a.B * a.N; r += a.groups)
+        if (a.draft_tok[r] < 0)
+            for (int i = threadIdx.x; i < a.kv_heads * a.per_kv * S::CPR; i += S::THREADS)
+                *(uint4v *)(a.out + (r / a.N) * a.os[0] + (r % a.N) * a.os[1] + (i / S::CPR) * a.os[2] + i % S::CPR * 8) = uint4v{0, 0, 0, 0};
     const long long W = attn_groups(total, a.groups);
     // neighbours in the order of the work share an XCD (workgroups go round the eight of them in turn) and so its L2
     const int per_xcd = (int)((W + 7) / 8);
@@ -190,6 +202,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
     }
     long long b_start = sums[b];
     int listed = -1, nodes = 0;
+    bool first_item = true;
     const float c = a.scale * 1.4426950408889634f;
     // weights are at most 2^8 (where the running maximum is left behind); fp16 ones are scaled up so that few are subnormal
     constexpr float kUp = S::F16 ? 6.0f : 0.0f;
@@ -221,6 +234,14 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
         const long long item_start = b_start + (long long)item * per_item;
         const int u0 = (int)(unit - item_start);
         const int u1 = (int)(unit_end - item_start < per_item ? unit_end - item_start : per_item);
+        bool leads = false;                            // this share is the second one of its first item
+        if (first_item) {
+            first_item = false;
+            const long long from = group_of(item_start, total, W);
+            leads = u0 > 0 && from == w - 1;
+            if (threadIdx.x == 0)
+                a.join[w] = JoinRecord{(int)from, (int)group_of(item_start + per_item - 1, total, W), leads ? min(TM, nodes * a.per_kv - tile * TM) : 0, 0};
+        }
         const int rows = nodes * a.per_kv, row = tile * TM + wr * 32 + col;
         const bool busy = tile * TM + wr * 32 < rows;  // this wave has rows
         const int my_row = row < rows ? row : rows - 1;
@@ -231,186 +252,207 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
             const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2] + 8 * half;
 #pragma unroll
             for (int i = 0; i < DC; ++i) q[i] = *(const uint4v *)(qp + 16 * i);
+            // the wait for them belongs here: in the loop it would be one for the copies in flight as well
+#pragma unroll
+            for (int i = 0; i < DC; ++i) asm volatile("" : "+v"(q[i]));
         }
         float16v o[DT];
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = float16v{0};
         float m = -1e38f, l = 0.0f;                    // running maximum (scaled scores, base 2) and sum of the weights
 
-        // addresses of this lane's fragments inside a stage
-        uint32_t ka[DC], va[DT];
-#pragma unroll
-        for (int i = 0; i < DC; ++i) ka[i] = lds0 + (wk * SUB * 32 + col) * S::ROW + (((2 * i + half) ^ S::swizzle_k(col)) << 4);
-        {
-            const int piece = lane & 3, j = (lane >> 2) & 3, dsub = (lane >> 4) & 1;
-#pragma unroll
-            for (int i = 0; i < DT; ++i)
-                va[i] = lds0 + KT * S::ROW + (wk * SUB * 32 + 4 * half + j) * S::ROW +
-                        (((4 * i + 2 * dsub + (piece >> 1)) ^ S::swizzle_v(j)) << 4) + (piece & 1) * 8;
-        }
+        // this lane's first fragments inside a stage (chunk 0 of the keys, elements 0 .. 31 of the values); the others differ
+        // in address bits that the swizzle only flips
+        const uint32_t k_at = lds0 + (wk * SUB * 32 + col) * S::ROW + ((half ^ S::swizzle_k(col)) << 4);
+        const int piece = lane & 3, j4 = (lane >> 2) & 3, dsub = (lane >> 4) & 1;
+        const uint32_t v_at = lds0 + KT * S::ROW + (wk * SUB * 32 + 4 * half + j4) * S::ROW +
+                              (((2 * dsub + (piece >> 1)) ^ S::swizzle_v(j4)) << 4) + (piece & 1) * 8;
 
-        // one stage: scores, weights, products with the values; keys of which `seen` (nullptr: all of them) says nothing are left out
-        auto stage = [&](uint32_t off, auto masked, const uint32_t (&word)[SUB]) {
-            float16v s[SUB];
-#pragma unroll
-            for (int t = 0; t < SUB; ++t) {
-                s[t] = float16v{0};
-#pragma unroll
-                for (int i = 0; i < DC; ++i) {
-                    const uint4v kf = *(const __attribute__((address_space(3))) uint4v *)(uintptr_t)(ka[i] + off + t * 32 * S::ROW);
-                    s[t] = mfma32<S::F16>(kf, q[i], s[t]);
-                }
-            }
-            if constexpr (decltype(masked)::value) {
-#pragma unroll
-                for (int t = 0; t < SUB; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) s[t][i] = (word[t] >> (8 * (i / 4) + i % 4 + 4 * half)) & 1u ? s[t][i] : -__builtin_huge_valf();
-            }
-            float top = s[0][0];
-#pragma unroll
-            for (int t = 0; t < SUB; ++t)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) top = fmaxf(top, s[t][i]);
-            top = other_half_max(top) * c;
-            if (__ballot(top > m + 8.0f)) {            // seldom after the first stages: the old maximum will do
-                const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - next);
-                m = next;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) o[d][i] *= f;
-            }
-            const float shift = kUp - m;
-#pragma unroll
-            for (int t = 0; t < SUB; ++t) {
-                uint32_t p[8];
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    p[i] = pack2<S::F16>(__builtin_amdgcn_exp2f(fmaf(s[t][2 * i], c, shift)), __builtin_amdgcn_exp2f(fmaf(s[t][2 * i + 1], c, shift)));
-                    l = add2<S::F16>(p[i], l);
-                }
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint4v pf = {p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]};
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) {
-                        const uint32_t at = va[d] + off + (t * 32 + 16 * k) * S::ROW;
-                        const short4v v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
-                        const short4v v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
-                        const short vf[8] __attribute__((aligned(16))) = {v0[0], v0[1], v0[2], v0[3], v1[0], v1[1], v1[2], v1[3]};
-                        o[d] = mfma32<S::F16>(__builtin_bit_cast(uint4v, vf), pf, o[d]);
-                    }
-                }
-            }
+        // ---- the units of this share: cached keys, then the tree's nodes; copies two stages ahead, page numbers two further ----
+        const int n = u1 - u0, cached = cache_units - u0;       // units, those (if any) of the cache
+        const int32_t *table = a.table + (long long)b * a.width;
+        const int share = wave * S::KW;                         // this wave's keys of a stage (ALONE: those it uses)
+        auto load_ids = [&](int i) {
+            int key = (u0 + i) * KT + share + lane % S::KW;
+            key = key < len ? key : len - 1;
+            key = key > 0 ? key : 0;
+            copy4_async(table + (key >> a.page_shift), __builtin_amdgcn_readfirstlane(lds0 + S::IDS + wave * 256 + (i & 3) * (S::LOADERS * 256)));
         };
-
-        // ---- cached keys: copies two stages ahead, their page numbers two further ----
-        const int n = (u1 < cache_units ? u1 : cache_units) - u0;
-        if (n > 0) {
-            const int32_t *table = a.table + (long long)b * a.width;
-            const uint32_t ids = lds0 + S::IDS + wave * 256;
-            const int share = wave * S::KW;            // this wave's keys of a stage (ALONE: those it uses)
-            auto load_ids = [&](int i) {
-                int key = (u0 + i) * KT + share + lane % S::KW;
-                key = key < len ? key : len - 1;
-                copy4_async(table + (key >> a.page_shift), __builtin_amdgcn_readfirstlane(ids + (i & 3) * (S::WAVES * 256)));
-            };
-            auto load_stage = [&](int i) {
-                const uint32_t buf = lds0 + (i % S::NBUF) * S::STAGE + share * S::ROW;
-                const int32_t *id = (const int32_t *)(attn_lds + S::IDS + (i & 3) * (S::WAVES * 256) + wave * 256);
+        auto load_stage = [&](int i) {
+            const uint32_t buf = lds0 + (i % S::NBUF) * S::STAGE + share * S::ROW;
+            const int32_t *id = (const int32_t *)(attn_lds + S::IDS + (i & 3) * (S::LOADERS * 256) + wave * 256);
+            const int ch = lane % S::CPR;
 #pragma unroll
-                for (int r = 0; r < S::KW / S::KPI; ++r) {
-                    const int at = r * S::KPI + lane / S::CPR, in_stage = share + at;
+            for (int r = 0; r < S::KW / S::KPI; ++r) {
+                const int at = r * S::KPI + lane / S::CPR, in_stage = share + at;
+                const uint16_t *kp, *vp;
+                if (i < cached) {
                     int key = (u0 + i) * KT + in_stage;
-                    key = key < len ? key : len - 1;   // behind the end: the last key again, weighted with zero
+                    key = key < len ? key : len - 1;            // behind the end: the last key again, weighted with zero
                     const long long page = clamp_page(id[at], a.pages);
                     const long long from = page * a.pool_page + (key & ((1 << a.page_shift) - 1)) * a.pool_slot + hk * a.pool_head;
-                    const int ch = lane % S::CPR;
-                    copy16_async(a.k_pool + from + ((ch ^ S::swizzle_k(in_stage)) << 3), __builtin_amdgcn_readfirstlane(buf + r * S::KPI * S::ROW));
-                    copy16_async(a.v_pool + from + ((ch ^ S::swizzle_v(in_stage)) << 3), __builtin_amdgcn_readfirstlane(buf + KT * S::ROW + r * S::KPI * S::ROW));
+                    kp = a.k_pool + from;
+                    vp = a.v_pool + from;
+                } else {
+                    int v = (i - cached) * KT + in_stage;
+                    v = v < a.N ? v : a.N - 1;
+                    kp = a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2];
+                    vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2];
                 }
-            };
+                copy16_async(kp + ((ch ^ S::swizzle_k(in_stage)) << 3), __builtin_amdgcn_readfirstlane(buf + r * S::KPI * S::ROW));
+                copy16_async(vp + ((ch ^ S::swizzle_v(in_stage)) << 3), __builtin_amdgcn_readfirstlane(buf + KT * S::ROW + r * S::KPI * S::ROW));
+            }
+        };
+        const bool loads = wave < S::LOADERS;
+        if (loads) {
             load_ids(0); load_ids(1); load_ids(2);
             wait_loads<0>();
             load_stage(0);
             if (n > 1) { load_ids(3); load_stage(1); }
-            for (int i = 0; i < n; ++i) {
-                if (i + 1 < n) wait_loads<S::COPIES + 1>();
-                else wait_loads<0>();
-                if constexpr (!S::ALONE) {
-                    group_barrier();                   // everyone's copies are there, and everyone is done with the stage before
-                    if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
-                }
-                const uint32_t off = (i % S::NBUF) * S::STAGE;
-                if (busy) {
-                    const int left = len - (u0 + i) * KT - wk * SUB * 32;
-                    uint32_t word[SUB];
-#pragma unroll
-                    for (int t = 0; t < SUB; ++t) word[t] = left >= 32 * (t + 1) ? ~0u : (left <= 32 * t ? 0u : (1u << (left - 32 * t)) - 1u);
-                    if (left >= 32 * SUB) stage(off, std::false_type{}, word);
-                    else if (left > 0) stage(off, std::true_type{}, word);
-                }
-                if constexpr (S::ALONE) {
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
-                }
-            }
         }
-
-        // ---- the tree's own keys: a node sees its ancestors and itself ----
-        for (int un = u0 > cache_units ? u0 : cache_units; un < u1; ++un) {
-            const int v0 = (un - cache_units) * KT;    // first node of the unit
-            uint32_t *odd = (uint32_t *)(attn_lds + S::MISC);   // [KT / 32] nodes with a value that is no finite number
-            __syncthreads();
-            if (threadIdx.x < KT / 32) odd[threadIdx.x] = 0;
-            __syncthreads();
-            for (int i = threadIdx.x; i < KT * S::CPR; i += S::THREADS) {
-                const int key = i / S::CPR, ch = i % S::CPR, v = v0 + key;
-                uint4v kw = {0, 0, 0, 0}, vw = {0, 0, 0, 0};
-                if (v < a.N && a.draft_tok[(long long)b * a.N + v] >= 0) {
-                    kw = *(const uint4v *)(a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2] + 8 * ch);
-                    vw = *(const uint4v *)(a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2] + 8 * ch);
-                    constexpr uint32_t kExp = S::F16 ? 0x7C00u : 0x7F80u;
-                    bool any = false;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {      // 0 * infinity would reach the rows that do not see this node
-                        const bool lo = (vw[e] & kExp) == kExp, hi = ((vw[e] >> 16) & kExp) == kExp;
-                        any |= lo | hi;
-                        vw[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-                    }
-                    if (any) atomicOr(&odd[key / 32], 1u << (key & 31));
-                }
-                *(uint4v *)(attn_lds + key * S::ROW + ((ch ^ S::swizzle_k(key)) << 4)) = kw;
-                *(uint4v *)(attn_lds + KT * S::ROW + key * S::ROW + ((ch ^ S::swizzle_v(key)) << 4)) = vw;
+        for (int i = 0; i < n; ++i) {
+            const uint32_t off = (i % S::NBUF) * S::STAGE;
+            if (i + 1 < n) wait_loads<S::COPIES + 1>();         // (the stage's own copies are all older than the newest that many)
+            else wait_loads<0>();
+            if constexpr (!S::ALONE) {
+                group_barrier();                                // everyone's copies are there, and everyone is done with the stage before
+                if (loads && i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
-            __syncthreads();
-            if (busy) {
-                uint32_t word[SUB];
-                bool any = false;
+            uint32_t word[SUB];                                 // keys of this wave that count, for this lane's query
+            bool all = false, some;
+            if (i < cached) {
+                const int left = len - (u0 + i) * KT - wk * SUB * 32;
+                all = left >= 32 * SUB;
+                some = busy && left > 0;
+#pragma unroll
+                for (int t = 0; t < SUB; ++t) word[t] = left >= 32 * (t + 1) ? ~0u : (left <= 32 * t ? 0u : (1u << (left - 32 * t)) - 1u);
+            } else {
+                const int v0 = (i - cached) * KT;               // the unit's first node
+                uint32_t any = 0;
 #pragma unroll
                 for (int t = 0; t < SUB; ++t) {
                     const int at = v0 / 32 + wk * SUB + t;
-                    word[t] = at * 32 < a.N ? a.anc[(long long)node * a.anc_words + at] : 0u;
-                    any |= word[t] != 0;
+                    word[t] = busy && at * 32 < a.N ? a.anc[(long long)node * a.anc_words + at] : 0u;   // a node sees its ancestors and itself
+                    any |= word[t];
                 }
-                if (__ballot(any)) stage(0, std::true_type{}, word);
+                some = __ballot(any != 0) != 0;
+                // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
+                // zeros here, and the rows that see them get them added below.
+                uint32_t *odd = (uint32_t *)(attn_lds + S::MISC);
+                if constexpr (S::ALONE) __syncthreads();        // (a wave may still read those of the unit before)
+                if (threadIdx.x < KT / 32) odd[threadIdx.x] = 0;
+                __syncthreads();
+                for (int x = threadIdx.x; x < KT * S::CPR; x += S::THREADS) {
+                    lds_uint4v *vp = (lds_uint4v *)(uintptr_t)(lds0 + off + KT * S::ROW + x * 16);
+                    uint4v vw = *vp;
+                    constexpr uint32_t kExp = S::F16 ? 0x7C00u : 0x7F80u;
+                    bool found = false;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool lo = (vw[e] & kExp) == kExp, hi = ((vw[e] >> 16) & kExp) == kExp;
+                        found |= lo | hi;
+                        vw[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+                    }
+                    if (found) {
+                        *vp = vw;
+                        atomicOr(&odd[x / S::CPR / 32], 1u << (x / S::CPR & 31));
+                    }
+                }
+                __syncthreads();
+            }
+            if (some) {
+                // scores, weights, products with the values.  (The addresses are made opaque: what is added to them below is to
+                // become part of the instructions.  The fences of the scheduler keep the reads of LDS ahead of their uses.)
+                uint32_t ka = k_at + off, va = v_at + off;
+                asm volatile("" : "+v"(ka), "+v"(va));
+                float16v s[SUB];
+                uint4v kf[SUB][DC];
+#pragma unroll
+                for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                    for (int x = 0; x < DC; ++x) kf[t][x] = *(const lds_uint4v *)(uintptr_t)((ka ^ (x << 5)) + t * 32 * S::ROW);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < SUB; ++t) {
+                    s[t] = float16v{0};
+#pragma unroll
+                    for (int x = 0; x < DC; ++x) s[t] = mfma32<S::F16>(kf[t][x], q[x], s[t]);
+                }
+                uint4v vf[2][DT];
+                auto read_values = [&](int t) {
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) {
+                            const uint32_t at = (va ^ (d << 6)) + (t * 32 + 16 * k) * S::ROW;
+                            const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
+                            const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
+                            vf[k][d] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                        }
+                };
+                read_values(0);
+                __builtin_amdgcn_sched_barrier(0);
+                if (!all) {
+#pragma unroll
+                    for (int t = 0; t < SUB; ++t) {
+                        const uint32_t w4 = word[t] >> (4 * half);
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) s[t][x] = w4 & (1u << (8 * (x / 4) + x % 4)) ? s[t][x] : -__builtin_huge_valf();
+                    }
+                }
+                float top = s[0][0];
+#pragma unroll
+                for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) top = fmaxf(top, s[t][x]);
+                top = other_half_max(top) * c;
+                if (__ballot(top > m + 8.0f)) {                 // seldom after the first stages: the old maximum will do
+                    const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - next);
+                    m = next;
+                    l *= f;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) o[d][x] *= f;
+                }
+                const float shift = kUp - m;
+#pragma unroll
+                for (int t = 0; t < SUB; ++t) {
+                    uint32_t p[8];
+#pragma unroll
+                    for (int x = 0; x < 8; ++x) {
+                        p[x] = pack2<S::F16>(__builtin_amdgcn_exp2f(fmaf(s[t][2 * x], c, shift)), __builtin_amdgcn_exp2f(fmaf(s[t][2 * x + 1], c, shift)));
+                        l = add2<S::F16>(p[x], l);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int d = 0; d < DT; ++d) o[d] = mfma32<S::F16>(vf[k][d], uint4v{p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]}, o[d]);
+                    if (t + 1 < SUB) read_values(t + 1);
+                }
+            }
+            if (i >= cached && busy) {
+                const uint32_t *odd = (const uint32_t *)(attn_lds + S::MISC);
                 for (int t = 0; t < SUB; ++t)
                     for (uint32_t bits = odd[wk * SUB + t]; bits; bits &= bits - 1) {
-                        // what was taken out above: an infinity or NaN reaches the rows that see the node, whatever their weight
-                        const int k = __builtin_ctz(bits), v = v0 + (wk * SUB + t) * 32 + k;
-                        const bool sees = (word[t] >> k) & 1u;
+                        // an infinity or NaN reaches the rows that see its node, whatever its weight
+                        const int k = __builtin_ctz(bits), v = (i - cached) * KT + (wk * SUB + t) * 32 + k;
+                        if (v >= a.N) break;
+                        const bool sees = (a.anc[(long long)node * a.anc_words + v / 32] >> k) & 1u;
                         const uint16_t *vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2] + 4 * half;
 #pragma unroll
                         for (int d = 0; d < DT; ++d)
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) {
-                                const uint16_t x = vp[32 * d + 8 * (i / 4) + i % 4];
-                                const float y = S::F16 ? (float)__builtin_bit_cast(_Float16, x) : __uint_as_float((uint32_t)x << 16);
-                                if (sees && !(fabsf(y) < __builtin_huge_valf())) o[d][i] += y;
+                            for (int x = 0; x < 16; ++x) {
+                                const uint16_t h = vp[32 * d + 8 * (x / 4) + x % 4];
+                                const float y = S::F16 ? (float)__builtin_bit_cast(_Float16, h) : __uint_as_float((uint32_t)h << 16);
+                                if (sees && !(fabsf(y) < __builtin_huge_valf())) o[d][x] += y;
                             }
                     }
+            }
+            if constexpr (S::ALONE) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
         }
 
@@ -469,6 +511,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) *(float4v *)(to + 32 * d + 8 * i) = float4v{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+                if (leads && half == 0) a.place[w * TM + at] = b * a.os[0] + node * a.os[1] + head * a.os[2];
             }
         }
         unit = item_start + u1;
@@ -476,70 +519,103 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
     }
 }
 
-// Rows of items that several workgroups took: their parts joined.  Rows of nodes that were not drafted: zeros.  One wave per
-// query head; a lane holds D / 64 elements, and the weight of one part in 64.
-template <int D, int TM, int KT, bool F16>
+// Rows of items that several workgroups took: their parts joined.  A task is four rows of an item, one for each wave, or one
+// row whose parts the waves share where there are many.  Every workgroup sums up the records for itself and takes every
+// gridDim.x-th task.  A lane holds D / 64 elements, and the weight of one part in 64.
+constexpr int kJoinShared = 8;        // more parts: the waves share them
+template <int D, int TM, bool F16>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
 {
     constexpr int E = D / 64;
-    const int b = blockIdx.x / a.N, u = blockIdx.x % a.N, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int32_t *tok = a.draft_tok + (long long)b * a.N;
-    const int heads = a.kv_heads * a.per_kv;
-    if (tok[u] < 0) {
-        for (int h = blockIdx.y * 4 + wave; h < heads; h += gridDim.y * 4) {
-            uint16_t *o = a.out + b * a.os[0] + u * a.os[1] + h * a.os[2] + lane * E;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] = 0;
+    __shared__ int tasks[kAttnMaxGroups + 1], wave_sum[4];
+    __shared__ float shared[4][D + 2];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int W = (int)attn_groups(*a.total, a.groups), per = (W + 255) / 256;
+    int sum = 0;
+    for (int i = 0; i < per; ++i) {
+        const int w = threadIdx.x * per + i;
+        if (w < W) {
+            const JoinRecord r = a.join[w];
+            sum += r.last - r.first + 1 > kJoinShared ? r.rows : (r.rows + 3) / 4;
+            tasks[w + 1] = sum;
         }
-        return;
     }
-    int rank = 0, nodes = 0;
-    for (int v0 = 0; v0 < a.N; v0 += 64) {
-        const int v = v0 + lane;
-        const unsigned long long bits = __ballot(v < a.N && tok[v] >= 0);
-        nodes += __popcll(bits);
-        if (v0 + 64 <= u) rank += __popcll(bits);
-        else if (v0 <= u) rank += __popcll(bits & ((1ull << (u - v0)) - 1));
+    int before = sum;
+    for (int off = 1; off < 64; off <<= 1) {
+        const int y = __shfl_up(before, off);
+        if (lane >= off) before += y;
     }
-    const long long total = a.prefix[a.B], W = attn_groups(total, a.groups);
-    const long long per_item = item_units(a.len[b], (long long)a.width << a.page_shift, a.N, KT);
-    const int tiles = tree_items(nodes, a.per_kv, 1, TM);
-    for (int h = blockIdx.y * 4 + wave; h < heads; h += gridDim.y * 4) {
-        const int row = rank * a.per_kv + h % a.per_kv, at = row % TM;
-        const long long start = a.prefix[b] + (h / a.per_kv * tiles + row / TM) * per_item;
-        const long long first = group_of(start, total, W), last = group_of(start + per_item - 1, total, W);
-        if (first == last) continue;                   // one workgroup had the whole item and wrote the row
-        float acc[E], top = -1e38f, sum = 0.0f;
+    if (lane == 63) wave_sum[wave] = before;
+    __syncthreads();
+    before -= sum;
+    for (int k = 0; k < wave; ++k) before += wave_sum[k];
+    for (int i = 0; i < per; ++i)
+        if (threadIdx.x * per + i < W) tasks[threadIdx.x * per + i + 1] += before;
+    if (threadIdx.x == 0) tasks[0] = 0;
+    __syncthreads();
+    const int total = W > 0 ? tasks[W] : 0;
+    for (int task = blockIdx.x; task < total; task += gridDim.x) {
+        int lo = 0, hi = W - 1;                        // the record: last one with tasks[] <= task
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (tasks[mid] <= task) lo = mid; else hi = mid - 1;
+        }
+        const int w = __builtin_amdgcn_readfirstlane(lo), sub = task - tasks[w];
+        const JoinRecord r = a.join[w];
+        const bool share = r.last - r.first + 1 > kJoinShared;
+        const int at = share ? sub : sub * 4 + wave;
+        const int step = share ? 4 : 1, from = share ? r.first + wave : r.first;
+        float acc[E], top = -1e38f, l = 0.0f;
 #pragma unroll
         for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-        for (long long g0 = first; g0 <= last; g0 += 64) {
-            const long long g = g0 + lane;
-            const float *mine = a.part + (2 * (g <= last ? g : last) + (g == first)) * (long long)TM * (D + 2);
-            const float m = g <= last ? mine[at] : -1e38f, l = g <= last ? mine[TM + at] : 0.0f;
+        const int parts = at < r.rows && from <= r.last ? (r.last - from) / step + 1 : 0;
+        for (int k1 = 0; k1 < parts; k1 += 64) {
+            const int here = min(parts - k1, 64), g = from + (k1 + min(lane, here - 1)) * step;
+            const float *mine = a.part + (2 * g + (g == r.first)) * (long long)(TM * (D + 2));
+            const float m = lane < here ? mine[at] : -1e38f, x = lane < here ? mine[TM + at] : 0.0f;
             float best = m;
             for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off));
             best = fmaxf(best, top);
             const float f = __builtin_amdgcn_exp2f(top - best), weight = __builtin_amdgcn_exp2f(m - best);
             top = best;
-            sum = fmaf(weight, l, sum * f);
+            l = fmaf(weight, x, l * f);
 #pragma unroll
             for (int e = 0; e < E; ++e) acc[e] *= f;
-            const int here = (int)(last - g0 < 63 ? last - g0 : 63) + 1;
             for (int k0 = 0; k0 < here; k0 += 8) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
-                    const int k = k0 + j < here ? k0 + j : here - 1;
-                    const float *p = a.part + (2 * (g0 + k) + (g0 + k == first)) * (long long)TM * (D + 2) + 2 * TM + at * D + lane * E;
-                    const float x = k0 + j < here ? __shfl(weight, k) : 0.0f;
+                    const int k = min(k0 + j, here - 1), gk = from + (k1 + k) * step;
+                    const float *p = a.part + (2 * gk + (gk == r.first)) * (long long)(TM * (D + 2)) + 2 * TM + at * D + lane * E;
+                    const float y = __shfl(weight, k);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] = fmaf(x, k0 + j < here ? p[e] : 0.0f, acc[e]);
+                    for (int e = 0; e < E; ++e) acc[e] = fmaf(k0 + j < here ? y : 0.0f, k0 + j < here ? p[e] : 0.0f, acc[e]);
                 }
             }
         }
-        for (int off = 32; off > 0; off >>= 1) sum += __shfl_xor(sum, off);
-        uint16_t *o = a.out + b * a.os[0] + u * a.os[1] + h * a.os[2] + lane * E;
-        if constexpr (E == 2) *(uint32_t *)o = pack2<F16>(acc[0] / sum, acc[1] / sum);
-        else o[0] = (uint16_t)pack2<F16>(acc[0] / sum, 0.0f);
+        for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
+        if (share) {
+            __syncthreads();                           // (the task before is done with them)
+#pragma unroll
+            for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = acc[e];
+            if (lane == 0) { shared[wave][D] = top; shared[wave][D + 1] = l; }
+            __syncthreads();
+            if (wave > 0) continue;
+            const float best = fmaxf(fmaxf(shared[0][D], shared[1][D]), fmaxf(shared[2][D], shared[3][D]));
+            l = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = __builtin_amdgcn_exp2f(shared[k][D] - best);
+                l = fmaf(f, shared[k][D + 1], l);
+#pragma unroll
+                for (int e = 0; e < E; ++e) acc[e] = fmaf(f, shared[k][lane * E + e], acc[e]);
+            }
+        }
+        if (at >= r.rows) continue;
+        uint16_t *o = a.out + a.place[(long long)w * TM + at] + lane * E;
+        if constexpr (E == 2) *(uint32_t *)o = pack2<F16>(acc[0] / l, acc[1] / l);
+        else o[0] = (uint16_t)pack2<F16>(acc[0] / l, 0.0f);
     }
 }
 
