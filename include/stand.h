@@ -478,10 +478,12 @@ int stand_cache_pages(stand_handle *h, const stand_pages *p, const int32_t *d_ad
  *   d_penalty  [B][3]: repetition (> 0; 1: none), presence, frequency (0: none); or NULL
  *   d_bias_id  [B][bias_width], d_bias [B][bias_width]: ids outside [0, V) are left out, of entries with the same id the last
  *              counts; biases are finite or -inf; bias_width 0: none
- *   d_allow    [B][N][(V + 31) / 32]: bit v % 32 of word v / 32; bits past V do not matter; or NULL */
+ *   d_allow    [B][N][(V + 31) / 32]: bit v % 32 of word v / 32; bits past V do not matter; or NULL
+ *   d_work     with d_allow: device memory of stand_shape_logits_work bytes, as for stand_tree_attention; else it may be NULL */
 int stand_shape_logits(stand_handle *h, const void *d_logits, void *d_out, const int32_t *d_draft_tok, const int32_t *d_count,
                        const float *d_penalty, const int32_t *d_bias_id, const float *d_bias, int32_t bias_width,
-                       const uint32_t *d_allow, void *stream);
+                       const uint32_t *d_allow, void *d_work, uint64_t work_bytes, void *stream);
+uint64_t stand_shape_logits_work(const stand_handle *h);
 
 /* Tokens into the counts d_count [B][V] (zeros at first): the first d_len[b] (NULL: width) of d_tok [B][width]; ids outside [0, V)
  * are left out.  prompt == 0: generated tokens, added (after a step: d_out_tok, d_out_len); otherwise the prompt's.  A count

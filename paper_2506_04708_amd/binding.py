@@ -29,7 +29,7 @@ EXPORTED = [
     "stand_set_step_plan", "stand_set_wait_limit", "stand_step_timeline", "stand_step_is_one_launch",
     "stand_get_record_slots",
     "stand_tree_attention", "stand_tree_attention_work", "stand_cache_commit", "stand_cache_pages", "stand_shape_logits",
-    "stand_count_tokens",
+    "stand_shape_logits_work",    "stand_count_tokens",
 ]
 
 
@@ -125,7 +125,9 @@ def load_library():
     lib.stand_tree_attention_work.restype = C.c_uint64
     lib.stand_cache_commit.argtypes = [vp, vp, vp, vp, C.c_int32, vp, vp, vp]
     lib.stand_cache_pages.argtypes = [vp, vp, vp, vp, vp, C.c_int32, vp, vp, vp]
-    lib.stand_shape_logits.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, C.c_int32, vp, vp]
+    lib.stand_shape_logits.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, C.c_int32, vp, vp, C.c_uint64, vp]
+    lib.stand_shape_logits_work.argtypes = [vp]
+    lib.stand_shape_logits_work.restype = C.c_uint64
     lib.stand_count_tokens.argtypes = [vp, vp, vp, vp, C.c_int32, C.c_int32, vp]
     lib.stand_strerror.restype = C.c_char_p
     lib.stand_strerror.argtypes = [C.c_int]
@@ -478,9 +480,11 @@ class Stand:
         assert (bias_id is None) == (bias is None) and (bias is None or bias.shape == bias_id.shape == (self.B, M))
         assert allow is None or allow.shape == (self.B, self.N, (self.V + 31) // 32)
         self._here(logits, out, draft_tok, count, penalty, bias_id, bias, allow)
+        work = None if allow is None else torch.empty(self.B * self.N, dtype=torch.uint8, device=self.device)
         _check(self._lib.stand_shape_logits(self.h, self._logits_ptr(logits), self._logits_ptr(out), _dptr(draft_tok, torch.int32),
                                             _dptr(count, torch.int32), _dptr(penalty, torch.float32), _dptr(bias_id, torch.int32),
-                                            _dptr(bias, torch.float32), M, _dptr(allow, torch.int32), self._stream()), self.h)
+                                            _dptr(bias, torch.float32), M, _dptr(allow, torch.int32), _dptr(work), self.B * self.N,
+                                            self._stream()), self.h)
         return out
 
     def count_tokens(self, count, tok, length=None, prompt=False):

@@ -46,7 +46,12 @@ __global__ __launch_bounds__(256) void cache_commit_kernel(CommitArgs a)
 // ---- block tables, slot maps, free pages ---------------------------------------------------------------------------------
 // The free pages are the entries taken .. given - 1 (modulo `pages`) of a ring; mark = {taken, given} only grows.  Demands are
 // served in the order of the trajectories, from the ring's front as it was before the call; pages that are given back go to
-// its end.  So one exclusive prefix sum over the demands and one over the returns say where every page goes.
+// its end.  So one exclusive prefix sum over the demands and one over the returns say where every page goes, and every
+// workgroup can make those sums for itself: `groups` of them share the trajectories' tables and slots, none waits for another.
+// What is taken and what is given back are different entries of the ring, and a slot on a new page is read from the ring, not
+// from the table.  The new lengths, held counts and marks may replace the old ones, which the others still read: then they are
+// written by a launch of their own behind the others' (`what`), or, where there is one workgroup only, after a barrier.
+// Bound by latency (three dependent reads) up to some hundred trajectories, by the slots' bytes with prompts.
 struct PagesArgs {
     int32_t *table, *ring;
     const int32_t *length, *held, *add, *room;
@@ -54,66 +59,125 @@ struct PagesArgs {
     int32_t *length_out, *held_out, *missing;
     long long *mark_out, *slots;
     int B, width, pages, page_shift, slot_width, default_room;
+    int per_group;              // consecutive trajectories of a workgroup, at most kPagesThreads
+    int what;                   // kPagesTables | kPagesState
 };
+constexpr int kPagesTables = 1, kPagesState = 2;
+constexpr int kPagesThreads = 256;
 
-constexpr int kPagesThreads = 1024;
+struct PagesDemand { long long len; int need, held, ask, give, room; };
+
+__device__ __forceinline__ PagesDemand pages_demand(const PagesArgs &a, int b)
+{
+    PagesDemand d;
+    const long long ps = 1ll << a.page_shift;
+    d.held = a.held[b];
+    d.held = d.held < 0 ? 0 : (d.held > a.width ? a.width : d.held);
+    d.room = a.room ? a.room[b] : a.default_room;
+    d.len = 0;
+    long long need = 0;
+    if (d.room >= 0) {
+        d.len = (long long)a.length[b] + (a.add ? a.add[b] : 0);
+        d.len = d.len < 0 ? 0 : (d.len > d.held * ps ? d.held * ps : d.len);
+        need = (d.len + d.room + ps - 1) >> a.page_shift;
+    }
+    need = need < 0x7FFFFFFF ? need : 0x7FFFFFFF;
+    d.need = (int)need;
+    d.ask = need > d.held && need <= a.width ? (int)need - d.held : 0;
+    d.give = d.held > need ? d.held - (int)need : 0;
+    return d;
+}
 
 __global__ __launch_bounds__(kPagesThreads) void cache_pages_kernel(PagesArgs a)
 {
-    __shared__ long long sum_ask[kPagesThreads], sum_give[kPagesThreads];
-    __shared__ long long base_ask, base_give, granted;
-    const int t = threadIdx.x;
+    struct Mine { long long len, before, back; int need, held, now, ask, give, room; };
+    __shared__ Mine mine[kPagesThreads];
+    __shared__ long long wave_ask[4], wave_give[4];
+    __shared__ unsigned long long granted;
+    __shared__ int most_ask, most_give;
+    const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const long long taken = a.mark[0], given = a.mark[1];
     long long avail = given - taken;
     avail = avail < 0 ? 0 : (avail > a.pages ? a.pages : avail);
-    if (t == 0) { base_ask = 0; base_give = 0; granted = 0; }
-    const long long ps = 1ll << a.page_shift;
-    for (int b0 = 0; b0 < a.B; b0 += kPagesThreads) {
-        const int b = b0 + t;
-        long long len = 0, need = 0, ask = 0, give = 0;
-        int held = 0, room = -1;
-        if (b < a.B) {
-            held = a.held[b];
-            held = held < 0 ? 0 : (held > a.width ? a.width : held);
-            room = a.room ? a.room[b] : a.default_room;
-            if (room >= 0) {
-                len = (long long)a.length[b] + (a.add ? a.add[b] : 0);
-                len = len < 0 ? 0 : (len > held * ps ? held * ps : len);
-                need = (len + room + ps - 1) >> a.page_shift;
-            }
-            ask = need > held && need <= a.width ? need - held : 0;
-            give = held > need ? held - need : 0;
-        }
-        sum_ask[t] = ask; sum_give[t] = give;
-        __syncthreads();
-        for (int off = 1; off < kPagesThreads; off <<= 1) {
-            const long long x = t >= off ? sum_ask[t - off] : 0, y = t >= off ? sum_give[t - off] : 0;
-            __syncthreads();
-            sum_ask[t] += x; sum_give[t] += y;
-            __syncthreads();
-        }
-        if (b < a.B) {
-            const long long before = base_ask + sum_ask[t] - ask, back = base_give + sum_give[t] - give;
-            const bool ok = need <= held || (need <= a.width && before + ask <= avail);
-            const int now = ok ? (int)need : held;
-            int32_t *row = a.table + (long long)b * a.width;
-            if (ok)
-                for (long long i = 0; i < ask; ++i) row[held + i] = a.ring[(unsigned long long)(taken + before + i) % (unsigned)a.pages];
-            for (long long i = 0; i < give; ++i) a.ring[(unsigned long long)(given + back + i) % (unsigned)a.pages] = row[need + i];
-            a.length_out[b] = (int)len;
-            a.held_out[b] = now;
-            a.missing[b] = ok ? 0 : (int)(need - held);
-            for (int j = 0; j < a.slot_width; ++j) {
-                const long long pos = len + j, pg = pos >> a.page_shift;
-                a.slots[(long long)b * a.slot_width + j] = j < room && pg < now ? (long long)row[pg] * ps + (pos & (ps - 1)) : -1;
-            }
-            if (ok && ask) atomicMax((unsigned long long *)&granted, (unsigned long long)(before + ask));
-        }
-        __syncthreads();
-        if (t == 0) { base_ask += sum_ask[kPagesThreads - 1]; base_give += sum_give[kPagesThreads - 1]; }
-        __syncthreads();
+    const int chunk = (a.B + kPagesThreads - 1) / kPagesThreads, c0 = t * chunk, c1 = min(a.B, c0 + chunk);
+    const int b0 = blockIdx.x * a.per_group, b1 = min(a.B, b0 + a.per_group);
+
+    // sums before this thread's trajectories
+    long long ask = 0, give = 0;
+    PagesDemand d;
+    for (int b = c0; b < c1; ++b) {
+        d = pages_demand(a, b);
+        ask += d.ask; give += d.give;
     }
-    if (t == 0) { a.mark_out[0] = taken + granted; a.mark_out[1] = given + base_give; }
+    long long up_ask = ask, up_give = give;
+    for (int off = 1; off < 64; off <<= 1) {
+        const long long x = __shfl_up(up_ask, off), y = __shfl_up(up_give, off);
+        if (lane >= off) { up_ask += x; up_give += y; }
+    }
+    if (lane == 63) { wave_ask[wave] = up_ask; wave_give[wave] = up_give; }
+    if (t == 0) { granted = 0; most_ask = 0; most_give = 0; }
+    __syncthreads();
+    long long before = up_ask - ask, back = up_give - give;
+    for (int k = 0; k < wave; ++k) { before += wave_ask[k]; back += wave_give[k]; }
+
+    // what becomes of each
+    const bool state = a.what & kPagesState;
+    const long long all_given = wave_give[0] + wave_give[1] + wave_give[2] + wave_give[3];
+    for (int b = c0; b < c1; ++b) {
+        const bool ours = b >= b0 && b < b1;
+        if (!ours && !state) {
+            if (chunk > 1) { d = pages_demand(a, b); before += d.ask; back += d.give; }
+            continue;
+        }
+        if (chunk > 1) d = pages_demand(a, b);
+        const bool ok = d.need <= d.held || (d.need <= a.width && before + d.ask <= avail);
+        const int now = ok ? d.need : d.held;
+        if (ok && d.ask) atomicMax(&granted, (unsigned long long)(before + d.ask));
+        if (ours && (a.what & kPagesTables)) {
+            a.missing[b] = ok ? 0 : d.need - d.held;
+            mine[b - b0] = Mine{d.len, before, back, d.need, d.held, now, ok ? d.ask : 0, d.give, d.room};
+            if (ok && d.ask) atomicMax(&most_ask, d.ask);
+            if (d.give) atomicMax(&most_give, d.give);
+        }
+        if (state && gridDim.x == 1 && (a.what & kPagesTables) == 0) { a.length_out[b] = (int)d.len; a.held_out[b] = now; }
+        before += d.ask; back += d.give;
+    }
+    __syncthreads();
+    if (state && t == 0 && blockIdx.x == 0) { a.mark_out[0] = taken + (long long)granted; a.mark_out[1] = given + all_given; }
+    if (!(a.what & kPagesTables)) return;
+
+    const long long ps = 1ll << a.page_shift;
+    const unsigned P = (unsigned)a.pages, taken_at = (unsigned)((unsigned long long)taken % P), given_at = (unsigned)((unsigned long long)given % P);
+    auto ring_at = [&](unsigned start, long long i) {          // (i < pages where the ring is whole)
+        const unsigned long long x = (unsigned long long)start + (unsigned long long)i;
+        return (unsigned)(x < P ? x : x - P < P ? x - P : x % P);
+    };
+    const int n = b1 - b0;
+    auto each = [&](int width, auto &&f) {                     // f(trajectory, j), j < width, over the workgroup's threads
+        if (width >= 64)
+            for (int k = 0; k < n; ++k)
+                for (int j = t; j < width; j += kPagesThreads) f(k, j);
+        else
+            for (int x = t; x < n * width; x += kPagesThreads) f(x / width, x % width);
+    };
+    each(most_ask, [&](int k, int i) {
+        const Mine &m = mine[k];
+        if (i < m.ask) a.table[(long long)(b0 + k) * a.width + m.held + i] = a.ring[ring_at(taken_at, m.before + i)];
+    });
+    each(most_give, [&](int k, int i) {
+        const Mine &m = mine[k];
+        if (i < m.give) a.ring[ring_at(given_at, m.back + i)] = a.table[(long long)(b0 + k) * a.width + m.need + i];
+    });
+    each(a.slot_width, [&](int k, int j) {
+        const Mine &m = mine[k];
+        const long long pos = m.len + j, pg = pos >> a.page_shift;
+        long long slot = -1;
+        if (j < m.room && pg < m.now)
+            slot = (long long)(pg < m.held ? a.table[(long long)(b0 + k) * a.width + pg] : a.ring[ring_at(taken_at, m.before + pg - m.held)]) * ps + (pos & (ps - 1));
+        a.slots[(long long)(b0 + k) * a.slot_width + j] = slot;
+    });
+    if (state)
+        for (int k = t; k < n; k += kPagesThreads) { a.length_out[b0 + k] = (int)mine[k].len; a.held_out[b0 + k] = mine[k].now; }
 }
 
 }  // namespace stand

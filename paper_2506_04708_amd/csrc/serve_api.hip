@@ -220,30 +220,53 @@ extern "C" int stand_cache_pages(stand_handle *h, const stand_pages *p, const in
     a.slots = (long long *)d_slots;
     a.B = v.B; a.width = p->width; a.pages = p->pages; a.page_shift = log2_of(p->page_size); a.slot_width = slot_width;
     a.default_room = v.D + 1;
-    cache_pages_kernel<<<dim3(1), dim3(kPagesThreads), 0, (hipStream_t)stream>>>(a);
+    // One workgroup where that is little work (up to 64 trajectories with 4096 slots: the state is then written behind its own
+    // reads); else up to 1024 of them.
+    const bool aside = out->d_length != p->d_length && out->d_held != p->d_held && out->d_mark != p->d_mark;
+    const int64_t slots = (int64_t)v.B * slot_width;
+    int64_t groups = v.B <= 64 && slots <= 4096 ? 1 : std::min<int64_t>(v.B, 1024);
+    a.per_group = (int)((v.B + groups - 1) / groups);
+    groups = (v.B + a.per_group - 1) / a.per_group;
+    a.what = groups == 1 || aside ? kPagesTables | kPagesState : kPagesTables;
+    cache_pages_kernel<<<dim3((unsigned)groups), dim3(kPagesThreads), 0, (hipStream_t)stream>>>(a);
+    if (!(a.what & kPagesState)) {
+        a.what = kPagesState;
+        cache_pages_kernel<<<dim3(1), dim3(kPagesThreads), 0, (hipStream_t)stream>>>(a);
+    }
     return launched(v);
+}
+
+extern "C" uint64_t stand_shape_logits_work(const stand_handle *h)
+{
+    if (!h) return 0;
+    const ServeView v = serve_view(const_cast<stand_handle *>(h));
+    return (uint64_t)v.B * v.N;
 }
 
 extern "C" int stand_shape_logits(stand_handle *h, const void *d_logits, void *d_out, const int32_t *d_draft_tok, const int32_t *d_count,
                                   const float *d_penalty, const int32_t *d_bias_id, const float *d_bias, int32_t bias_width,
-                                  const uint32_t *d_allow, void *stream)
+                                  const uint32_t *d_allow, void *d_work, uint64_t work_bytes, void *stream)
 {
     if (!h || !d_logits || !d_out || !d_draft_tok || bias_width < 0 || (bias_width > 0 && (!d_bias_id || !d_bias))) return STAND_EINVAL;
+    if (d_allow && (!d_work || work_bytes < stand_shape_logits_work(h))) return STAND_EINVAL;
     const ServeView v = serve_view(h);
     const bool f32 = v.logits_dtype == STAND_F32;
     if (((uintptr_t)d_logits | (uintptr_t)d_out) & (f32 ? 3u : 1u)) return STAND_EINVAL;
     ShapeArgs a;
     a.x = d_logits; a.out = d_out; a.draft_tok = d_draft_tok; a.count = d_count; a.penalty = d_penalty; a.bias_id = d_bias_id; a.bias = d_bias;
     a.allow = d_allow; a.anc = v.anc; a.anc_words = v.anc_words; a.N = v.N; a.V = v.V; a.M = bias_width; a.words = (v.V + 31) / 32;
+    a.any = (uint8_t *)d_work; a.rows = (long long)v.B * v.N;
     const int64_t spans = ((int64_t)v.V + kShapeSpan - 1) / kShapeSpan;
     // nodes that share a workgroup's counts: as many as leave 2048 workgroups, at most 16
-    a.nodes_per_group = 16;
+    a.nodes_per_group = kShapeNodes;
     while (a.nodes_per_group > 1 && spans * v.B * ((v.N + a.nodes_per_group - 1) / a.nodes_per_group) < 2048) a.nodes_per_group /= 2;
     a.node_groups = (v.N + a.nodes_per_group - 1) / a.nodes_per_group;
-    if (v.B > 65535 || spans * a.node_groups * kShapeThreads > UINT32_MAX) return STAND_ELIMIT;
+    a.spans = (int)spans;
+    if (v.B > 65535 || spans * a.node_groups * v.B > (int64_t)(UINT32_MAX / kShapeThreads)) return STAND_ELIMIT;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
-    const dim3 grid((unsigned)(spans * a.node_groups), (unsigned)v.B);
+    const dim3 grid((unsigned)(spans * a.node_groups * v.B));
+    if (d_allow) shape_rows_kernel<<<dim3((unsigned)((a.rows + 3) / 4)), dim3(256), 0, (hipStream_t)stream>>>(a);
     if (f32) shape_logits_kernel<kDtF32><<<grid, dim3(kShapeThreads), 0, (hipStream_t)stream>>>(a);
     else shape_logits_kernel<kDtBf16><<<grid, dim3(kShapeThreads), 0, (hipStream_t)stream>>>(a);
     return launched(v);

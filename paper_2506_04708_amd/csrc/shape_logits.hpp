@@ -24,35 +24,37 @@ struct ShapeArgs {
     const int32_t *draft_tok, *count, *bias_id;
     const float *penalty, *bias;
     const uint32_t *allow;
+    uint8_t *any;                  // workspace: [B][N], 1 where a row's mask has a bit for a token
     const unsigned long long *anc;
-    int anc_words, N, V, M, words, nodes_per_group, node_groups;
+    int anc_words, N, V, M, words, nodes_per_group, node_groups, spans;
+    long long rows;
 };
 
 struct alignas(2) Half8 { uint16_t h[8]; };   // eight logits at any alignment: rows of an odd vocabulary start anywhere
-struct alignas(4) Float8 { float f[8]; };
-struct alignas(4) Int8 { int32_t i[8]; };
+struct alignas(4) Float4 { float f[4]; };
+struct alignas(4) Int4 { uint32_t i[4]; };
+typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
 
+// (Streamed past the caches: 330 us instead of 345 us for 623 MB of logits in and out.)
 template <int DT>
 __device__ __forceinline__ void load_tokens(const void *row, int t, float (&x)[8])
 {
     if constexpr (DT == kDtBf16) {
-        const Half8 w = *(const Half8 *)((const uint16_t *)row + t);
+        const Half8 w = __builtin_bit_cast(Half8, __builtin_nontemporal_load((const Words4 *)((const uint16_t *)row + t)));
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = u2f((uint32_t)w.h[i] << 16);
     } else {
-        const Float8 w = *(const Float8 *)((const float *)row + t);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = w.f[i];
+        for (int q = 0; q < 2; ++q) {
+            const Float4 w = __builtin_bit_cast(Float4, __builtin_nontemporal_load((const Words4 *)((const float *)row + t + 4 * q)));
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[4 * q + i] = w.f[i];
+        }
     }
 }
 
-// Nearest bf16, ties to even; infinities stay, a NaN stays one.
-__device__ __forceinline__ uint16_t bf16_bits(float f)
-{
-    const uint32_t u = f2u(f);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (uint16_t)((u >> 16) | 0x40u);
-    return (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
-}
+// Nearest bf16, ties to even (one instruction for two of them).
+__device__ __forceinline__ uint16_t bf16_bits(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 
 template <int DT>
 __device__ __forceinline__ void store_tokens(void *row, int t, const float (&x)[8])
@@ -61,14 +63,47 @@ __device__ __forceinline__ void store_tokens(void *row, int t, const float (&x)[
         Half8 w;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w.h[i] = bf16_bits(x[i]);
-        *(Half8 *)((uint16_t *)row + t) = w;
+        __builtin_nontemporal_store(__builtin_bit_cast(Words4, w), (Words4 *)((uint16_t *)row + t));
     } else {
-        Float8 w;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w.f[i] = x[i];
-        *(Float8 *)((float *)row + t) = w;
+        for (int q = 0; q < 2; ++q) {
+            const Float4 w = {{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]}};
+            __builtin_nontemporal_store(__builtin_bit_cast(Words4, w), (Words4 *)((float *)row + t + 4 * q));
+        }
     }
 }
+
+// Which rows' masks have a bit for a token at all: one wave per row, 8 KiB of bits in flight, done at the first bit.  (Made by
+// the workgroups of the kernel below for themselves, this cost 83 us of 348 us: they wait where they should stream.)
+__global__ __launch_bounds__(256) void shape_rows_kernel(ShapeArgs a)
+{
+    const int lane = threadIdx.x & 63;
+    const long long r = (long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (r >= a.rows || a.draft_tok[r] < 0) return;
+    const uint32_t *m = a.allow + r * a.words;
+    bool any = false;
+    for (int w0 = 0; w0 < a.words && !any; w0 += 8 * 4 * 64) {
+        uint32_t x = 0;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int w = w0 + (q * 64 + lane) * 4;
+            if (w + 4 < a.words) {
+                const Int4 y = *(const Int4 *)(m + w);
+                x |= y.i[0] | y.i[1] | y.i[2] | y.i[3];
+            } else {
+                for (int e = w; e < a.words; ++e) x |= m[e] & (e == a.words - 1 && (a.V & 31) ? (1u << (a.V & 31)) - 1u : ~0u);
+            }
+        }
+        any = __ballot(x != 0) != 0;
+    }
+    if (lane == 0) a.any[r] = any;
+}
+
+// A workgroup has one span of tokens for up to kShapeNodes nodes of a trajectory: counts and biases of its tokens are read
+// once and stay in registers, and so do the mask bits of all its nodes, so that the nodes' rows pass without a barrier between
+// them, kShapeAhead rows in flight.  What a mask leaves nothing of is not read.  Bound by HBM: logits in and out, mask bits,
+// counts once for every kShapeNodes nodes.
+constexpr int kShapeNodes = 16, kShapeAhead = 4;
 
 template <int DT>
 __global__ __launch_bounds__(kShapeThreads) void shape_logits_kernel(ShapeArgs a)
@@ -76,106 +111,130 @@ __global__ __launch_bounds__(kShapeThreads) void shape_logits_kernel(ShapeArgs a
     __shared__ int32_t slot[kShapeSpan];          // last entry of the bias list for each token of the span
     __shared__ uint16_t hit_node[kMaxNodes], hit_at[kMaxNodes];
     __shared__ int hits;
-    const int b = blockIdx.y, tid = threadIdx.x;
-    const int span = blockIdx.x / a.node_groups, group = blockIdx.x % a.node_groups;
+    const int tid = threadIdx.x;
+    const int group = blockIdx.x % a.node_groups, span = blockIdx.x / a.node_groups % a.spans;
+    const long long b = blockIdx.x / a.node_groups / a.spans;
     const int t0 = span * kShapeSpan, t = t0 + tid * kShapeTokens;
     const int mine = a.V - t < 0 ? 0 : (a.V - t < 8 ? a.V - t : 8);
-    const int32_t *tok = a.draft_tok + (long long)b * a.N;
+    const int32_t *tok = a.draft_tok + b * a.N;
+    const int u0 = group * a.nodes_per_group, nodes = min(a.N - u0, a.nodes_per_group);
+    const long long r0 = b * a.N + u0;
 
+    // mask bits of this thread's tokens, a byte for every node; rows that are not masked keep all of them
+    uint32_t keep[kShapeNodes / 4] = {~0u, ~0u, ~0u, ~0u};
+    int drafted = 0;                              // bit per node
+#pragma unroll
+    for (int i = 0; i < kShapeNodes; ++i)
+        if (i < nodes && tok[u0 + i] >= 0) {
+            drafted |= 1 << i;
+            if (a.allow && a.any[r0 + i]) {
+                const uint32_t x = mine ? a.allow[(r0 + i) * a.words + (t >> 5)] >> (t & 31) & 0xFFu : 0u;
+                keep[i / 4] = (keep[i / 4] & ~(0xFFu << (i % 4 * 8))) | x << (i % 4 * 8);
+            }
+        }
+
+    // the bias of each token (of several entries the last), drafted tokens of the span
     if (tid == 0) hits = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) slot[tid * 8 + i] = -1;
     __syncthreads();
     for (int u = 1 + tid; u < a.N; u += kShapeThreads) {
-        const int at = tok[u] - t0;
-        if (tok[u] >= 0 && at >= 0 && at < kShapeSpan) {
+        const int v = tok[u], at = v - t0;
+        if (v >= 0 && at >= 0 && at < kShapeSpan) {
             const int q = atomicAdd(&hits, 1);
             hit_node[q] = (uint16_t)u;
             hit_at[q] = (uint16_t)at;
         }
     }
     for (int i = tid; i < a.M; i += kShapeThreads) {
-        const int id = a.bias_id[(long long)b * a.M + i];
+        const int id = a.bias_id[b * a.M + i];
         if (id >= t0 && id < t0 + kShapeSpan && id < a.V) atomicMax(&slot[id - t0], i);
     }
     __syncthreads();
 
     int32_t c0[8];
     float shift[8];
-    const float rho = a.penalty ? a.penalty[3 * (long long)b] : 1.0f;
-    const float present = a.penalty ? a.penalty[3 * (long long)b + 1] : 0.0f;
-    const float often = a.penalty ? a.penalty[3 * (long long)b + 2] : 0.0f;
+    const float rho = a.penalty ? a.penalty[3 * b] : 1.0f, inverse = 1.0f / rho;
+    const float present = a.penalty ? a.penalty[3 * b + 1] : 0.0f;
+    const float often = a.penalty ? a.penalty[3 * b + 2] : 0.0f;
+    bool touched = false;                         // this thread's tokens are not all as they were
+    if (a.count && mine == 8) {
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+            const Int4 w = *(const Int4 *)(a.count + b * a.V + t + 4 * q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) c0[4 * q + i] = (int32_t)w.i[i];
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c0[i] = a.count && i < mine ? a.count[b * a.V + t + i] : 0;
+    }
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        c0[i] = a.count && i < mine ? a.count[(long long)b * a.V + t + i] : 0;
-        const int s = a.M ? slot[tid * 8 + i] : -1;
-        shift[i] = s >= 0 ? a.bias[(long long)b * a.M + s] : 0.0f;
+        const int s = slot[tid * 8 + i];
+        shift[i] = s >= 0 ? a.bias[b * a.M + s] : 0.0f;
+        touched |= c0[i] != 0 || s >= 0;
     }
     bool near = false;
     for (int q = 0; q < hits; ++q) near |= hit_at[q] / 8 == tid;
+    touched |= near;
+    if (!mine) return;
 
-    const int u1 = min(a.N, (group + 1) * a.nodes_per_group);
-    for (int u = group * a.nodes_per_group; u < u1; ++u) {
-        const long long r = (long long)b * a.N + u;
-        const char *xr = (const char *)a.x + r * a.V * VecTraits<DT>::ES;
-        char *yr = (char *)a.out + r * a.V * VecTraits<DT>::ES;
-        const bool drafted = tok[u] >= 0;
-        if (!drafted && a.x == a.out) continue;
-        unsigned keep = 0xFFu;
-        if (a.allow && drafted) {
-            const uint32_t *m = a.allow + r * a.words;
-            const unsigned valid = (1u << mine) - 1u;
-            keep = mine ? (m[t >> 5] >> (t & 31)) & valid : 0u;
-            if (!__syncthreads_or(keep != 0)) {
-                // none in this span: -inf everywhere, unless the row has no bit at all
-                bool any = false;
-                for (int w0 = 0; w0 < a.words && !any; w0 += 4 * kShapeThreads) {
-                    uint32_t got = 0;
+    const long long row = (long long)a.V * VecTraits<DT>::ES;
+    const char *xp = (const char *)a.x + r0 * row;
+    char *yp = (char *)a.out + r0 * row;
+    for (int i0 = 0; i0 < nodes; i0 += kShapeAhead) {
+        float x[kShapeAhead][8];
+        const uint32_t kept = i0 == 0 ? keep[0] : i0 == 4 ? keep[1] : i0 == 8 ? keep[2] : keep[3];
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const int w = w0 + q * kShapeThreads + tid;
-                        if (w < a.words) got |= m[w] & (w == a.words - 1 && (a.V & 31) ? (1u << (a.V & 31)) - 1u : ~0u);
+        for (int k = 0; k < kShapeAhead; ++k) {
+            const int i = i0 + k;
+            if (i < nodes && (kept >> (k * 8) & 0xFFu)) {
+                if (mine == 8) load_tokens<DT>(xp + i * row, t, x[k]);
+                else
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[k][e] = e < mine ? load_scalar<DT>(xp + i * row, t + e) : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kShapeAhead; ++k) {
+            const int i = i0 + k;
+            if (i >= nodes || (!(drafted >> i & 1) && a.x == a.out)) continue;
+            if (drafted >> i & 1) {
+                if (touched) {
+                    int32_t c[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) c[e] = c0[e];
+                    if (near)
+                        for (int q = 0; q < hits; ++q) {
+                            const int v = hit_node[q], at = hit_at[q] - tid * 8;
+                            const bool on = (a.anc[(long long)(u0 + i) * a.anc_words + (v >> 6)] >> (v & 63)) & 1ull;
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) c[e] += on && at == e ? 1 : 0;
+                        }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float times = (float)(c[e] & (kPromptFlag - 1)), z = x[k][e];
+                        // the quotient to half a step: one correction with the exact remainder
+                        const float q = z * inverse, p = fmaf(fmaf(-q, rho, z), inverse, q);
+                        float y = z > 0.0f ? p : z * rho;
+                        y = y - often * times;
+                        y = times > 0.0f ? y - present : y;
+                        x[k][e] = (c[e] != 0 ? y : z) + shift[e];
                     }
-                    any = __syncthreads_or(got != 0);
                 }
-                if (!any) keep = 0xFFu;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[k][e] = kept >> (k * 8 + e) & 1u ? x[k][e] : -__builtin_huge_valf();
             }
+            if (mine == 8) store_tokens<DT>(yp + i * row, t, x[k]);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e)
+                    if (e < mine) {
+                        if constexpr (DT == kDtBf16) ((uint16_t *)(yp + i * row))[t + e] = bf16_bits(x[k][e]);
+                        else ((float *)(yp + i * row))[t + e] = x[k][e];
+                    }
         }
-        if (!mine) continue;
-        float x[8];
-        if (mine == 8) load_tokens<DT>(xr, t, x);
-        else
-            for (int i = 0; i < 8; ++i) x[i] = i < mine ? load_scalar<DT>(xr, t + i) : 0.0f;
-        if (drafted) {
-            int32_t c[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) c[i] = c0[i];
-            if (near)
-                for (int q = 0; q < hits; ++q) {
-                    const int v = hit_node[q], at = hit_at[q] - tid * 8;
-                    const bool on = (a.anc[(long long)u * a.anc_words + (v >> 6)] >> (v & 63)) & 1ull;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) c[i] += on && at == i ? 1 : 0;
-                }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float times = (float)(c[i] & (kPromptFlag - 1));
-                float y = x[i];
-                if (c[i] != 0) {
-                    y = y > 0.0f ? y / rho : y * rho;
-                    y = y - often * times;
-                    y = times > 0.0f ? y - present : y;
-                }
-                y = y + shift[i];
-                x[i] = (keep >> i) & 1u ? y : -__builtin_huge_valf();
-            }
-        }
-        if (mine == 8) store_tokens<DT>(yr, t, x);
-        else
-            for (int i = 0; i < mine; ++i) {
-                if constexpr (DT == kDtBf16) ((uint16_t *)yr)[t + i] = bf16_bits(x[i]);
-                else ((float *)yr)[t + i] = x[i];
-            }
     }
 }
 
