@@ -31,6 +31,8 @@ STAND_BOTH int tree_items(int drafted, int per_kv, int kv_heads, int tile_rows)
 {
     return (drafted * per_kv + tile_rows - 1) / tile_rows * kv_heads;
 }
+// Rows of each of a head's tiles but the last: equal ones, in whole waves.
+STAND_BOTH int rows_of_tile(int rows, int tiles) { return ((rows + tiles - 1) / tiles + 31) / 32 * 32; }
 // Workgroups that get a share, of `groups` launched.
 STAND_BOTH long long attn_groups(long long total, int groups)
 {

@@ -93,7 +93,13 @@ auto with_attn_shape(int head_dim, bool f16, AttnForm f, Call call)
 template <typename S>
 int attn_launch_groups(int cus)
 {
-    const int per_cu = std::max(1, std::min(160 * 1024 / S::BYTES, 8 / S::WAVES));
+    static const int per_cu = [] {
+        int n = 0;
+        // (above 64 KiB dynamic LDS has to be asked for)
+        if (hipFuncSetAttribute((const void *)tree_attn_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES) != hipSuccess) return 1;
+        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)tree_attn_kernel<S>, S::THREADS, S::BYTES) != hipSuccess) return 1;
+        return std::max(n, 1);
+    }();
     return std::max(8, std::min(cus * per_cu, kAttnMaxGroups) / 8 * 8);
 }
 // Workspace: units, records, places, parts.
@@ -112,9 +118,6 @@ hipError_t attn_launch(TreeAttnArgs &a, int cus, hipStream_t s)
     a.join = (JoinRecord *)((char *)a.total + kAttnHead);
     a.place = (long long *)(a.join + a.groups);
     a.part = (float *)(a.place + (size_t)a.groups * S::TM);
-    // (above 64 KiB dynamic LDS has to be asked for, once per device; the call is cheap and says so of any later one)
-    const hipError_t e = hipFuncSetAttribute((const void *)tree_attn_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
-    if (e != hipSuccess) return e;
     tree_attn_kernel<S><<<dim3((unsigned)a.groups), dim3(S::THREADS), S::BYTES, s>>>(a);
     tree_attn_join_kernel<S::D, S::TM, S::F16><<<dim3(4u * (unsigned)cus), dim3(256), 0, s>>>(a);
     return hipGetLastError();

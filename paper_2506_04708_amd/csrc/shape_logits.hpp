@@ -122,16 +122,23 @@ __global__ __launch_bounds__(kShapeThreads) void shape_logits_kernel(ShapeArgs a
 
     // mask bits of this thread's tokens, a byte for every node; rows that are not masked keep all of them
     uint32_t keep[kShapeNodes / 4] = {~0u, ~0u, ~0u, ~0u};
-    int drafted = 0;                              // bit per node
+    int drafted, masked;                          // bit per node
+    {
+        const int lane = tid & 63;
+        const bool here = lane < nodes;
+        const int v = here ? tok[u0 + lane] : -1;
+        const bool any = a.allow && here && a.any[r0 + lane];
+        drafted = (int)__ballot(v >= 0);
+        masked = (int)__ballot(any) & drafted;    // (nothing has been written for the other rows)
+    }
+    if (masked) {
+        uint32_t got[kShapeNodes];
 #pragma unroll
-    for (int i = 0; i < kShapeNodes; ++i)
-        if (i < nodes && tok[u0 + i] >= 0) {
-            drafted |= 1 << i;
-            if (a.allow && a.any[r0 + i]) {
-                const uint32_t x = mine ? a.allow[(r0 + i) * a.words + (t >> 5)] >> (t & 31) & 0xFFu : 0u;
-                keep[i / 4] = (keep[i / 4] & ~(0xFFu << (i % 4 * 8))) | x << (i % 4 * 8);
-            }
-        }
+        for (int i = 0; i < kShapeNodes; ++i) got[i] = (masked >> i & 1) && mine ? a.allow[(r0 + i) * a.words + (t >> 5)] : 0u;
+#pragma unroll
+        for (int i = 0; i < kShapeNodes; ++i)
+            if (masked >> i & 1) keep[i / 4] = (keep[i / 4] & ~(0xFFu << (i % 4 * 8))) | (got[i] >> (t & 31) & 0xFFu) << (i % 4 * 8);
+    }
 
     // the bias of each token (of several entries the last), drafted tokens of the span
     if (tid == 0) hits = 0;

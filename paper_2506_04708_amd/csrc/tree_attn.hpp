@@ -1,8 +1,7 @@
 // tree_attn.hpp -- attention of the nodes of a drafted tree over a paged key/value cache and over their own ancestors.
 #pragma once
 #include "attn_plan.hpp"
-#include <hip/hip_runtime.h>
-#include <stdint.h>
+#include "wave_ops.hpp"
 
 #include <type_traits>
 
@@ -104,25 +103,26 @@ struct AttnShape {
     static constexpr int D = D_, WR = WR_, WK = WK_, SUB = SUB_;
     static constexpr bool F16 = F16_;
     static constexpr int WAVES = WR * WK, THREADS = 64 * WAVES;
+    static constexpr int MIN_WAVES = 2;                // of a SIMD: 256 registers for each
     static constexpr int TM = 32 * WR;                 // query rows of a tile
     static constexpr int KT = 32 * WK * SUB;           // keys of a stage
     static constexpr bool ALONE = WR == 1;             // every wave loads the keys that it alone uses
-    static constexpr int NBUF = ALONE ? 2 : 3;
+    static constexpr int NBUF = ALONE ? 2 : 4;         // stages in LDS: two on their way, one in work, one whose values are still read
     static constexpr int ROW = 2 * D;                  // bytes of a key
     static constexpr int CPR = D / 8;                  // 16-byte chunks of a key
     static constexpr int KPI = 64 / CPR;               // keys of one copy instruction
-    static constexpr int LOADERS = WAVES >= 8 ? 8 : WAVES;  // waves that load
+    static constexpr int LOADERS = ALONE ? WAVES : WAVES >= 8 && KT / KPI >= 8 ? 8 : 4;  // waves that load (WAVES >= 4)
     static constexpr int KW = KT / LOADERS;            // keys that each of them loads per stage
     static constexpr int COPIES = 2 * KW / KPI;
     static constexpr int STAGE = 2 * KT * ROW;
-    static constexpr int IDS = NBUF * STAGE;           // LDS: stages | page ids [4][LOADERS][64] | node list | scratch
+    static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
+    static constexpr int IDS = NBUF * STAGE > SUMS ? NBUF * STAGE : SUMS;  // LDS: stages (unit sums before them) | page ids [4][LOADERS][64] | node list | scratch
     static constexpr int LIST = IDS + 4 * LOADERS * 256;
     static constexpr int MISC = LIST + 2048;
     static constexpr int BYTES = MISC + 256;
     static_assert(KW % KPI == 0 && KW >= KPI && KW <= 64, "a copy instruction brings whole keys of one wave");
     static_assert(!ALONE || LOADERS == WAVES, "every wave loads for itself");
     static_assert((WK - 1) * TM * (D + 2) * 4 <= NBUF * STAGE, "parts of the key waves are joined in the stages' memory");
-    static_assert(8 * (kAttnMaxBatch + 1) <= NBUF * STAGE, "unit sums are made in the stages' memory");
     // 16-byte chunk c of key k stands at chunk c ^ swizzle(k): reads of one chunk of 16 keys (K) and of four chunks of four
     // keys (V) touch every bank once
     static __device__ __forceinline__ int swizzle_k(int k) { return D == 128 ? k & 15 : (k >> 1) & 7; }
@@ -130,45 +130,79 @@ struct AttnShape {
 };
 
 // Units of work before each trajectory, prefix[0 .. B], in LDS: a unit is a stage of KT keys for one tile of rows and one
-// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of ceil(len / KT) + ceil(N / KT) units.
+// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of ceil(len / KT) + ceil(N / KT) units.  Every
+// workgroup counts all drafted nodes for itself, eight reads in flight (one after the other they took 17 us for 128 trees of
+// 128 nodes).
 template <int TM, int KT, int THREADS>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int b = threadIdx.x; b <= a.B; b += THREADS) prefix[b] = 0;
+    __syncthreads();
     int p2 = 1;
     while (p2 < a.N && p2 < 64) p2 <<= 1;
-    const int at_once = 64 / p2;                       // trajectories that a wave counts at once
-    for (int b0 = wave * at_once; b0 < a.B; b0 += THREADS / 64 * at_once) {
-        const int b = b0 + lane / p2;
-        int count = 0;
-        for (int u = lane % p2; u - lane % p2 < a.N; u += p2) {
-            const bool there = b < a.B && u < a.N && a.draft_tok[(long long)b * a.N + u] >= 0;
-            const unsigned long long bits = __ballot(there) >> (lane & ~(p2 - 1));
-            count += __popcll(p2 == 64 ? bits : bits & ((1ull << p2) - 1));
+    // a wave counts 64 / p2 trajectories at once, or 64 nodes of one
+    const int at_once = 64 / p2, per_b = (a.N + 63) / 64, rounds = (a.B + at_once - 1) / at_once * per_b;
+    const int turn = (int)(blockIdx.x * 5u % (unsigned)rounds);   // (not all of them the same line of the L2 at one time)
+    for (int i0 = wave; i0 < rounds; i0 += THREADS / 64 * 8) {
+        int tok[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int x = i0 + k * (THREADS / 64), i = x + turn < rounds ? x + turn : x + turn - rounds;
+            const int b = i / per_b * at_once + lane / p2, u = i % per_b * 64 + lane % p2;
+            const bool there = x < rounds && b < a.B && u < a.N;
+            const int v = a.draft_tok[there ? (long long)b * a.N + u : 0];   // (read by all: a branch would wait for each)
+            tok[k] = there ? v : -1;
         }
-        if (b < a.B && lane % p2 == 0) prefix[b + 1] = item_units(a.len[b], (long long)a.width << a.page_shift, a.N, KT) * tree_items(count, a.per_kv, a.kv_heads, TM);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int x = i0 + k * (THREADS / 64), i = x + turn < rounds ? x + turn : x + turn - rounds;
+            const int b = i / per_b * at_once + lane / p2;
+            const unsigned long long bits = __ballot(tok[k] >= 0) >> (lane & ~(p2 - 1));
+            const int count = __popcll(p2 == 64 ? bits : bits & ((1ull << p2) - 1));
+            if (x < rounds && count && lane % p2 == 0) atomicAdd((unsigned long long *)&prefix[b + 1], (unsigned long long)count);
+        }
     }
-    if (threadIdx.x == 0) prefix[0] = 0;
     __syncthreads();
     if (wave == 0) {
         long long base = 0;
         for (int b0 = 0; b0 < a.B; b0 += 64) {
-            long long x = b0 + lane < a.B ? prefix[b0 + lane + 1] : 0;
+            const int b = b0 + lane;
+            long long x = 0;
+            if (b < a.B) x = item_units(a.len[b], (long long)a.width << a.page_shift, a.N, KT) * tree_items((int)prefix[b + 1], a.per_kv, a.kv_heads, TM);
             for (int off = 1; off < 64; off <<= 1) {
                 const long long y = __shfl_up(x, off);
                 if (lane >= off) x += y;
             }
             x += base;
-            if (b0 + lane < a.B) prefix[b0 + lane + 1] = x;
+            if (b < a.B) prefix[b + 1] = x;
             base = __shfl(x, 63);
         }
     }
     __syncthreads();
 }
 
+// Rows of nodes that were not drafted: zeros, an equal number of rows for every workgroup.
 template <typename S>
-__global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_attn_kernel(TreeAttnArgs a)
+__device__ __forceinline__ void zero_rows(const TreeAttnArgs &a)
 {
+    const int lane = threadIdx.x & 63;
+    const long long all = (long long)a.B * a.N, r0 = all * blockIdx.x / a.groups, r1 = all * (blockIdx.x + 1) / a.groups;
+    for (long long x = r0; x < r1; x += 64) {
+        unsigned long long gone = __ballot(x + lane < r1 && a.draft_tok[x + lane < r1 ? x + lane : r0] < 0);
+        for (; gone; gone &= gone - 1) {
+            const long long r = x + __builtin_ctzll(gone);
+            for (int i = threadIdx.x; i < a.kv_heads * a.per_kv * S::CPR; i += S::THREADS)
+                *(uint4v *)(a.out + (r / a.N) * a.os[0] + (r % a.N) * a.os[1] + (i / S::CPR) * a.os[2] + i % S::CPR * 8) = uint4v{0, 0, 0, 0};
+        }
+    }
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(TreeAttnArgs args)
+{
+    // (every phase reads the arguments it needs anew: all of them at once do not fit the scalar registers)
+    const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
     constexpr int D = S::D, KT = S::KT, SUB = S::SUB, TM = S::TM, DT = D / 32, DC = D / 16;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int wr = wave % S::WR, wk = wave / S::WR, col = lane & 31, half = lane >> 5;
@@ -178,19 +212,16 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
     unit_sums<TM, KT, S::THREADS>(a, sums);
     const long long total = sums[a.B];
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.total = total;
-    // rows of nodes that were not drafted
-    for (int r = blockIdx.x; r < a.B * a.N; r += a.groups)
-        if (a.draft_tok[r] < 0)
-            for (int i = threadIdx.x; i < a.kv_heads * a.per_kv * S::CPR; i += S::THREADS)
-                *(uint4v *)(a.out + (r / a.N) * a.os[0] + (r % a.N) * a.os[1] + (i / S::CPR) * a.os[2] + i % S::CPR * 8) = uint4v{0, 0, 0, 0};
     const long long W = attn_groups(total, a.groups);
     // neighbours in the order of the work share an XCD (workgroups go round the eight of them in turn) and so its L2
     const int per_xcd = (int)((W + 7) / 8);
     const long long w = (long long)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
-    if ((int)blockIdx.x / 8 >= per_xcd || w >= W) return;
+    if ((int)blockIdx.x / 8 >= per_xcd || w >= W) {
+        zero_rows<S>(a);
+        return;
+    }
     long long unit = group_start(w, total, W);
     const long long unit_end = group_start(w + 1, total, W);
-    if (unit >= unit_end) return;
     int b = 0;
     {
         int lo = 0, hi = a.B - 1;                      // last b with sums[b] <= unit (and units of its own)
@@ -207,9 +238,12 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
     // weights are at most 2^8 (where the running maximum is left behind); fp16 ones are scaled up so that few are subnormal
     constexpr float kUp = S::F16 ? 6.0f : 0.0f;
 
-    while (unit < unit_end && b < a.B) {
+    const int B = a.B;
+    while (unit < unit_end && b < B) {
         // ---- the item: trajectory, key/value head, tile of rows ----
-        __syncthreads();
+        const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        group_barrier();                               // (not the fence of __syncthreads: it waits for the outputs' stores)
         uint16_t *list = (uint16_t *)(attn_lds + S::LIST);
         if (listed != b) {
             int base = 0;
@@ -230,7 +264,9 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
         const int per_item = (int)item_units(len, most, a.N, KT), cache_units = (len + KT - 1) / KT;
         const int tiles = tree_items(nodes, a.per_kv, 1, TM);
         const int item = (int)((unit - b_start) / per_item);
-        const int hk = item / tiles, tile = item % tiles;
+        // (trajectories begin with different heads: at one time the same head of all of them would use a part of the memory
+        // channels, where a token's heads stand side by side)
+        const int hk = (item / tiles + b) % a.kv_heads, tile = item % tiles;
         const long long item_start = b_start + (long long)item * per_item;
         const int u0 = (int)(unit - item_start);
         const int u1 = (int)(unit_end - item_start < per_item ? unit_end - item_start : per_item);
@@ -240,22 +276,14 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
             const long long from = group_of(item_start, total, W);
             leads = u0 > 0 && from == w - 1;
             if (threadIdx.x == 0)
-                a.join[w] = JoinRecord{(int)from, (int)group_of(item_start + per_item - 1, total, W), leads ? min(TM, nodes * a.per_kv - tile * TM) : 0, 0};
+                a.join[w] = JoinRecord{(int)from, (int)group_of(item_start + per_item - 1, total, W), leads ? min(rows_of_tile(nodes * a.per_kv, tiles), nodes * a.per_kv - tile * rows_of_tile(nodes * a.per_kv, tiles)) : 0, 0};
         }
-        const int rows = nodes * a.per_kv, row = tile * TM + wr * 32 + col;
-        const bool busy = tile * TM + wr * 32 < rows;  // this wave has rows
+        const int all_rows = nodes * a.per_kv, tile_rows = rows_of_tile(all_rows, tiles), row0 = tile * tile_rows;
+        const int rows = min(all_rows, row0 + tile_rows), row = row0 + wr * 32 + col;
+        const bool busy = row0 + wr * 32 < rows;       // this wave has rows
         const int my_row = row < rows ? row : rows - 1;
         const int node = list[my_row / a.per_kv], head = hk * a.per_kv + my_row % a.per_kv;
 
-        uint4v q[DC];
-        {
-            const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2] + 8 * half;
-#pragma unroll
-            for (int i = 0; i < DC; ++i) q[i] = *(const uint4v *)(qp + 16 * i);
-            // the wait for them belongs here: in the loop it would be one for the copies in flight as well
-#pragma unroll
-            for (int i = 0; i < DC; ++i) asm volatile("" : "+v"(q[i]));
-        }
         float16v o[DT];
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = float16v{0};
@@ -271,12 +299,15 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
         // ---- the units of this share: cached keys, then the tree's nodes; copies two stages ahead, page numbers two further ----
         const int n = u1 - u0, cached = cache_units - u0;       // units, those (if any) of the cache
         const int32_t *table = a.table + (long long)b * a.width;
+        const uint16_t *k_pool = a.k_pool + hk * a.pool_head, *v_pool = a.v_pool + hk * a.pool_head;
+        const long long pool_page = a.pool_page, pool_slot = a.pool_slot;
+        const int pages = a.pages, page_shift = a.page_shift;
         const int share = wave * S::KW;                         // this wave's keys of a stage (ALONE: those it uses)
         auto load_ids = [&](int i) {
             int key = (u0 + i) * KT + share + lane % S::KW;
             key = key < len ? key : len - 1;
             key = key > 0 ? key : 0;
-            copy4_async(table + (key >> a.page_shift), __builtin_amdgcn_readfirstlane(lds0 + S::IDS + wave * 256 + (i & 3) * (S::LOADERS * 256)));
+            copy4_async(table + (key >> page_shift), __builtin_amdgcn_readfirstlane(lds0 + S::IDS + wave * 256 + (i & 3) * (S::LOADERS * 256)));
         };
         auto load_stage = [&](int i) {
             const uint32_t buf = lds0 + (i % S::NBUF) * S::STAGE + share * S::ROW;
@@ -289,11 +320,12 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
                 if (i < cached) {
                     int key = (u0 + i) * KT + in_stage;
                     key = key < len ? key : len - 1;            // behind the end: the last key again, weighted with zero
-                    const long long page = clamp_page(id[at], a.pages);
-                    const long long from = page * a.pool_page + (key & ((1 << a.page_shift) - 1)) * a.pool_slot + hk * a.pool_head;
-                    kp = a.k_pool + from;
-                    vp = a.v_pool + from;
+                    const long long page = clamp_page(id[at], pages);
+                    const long long from = page * pool_page + (key & ((1 << page_shift) - 1)) * pool_slot;
+                    kp = k_pool + from;
+                    vp = v_pool + from;
                 } else {
+                    const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
                     int v = (i - cached) * KT + in_stage;
                     v = v < a.N ? v : a.N - 1;
                     kp = a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2];
@@ -303,156 +335,272 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
                 copy16_async(vp + ((ch ^ S::swizzle_v(in_stage)) << 3), __builtin_amdgcn_readfirstlane(buf + KT * S::ROW + r * S::KPI * S::ROW));
             }
         };
+        uint4v q[DC];
+        float16v s[SUB];
+        // Scores of a stage.  (The addresses are made opaque: what is added to them below is to become part of the instructions.
+        // The fences of the scheduler keep the reads of LDS ahead of their uses.)
+        auto scores = [&](uint32_t off, bool all, const uint32_t (&word)[SUB]) {
+            uint32_t ka = k_at + off;
+            asm volatile("" : "+v"(ka));
+#pragma unroll
+            for (int t = 0; t < SUB; ++t) {
+                uint4v kf[DC];
+#pragma unroll
+                for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)((ka ^ (x << 5)) + t * 32 * S::ROW);
+                if (t == 0) __builtin_amdgcn_sched_barrier(0);
+                s[t] = float16v{0};
+#pragma unroll
+                for (int x = 0; x < DC; ++x) s[t] = mfma32<S::F16>(kf[x], q[x], s[t]);
+            }
+            if (!all) {
+#pragma unroll
+                for (int t = 0; t < SUB; ++t) {
+                    const uint32_t w4 = word[t] >> (4 * half);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) s[t][x] = w4 & (1u << (8 * (x / 4) + x % 4)) ? s[t][x] : -__builtin_huge_valf();
+                }
+            }
+        };
+        // Weights of these scores, their products with the values.
+        auto values = [&](uint32_t off) {
+            uint32_t va = v_at + off;
+            asm volatile("" : "+v"(va));
+            uint4v vf[2][DT];
+            auto read_values = [&](int t) {
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        const uint32_t at = (va ^ (d << 6)) + (t * 32 + 16 * k) * S::ROW;
+                        const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
+                        const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
+                        vf[k][d] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
+            };
+            read_values(0);
+            __builtin_amdgcn_sched_barrier(0);
+            float top = s[0][0];
+#pragma unroll
+            for (int t = 0; t < SUB; ++t)
+#pragma unroll
+                for (int x = 0; x < 16; ++x) top = fmaxf(top, s[t][x]);
+            top = other_half_max(top) * c;
+            if (__ballot(top > m + 8.0f)) {            // seldom after the first stages: the old maximum will do
+                const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - next);
+                m = next;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[d][x] *= f;
+            }
+            const float shift = kUp - m;
+#pragma unroll
+            for (int t = 0; t < SUB; ++t) {
+                uint32_t p[8];
+#pragma unroll
+                for (int x = 0; x < 8; ++x) {
+                    p[x] = pack2<S::F16>(__builtin_amdgcn_exp2f(fmaf(s[t][2 * x], c, shift)), __builtin_amdgcn_exp2f(fmaf(s[t][2 * x + 1], c, shift)));
+                    l = add2<S::F16>(p[x], l);
+                }
+#pragma unroll
+                for (int k = 0; k < 2; ++k)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[d] = mfma32<S::F16>(vf[k][d], uint4v{p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]}, o[d]);
+                if (t + 1 < SUB) read_values(t + 1);
+            }
+        };
+        // The same, 32 keys at a time and one step apart: scores of these keys, in whose products' shadow the weights of the keys
+        // before are made; then the products of those with their values, beside the search for these keys' maximum.  A wave issues
+        // in order, so vector instructions between the matrix instructions are what keeps both units busy.
+        auto step = [&](const float16v &old, float16v &t, uint32_t k_off, uint32_t v_off, bool all, uint32_t word, bool last) {
+            uint32_t ka = k_at + k_off, va = v_at + v_off;
+            asm volatile("" : "+v"(ka), "+v"(va));
+            uint4v kf[DC], vf[2][DT];
+#pragma unroll
+            for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)(ka ^ (x << 5));
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const uint32_t at = (va ^ (d << 6)) + 16 * k * S::ROW;
+                    const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
+                    const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
+                    vf[k][d] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+            __builtin_amdgcn_sched_barrier(0);
+            const float shift = kUp - m;
+            constexpr int PER = 16 / DC;               // weights beside a matrix instruction
+            t = float16v{0};
+            uint32_t p[8];
+            float e[2][PER];
+#pragma unroll
+            for (int x = 0; x <= DC; ++x) {
+                if (x < DC) {
+                    t = mfma32<S::F16>(kf[x], q[x], t);
+#pragma unroll
+                    for (int y = 0; y < PER; ++y) e[x & 1][y] = __builtin_amdgcn_exp2f(fmaf(old[x * PER + y], c, shift));
+                }
+                if (x > 0) {
+#pragma unroll
+                    for (int y = 0; y < PER; y += 2) {
+                        const int at = ((x - 1) * PER + y) / 2;
+                        p[at] = pack2<S::F16>(e[(x - 1) & 1][y], e[(x - 1) & 1][y + 1]);
+                        l = add2<S::F16>(p[at], l);
+                        asm volatile("" : "+v"(p[at]), "+v"(l));   // (made here, not where they are used)
+                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (!all) {
+                const uint32_t w4 = word >> (4 * half);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) t[x] = w4 & (1u << (8 * (x / 4) + x % 4)) ? t[x] : -__builtin_huge_valf();
+            }
+            float top = t[0];
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const uint4v pf = {p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]};
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    o[d] = mfma32<S::F16>(vf[k][d], pf, o[d]);
+                    constexpr int EACH = 8 / DT;
+#pragma unroll
+                    for (int y = 0; y < EACH; ++y) top = fmaxf(top, t[(k * DT + d) * EACH + y]);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            }
+            top = other_half_max(top) * c;
+            if (__ballot(!last && top > m + 8.0f)) {   // seldom after the first stages: the old maximum will do
+                const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - next);
+                m = next;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) o[d][x] *= f;
+            }
+        };
         const bool loads = wave < S::LOADERS;
+        if (loads) { load_ids(0); load_ids(1); load_ids(2); }
+        {
+            const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2] + 8 * half;
+#pragma unroll
+            for (int i = 0; i < DC; ++i) q[i] = *(const uint4v *)(qp + 16 * i);
+            // the wait for them belongs here: in the loop it would be one for the copies in flight as well
+#pragma unroll
+            for (int i = 0; i < DC; ++i) asm volatile("" : "+v"(q[i]));
+        }
+        wait_loads<0>();
         if (loads) {
-            load_ids(0); load_ids(1); load_ids(2);
-            wait_loads<0>();
             load_stage(0);
             if (n > 1) { load_ids(3); load_stage(1); }
         }
-        for (int i = 0; i < n; ++i) {
-            const uint32_t off = (i % S::NBUF) * S::STAGE;
-            if (i + 1 < n) wait_loads<S::COPIES + 1>();         // (the stage's own copies are all older than the newest that many)
+        uint32_t *odd = (uint32_t *)(attn_lds + S::MISC);       // [N / 32]: nodes with a value that is no finite number
+        if (threadIdx.x < 32) odd[threadIdx.x] = 0;
+        // A unit that has come: everyone's copies are there, two units ahead are on their way, the tree's values are finite.
+        // -> the keys of this wave's subtile t that count for this lane's query: bits, `all` of them.
+        auto arrive = [&](int i) {
+            if (i + 1 < n) wait_loads<S::COPIES + 1>();         // (the unit's own copies are all older than the newest that many)
             else wait_loads<0>();
             if constexpr (!S::ALONE) {
-                group_barrier();                                // everyone's copies are there, and everyone is done with the stage before
+                group_barrier();                                // ... and everyone is done with the unit two before
                 if (loads && i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
-            uint32_t word[SUB];                                 // keys of this wave that count, for this lane's query
-            bool all = false, some;
-            if (i < cached) {
-                const int left = len - (u0 + i) * KT - wk * SUB * 32;
-                all = left >= 32 * SUB;
-                some = busy && left > 0;
+            if (i < cached) return;
+            // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
+            // zeros here, and the rows that see them get them added below.
+            const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
+            const uint32_t off = (i % S::NBUF) * S::STAGE;
+            __syncthreads();
+            for (int x = threadIdx.x; x < KT * S::CPR; x += S::THREADS) {
+                lds_uint4v *vp = (lds_uint4v *)(uintptr_t)(lds0 + off + KT * S::ROW + x * 16);
+                uint4v vw = *vp;
+                constexpr uint32_t kExp = S::F16 ? 0x7C00u : 0x7F80u;
+                bool found = false;
 #pragma unroll
-                for (int t = 0; t < SUB; ++t) word[t] = left >= 32 * (t + 1) ? ~0u : (left <= 32 * t ? 0u : (1u << (left - 32 * t)) - 1u);
-            } else {
-                const int v0 = (i - cached) * KT;               // the unit's first node
-                uint32_t any = 0;
-#pragma unroll
-                for (int t = 0; t < SUB; ++t) {
-                    const int at = v0 / 32 + wk * SUB + t;
-                    word[t] = busy && at * 32 < a.N ? a.anc[(long long)node * a.anc_words + at] : 0u;   // a node sees its ancestors and itself
-                    any |= word[t];
+                for (int e = 0; e < 4; ++e) {
+                    const bool lo = (vw[e] & kExp) == kExp, hi = ((vw[e] >> 16) & kExp) == kExp;
+                    found |= lo | hi;
+                    vw[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
                 }
-                some = __ballot(any != 0) != 0;
-                // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
-                // zeros here, and the rows that see them get them added below.
-                uint32_t *odd = (uint32_t *)(attn_lds + S::MISC);
-                if constexpr (S::ALONE) __syncthreads();        // (a wave may still read those of the unit before)
-                if (threadIdx.x < KT / 32) odd[threadIdx.x] = 0;
-                __syncthreads();
-                for (int x = threadIdx.x; x < KT * S::CPR; x += S::THREADS) {
-                    lds_uint4v *vp = (lds_uint4v *)(uintptr_t)(lds0 + off + KT * S::ROW + x * 16);
-                    uint4v vw = *vp;
-                    constexpr uint32_t kExp = S::F16 ? 0x7C00u : 0x7F80u;
-                    bool found = false;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const bool lo = (vw[e] & kExp) == kExp, hi = ((vw[e] >> 16) & kExp) == kExp;
-                        found |= lo | hi;
-                        vw[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-                    }
-                    if (found) {
-                        *vp = vw;
-                        atomicOr(&odd[x / S::CPR / 32], 1u << (x / S::CPR & 31));
-                    }
+                if (found) {
+                    *vp = vw;
+                    const int v = (i - cached) * KT + x / S::CPR;
+                    if (v < a.N) atomicOr(&odd[v / 32], 1u << (v & 31));
                 }
-                __syncthreads();
             }
-            if (some) {
-                // scores, weights, products with the values.  (The addresses are made opaque: what is added to them below is to
-                // become part of the instructions.  The fences of the scheduler keep the reads of LDS ahead of their uses.)
-                uint32_t ka = k_at + off, va = v_at + off;
-                asm volatile("" : "+v"(ka), "+v"(va));
-                float16v s[SUB];
-                uint4v kf[SUB][DC];
-#pragma unroll
-                for (int t = 0; t < SUB; ++t)
-#pragma unroll
-                    for (int x = 0; x < DC; ++x) kf[t][x] = *(const lds_uint4v *)(uintptr_t)((ka ^ (x << 5)) + t * 32 * S::ROW);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int t = 0; t < SUB; ++t) {
-                    s[t] = float16v{0};
-#pragma unroll
-                    for (int x = 0; x < DC; ++x) s[t] = mfma32<S::F16>(kf[t][x], q[x], s[t]);
+            __syncthreads();
+        };
+        auto counting = [&](int i, int t, bool &all) {
+            const int first = wk * SUB * 32 + t * 32;           // the subtile's first key in the unit
+            all = false;
+            if (i < cached) {
+                const int left = len - (u0 + i) * KT - first;
+                all = left >= 32;
+                return left >= 32 ? ~0u : (left <= 0 ? 0u : (1u << left) - 1u);
+            }
+            const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
+            const int v = (i - cached) * KT + first;            // a node sees its ancestors and itself
+            uint32_t word = busy && v < a.N ? a.anc[(long long)node * a.anc_words + v / 32] : 0u;
+            asm volatile("" : "+v"(word));                      // (waited for here: elsewhere it would be a wait for the copies too)
+            return word;
+        };
+        if constexpr (S::ALONE) {
+            for (int i = 0; i < n; ++i) {
+                const uint32_t off = (i % S::NBUF) * S::STAGE;
+                arrive(i);
+                bool all;
+                const uint32_t word[1] = {counting(i, 0, all)};
+                if (__ballot(word[0] != 0)) {
+                    scores(off, all, word);
+                    values(off);
                 }
-                uint4v vf[2][DT];
-                auto read_values = [&](int t) {
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
+            }
+        } else {
+            float16v even, odd_s;                               // scores of every other subtile: they change places, not registers
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) {
-                            const uint32_t at = (va ^ (d << 6)) + (t * 32 + 16 * k) * S::ROW;
-                            const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
-                            const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
-                            vf[k][d] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-                        }
-                };
-                read_values(0);
-                __builtin_amdgcn_sched_barrier(0);
-                if (!all) {
-#pragma unroll
-                    for (int t = 0; t < SUB; ++t) {
-                        const uint32_t w4 = word[t] >> (4 * half);
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) s[t][x] = w4 & (1u << (8 * (x / 4) + x % 4)) ? s[t][x] : -__builtin_huge_valf();
-                    }
+            for (int x = 0; x < 16; ++x) even[x] = -__builtin_huge_valf();
+            uint32_t before = 0;
+            const int steps = n * SUB;
+            auto subtile = [&](int j, const float16v &old, float16v &now) {
+                const bool last = j == steps;                   // (no new keys)
+                if (!last && j % SUB == 0) arrive(j / SUB);
+                bool all = true;
+                uint32_t word = 0, off = before;
+                if (!last) {
+                    word = counting(j / SUB, j % SUB, all);
+                    off = (j / SUB % S::NBUF) * S::STAGE + j % SUB * 32 * S::ROW;
                 }
-                float top = s[0][0];
-#pragma unroll
-                for (int t = 0; t < SUB; ++t)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) top = fmaxf(top, s[t][x]);
-                top = other_half_max(top) * c;
-                if (__ballot(top > m + 8.0f)) {                 // seldom after the first stages: the old maximum will do
-                    const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - next);
-                    m = next;
-                    l *= f;
+                // (before the first keys: no weight at all, and values that are there)
+                if (busy) step(old, now, off, j == 0 ? off : before, all, word, last);
+                before = off;
+            };
+            for (int j = 0; j <= steps; j += 2) {
+                subtile(j, even, odd_s);
+                if (j < steps) subtile(j + 1, odd_s, even);
+            }
+        }
+        if (busy && u1 > cache_units) {
+            const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
+            for (int x = 0; x < (a.N + 31) / 32; ++x) {
+                if (x % (KT / 32) / SUB != wk) continue;
+                for (uint32_t bits = odd[x]; bits; bits &= bits - 1) {
+                    // an infinity or NaN reaches the rows that see its node, whatever its weight
+                    const int v = 32 * x + __builtin_ctz(bits);
+                    const bool sees = (a.anc[(long long)node * a.anc_words + x] >> (v & 31)) & 1u;
+                    const uint16_t *vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2] + 4 * half;
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
 #pragma unroll
-                        for (int x = 0; x < 16; ++x) o[d][x] *= f;
+                        for (int e = 0; e < 16; ++e) {
+                            const uint16_t h = vp[32 * d + 8 * (e / 4) + e % 4];
+                            const float y = S::F16 ? (float)__builtin_bit_cast(_Float16, h) : __uint_as_float((uint32_t)h << 16);
+                            if (sees && !(fabsf(y) < __builtin_huge_valf())) o[d][e] += y;
+                        }
                 }
-                const float shift = kUp - m;
-#pragma unroll
-                for (int t = 0; t < SUB; ++t) {
-                    uint32_t p[8];
-#pragma unroll
-                    for (int x = 0; x < 8; ++x) {
-                        p[x] = pack2<S::F16>(__builtin_amdgcn_exp2f(fmaf(s[t][2 * x], c, shift)), __builtin_amdgcn_exp2f(fmaf(s[t][2 * x + 1], c, shift)));
-                        l = add2<S::F16>(p[x], l);
-                    }
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int d = 0; d < DT; ++d) o[d] = mfma32<S::F16>(vf[k][d], uint4v{p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]}, o[d]);
-                    if (t + 1 < SUB) read_values(t + 1);
-                }
-            }
-            if (i >= cached && busy) {
-                const uint32_t *odd = (const uint32_t *)(attn_lds + S::MISC);
-                for (int t = 0; t < SUB; ++t)
-                    for (uint32_t bits = odd[wk * SUB + t]; bits; bits &= bits - 1) {
-                        // an infinity or NaN reaches the rows that see its node, whatever its weight
-                        const int k = __builtin_ctz(bits), v = (i - cached) * KT + (wk * SUB + t) * 32 + k;
-                        if (v >= a.N) break;
-                        const bool sees = (a.anc[(long long)node * a.anc_words + v / 32] >> k) & 1u;
-                        const uint16_t *vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2] + 4 * half;
-#pragma unroll
-                        for (int d = 0; d < DT; ++d)
-#pragma unroll
-                            for (int x = 0; x < 16; ++x) {
-                                const uint16_t h = vp[32 * d + 8 * (x / 4) + x % 4];
-                                const float y = S::F16 ? (float)__builtin_bit_cast(_Float16, h) : __uint_as_float((uint32_t)h << 16);
-                                if (sees && !(fabsf(y) < __builtin_huge_valf())) o[d][x] += y;
-                            }
-                    }
-            }
-            if constexpr (S::ALONE) {
-                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
         }
 
@@ -494,6 +642,7 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
             }
         }
         if (wk == 0 && row < rows) {
+            const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
             if (u0 == 0 && u1 == per_item) {
                 const float r = 1.0f / l;
                 uint16_t *op = a.out + b * a.os[0] + node * a.os[1] + head * a.os[2] + 4 * half;
@@ -503,32 +652,36 @@ __global__ __launch_bounds__(S::THREADS, S::THREADS == 512 ? 2 : 1) void tree_at
                     for (int i = 0; i < 4; ++i)
                         *(uint2 *)(op + 32 * d + 8 * i) = uint2{pack2<S::F16>(o[d][4 * i] * r, o[d][4 * i + 1] * r), pack2<S::F16>(o[d][4 * i + 2] * r, o[d][4 * i + 3] * r)};
             } else {
-                float *to = a.part + (2 * w + (u0 == 0)) * (long long)TM * (D + 2);
+                // (as the registers stand, so that every store is one run of 1 KiB)
+                float *to = a.part + (2 * w + (u0 == 0)) * (long long)(TM * (D + 2));
                 const int at = wr * 32 + col;
                 if (half == 0) { to[at] = m; to[TM + at] = l; }
-                to += 2 * TM + at * D + 4 * half;
+                float4v *to4 = (float4v *)(to + 2 * TM) + wr * (4 * DT * 64) + lane;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) *(float4v *)(to + 32 * d + 8 * i) = float4v{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+                    for (int i = 0; i < 4; ++i) to4[(4 * d + i) * 64] = float4v{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
                 if (leads && half == 0) a.place[w * TM + at] = b * a.os[0] + node * a.os[1] + head * a.os[2];
             }
         }
         unit = item_start + u1;
-        if (unit == b_start + (long long)per_item * tiles * a.kv_heads) { b_start = unit; ++b; }
+        if (unit == b_start + (long long)per_item * tiles * fresh_args<TreeAttnArgs>().kv_heads) { b_start = unit; ++b; }
     }
+    zero_rows<S>(fresh_args<TreeAttnArgs>());          // (last: the first ones to be done have the time)
 }
 
-// Rows of items that several workgroups took: their parts joined.  A task is four rows of an item, one for each wave, or one
-// row whose parts the waves share where there are many.  Every workgroup sums up the records for itself and takes every
-// gridDim.x-th task.  A lane holds D / 64 elements, and the weight of one part in 64.
+// Rows of items that several workgroups took: their parts joined, 32 rows (those of one wave) at a time and in the layout of its
+// registers: lane l has the row l % 32 and every second group of four elements.  Each wave takes a quarter of the elements of all
+// parts; where there are many parts, a workgroup takes one quarter and its waves share the parts.  Every workgroup sums up the
+// records for itself and takes every gridDim.x-th task.
 constexpr int kJoinShared = 8;        // more parts: the waves share them
 template <int D, int TM, bool F16>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
 {
-    constexpr int E = D / 64;
+    constexpr int Q = D / 32;                          // groups of four elements in a quarter of a lane's
+    constexpr long long kSlot = TM * (D + 2);
     __shared__ int tasks[kAttnMaxGroups + 1], wave_sum[4];
-    __shared__ float shared[4][D + 2];
+    __shared__ float shared[4][4 * Q + 2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int W = (int)attn_groups(*a.total, a.groups), per = (W + 255) / 256;
     int sum = 0;
@@ -536,7 +689,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
         const int w = threadIdx.x * per + i;
         if (w < W) {
             const JoinRecord r = a.join[w];
-            sum += r.last - r.first + 1 > kJoinShared ? r.rows : (r.rows + 3) / 4;
+            sum += (r.rows + 31) / 32 * (r.last - r.first + 1 > kJoinShared ? 4 : 1);
             tasks[w + 1] = sum;
         }
     }
@@ -563,59 +716,72 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
         const int w = __builtin_amdgcn_readfirstlane(lo), sub = task - tasks[w];
         const JoinRecord r = a.join[w];
         const bool share = r.last - r.first + 1 > kJoinShared;
-        const int at = share ? sub : sub * 4 + wave;
+        const int wr = share ? sub / 4 : sub, quarter = share ? sub % 4 : wave;
         const int step = share ? 4 : 1, from = share ? r.first + wave : r.first;
-        float acc[E], top = -1e38f, l = 0.0f;
+        const int at = wr * 32 + (lane & 31);
+        const long long place = at < r.rows ? a.place[(long long)w * TM + at] : 0;
+        float4v acc[Q];
+        float top = -1e38f, l = 0.0f;
 #pragma unroll
-        for (int e = 0; e < E; ++e) acc[e] = 0.0f;
-        const int parts = at < r.rows && from <= r.last ? (r.last - from) / step + 1 : 0;
-        for (int k1 = 0; k1 < parts; k1 += 64) {
-            const int here = min(parts - k1, 64), g = from + (k1 + min(lane, here - 1)) * step;
-            const float *mine = a.part + (2 * g + (g == r.first)) * (long long)(TM * (D + 2));
-            const float m = lane < here ? mine[at] : -1e38f, x = lane < here ? mine[TM + at] : 0.0f;
-            float best = m;
-            for (int off = 32; off > 0; off >>= 1) best = fmaxf(best, __shfl_xor(best, off));
-            best = fmaxf(best, top);
-            const float f = __builtin_amdgcn_exp2f(top - best), weight = __builtin_amdgcn_exp2f(m - best);
-            top = best;
-            l = fmaf(weight, x, l * f);
+        for (int i = 0; i < Q; ++i) acc[i] = float4v{0, 0, 0, 0};
+        for (int g0 = from; g0 <= r.last; g0 += 4 * step) {
+            float m[4], x[4];
+            float4v p[4][Q];
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] *= f;
-            for (int k0 = 0; k0 < here; k0 += 8) {
+            for (int k = 0; k < 4; ++k) {              // (past the last one: that one again, with no weight)
+                const int g = min(g0 + k * step, r.last);
+                const float *slot = a.part + (2 * g + (g == r.first)) * kSlot;
+                m[k] = slot[at]; x[k] = slot[TM + at];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {
-                    const int k = min(k0 + j, here - 1), gk = from + (k1 + k) * step;
-                    const float *p = a.part + (2 * gk + (gk == r.first)) * (long long)(TM * (D + 2)) + 2 * TM + at * D + lane * E;
-                    const float y = __shfl(weight, k);
-#pragma unroll
-                    for (int e = 0; e < E; ++e) acc[e] = fmaf(k0 + j < here ? y : 0.0f, k0 + j < here ? p[e] : 0.0f, acc[e]);
-                }
+                for (int i = 0; i < Q; ++i) p[k][i] = ((const float4v *)(slot + 2 * TM))[(wr * (4 * Q) + quarter * Q + i) * 64 + lane];
             }
-        }
-        for (int off = 32; off > 0; off >>= 1) l += __shfl_xor(l, off);
-        if (share) {
-            __syncthreads();                           // (the task before is done with them)
+            float best = top;
 #pragma unroll
-            for (int e = 0; e < E; ++e) shared[wave][lane * E + e] = acc[e];
-            if (lane == 0) { shared[wave][D] = top; shared[wave][D + 1] = l; }
-            __syncthreads();
-            if (wave > 0) continue;
-            const float best = fmaxf(fmaxf(shared[0][D], shared[1][D]), fmaxf(shared[2][D], shared[3][D]));
-            l = 0.0f;
+            for (int k = 0; k < 4; ++k) best = fmaxf(best, m[k]);
+            const float f = __builtin_amdgcn_exp2f(top - best);
+            top = best;
+            l *= f;
 #pragma unroll
-            for (int e = 0; e < E; ++e) acc[e] = 0.0f;
+            for (int i = 0; i < Q; ++i) acc[i] = acc[i] * f;
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float f = __builtin_amdgcn_exp2f(shared[k][D] - best);
-                l = fmaf(f, shared[k][D + 1], l);
+                if (g0 + k * step > r.last) continue;
+                const float y = __builtin_amdgcn_exp2f(m[k] - best);
+                l = fmaf(y, x[k], l);
 #pragma unroll
-                for (int e = 0; e < E; ++e) acc[e] = fmaf(f, shared[k][lane * E + e], acc[e]);
+                for (int i = 0; i < Q; ++i)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(y, p[k][i][e], acc[i][e]);
+            }
+        }
+        if (share) {
+            __syncthreads();                           // (the task before is done with them)
+            shared[wave][4 * Q][lane] = top;
+            shared[wave][4 * Q + 1][lane] = l;
+#pragma unroll
+            for (int i = 0; i < 4 * Q; ++i) shared[wave][i][lane] = acc[i / 4][i % 4];
+            __syncthreads();
+            if (wave > 0) continue;
+            const float best = fmaxf(fmaxf(shared[0][4 * Q][lane], shared[1][4 * Q][lane]), fmaxf(shared[2][4 * Q][lane], shared[3][4 * Q][lane]));
+            l = 0.0f;
+#pragma unroll
+            for (int i = 0; i < Q; ++i) acc[i] = float4v{0, 0, 0, 0};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float f = __builtin_amdgcn_exp2f(shared[k][4 * Q][lane] - best);
+                l = fmaf(f, shared[k][4 * Q + 1][lane], l);
+#pragma unroll
+                for (int i = 0; i < 4 * Q; ++i) acc[i / 4][i % 4] = fmaf(f, shared[k][i][lane], acc[i / 4][i % 4]);
             }
         }
         if (at >= r.rows) continue;
-        uint16_t *o = a.out + a.place[(long long)w * TM + at] + lane * E;
-        if constexpr (E == 2) *(uint32_t *)o = pack2<F16>(acc[0] / l, acc[1] / l);
-        else o[0] = (uint16_t)pack2<F16>(acc[0] / l, 0.0f);
+        // group j of a lane's: elements 32 (j / 4) + 8 (j % 4) + 4 (lane / 32) and the three behind
+        uint16_t *o = a.out + place + 4 * (lane >> 5);
+#pragma unroll
+        for (int i = 0; i < Q; ++i) {
+            const int j = quarter * Q + i;
+            *(uint2 *)(o + 32 * (j / 4) + 8 * (j % 4)) = uint2{pack2<F16>(acc[i][0] / l, acc[i][1] / l), pack2<F16>(acc[i][2] / l, acc[i][3] / l)};
+        }
     }
 }
 
