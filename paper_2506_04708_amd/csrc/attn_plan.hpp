@@ -16,8 +16,6 @@ namespace stand {
 
 constexpr int kAttnMaxBatch = 4096;   // trajectories of a call: their unit sums are made in LDS
 constexpr int kAttnMaxGroups = 2048;  // workgroups of a launch: their records are summed up in LDS
-constexpr int kAttnMinUnits = 2;      // a share is no smaller: a part costs about as much as a unit to write and join
-
 STAND_BOTH long long clamp_length(long long len, long long most) { return len < 0 ? 0 : (len > most ? most : len); }
 STAND_BOTH int clamp_page(int page, int pages) { return page < 0 ? 0 : (page >= pages ? pages - 1 : page); }
 
@@ -33,14 +31,22 @@ STAND_BOTH int tree_items(int drafted, int per_kv, int kv_heads, int tile_rows)
 }
 // Rows of each of a head's tiles but the last: equal ones, in whole waves.
 STAND_BOTH int rows_of_tile(int rows, int tiles) { return ((rows + tiles - 1) / tiles + 31) / 32 * 32; }
-// Workgroups that get a share, of `groups` launched.
-STAND_BOTH long long attn_groups(long long total, int groups)
+// What an item costs beside its units (nodes, queries, page numbers and first keys to wait for) counts as `start` units at its
+// beginning, so that shares of many short items are no longer than others.  A share that would begin or end among them begins
+// or ends at the item's beginning instead.
+// Workgroups that get a share, of `groups` launched: no share is shorter than start + 2.
+STAND_BOTH long long attn_groups(long long total, int groups, int start)
 {
-    const long long w = (total + kAttnMinUnits - 1) / kAttnMinUnits;
-    return w < groups ? w : groups;
+    const long long w = total / (start + 2);
+    return w >= groups ? groups : w > 0 ? w : total > 0;
 }
 STAND_BOTH long long group_start(long long w, long long total, long long W) { return w * total / W; }
-// The workgroup whose share holds a unit: the last one that starts at or before it.
+// The last workgroup whose share would begin at or before a unit.
 STAND_BOTH long long group_of(long long unit, long long total, long long W) { return ((unit + 1) * W - 1) / total; }
+// The workgroup that has an item's first part.
+STAND_BOTH long long first_group(long long item_start, long long total, long long W, int start)
+{
+    return group_of(item_start + start, total, W);
+}
 
 }  // namespace stand

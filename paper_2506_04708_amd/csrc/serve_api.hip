@@ -119,7 +119,7 @@ hipError_t attn_launch(TreeAttnArgs &a, int cus, hipStream_t s)
     a.place = (long long *)(a.join + a.groups);
     a.part = (float *)(a.place + (size_t)a.groups * S::TM);
     tree_attn_kernel<S><<<dim3((unsigned)a.groups), dim3(S::THREADS), S::BYTES, s>>>(a);
-    tree_attn_join_kernel<S::D, S::TM, S::F16><<<dim3(4u * (unsigned)cus), dim3(256), 0, s>>>(a);
+    tree_attn_join_kernel<S::D, S::TM, S::F16, S::START><<<dim3(4u * (unsigned)cus), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 

@@ -107,7 +107,9 @@ struct AttnShape {
     static constexpr int TM = 32 * WR;                 // query rows of a tile
     static constexpr int KT = 32 * WK * SUB;           // keys of a stage
     static constexpr bool ALONE = WR == 1;             // every wave loads the keys that it alone uses
+    static constexpr bool SPLIT = WR == 8 && WK == 1 && SUB == 2;  // groups of rows may be shared by two waves, see the kernel
     static constexpr int NBUF = ALONE ? 2 : 4;         // stages in LDS: two on their way, one in work, one whose values are still read
+    static constexpr int START = ALONE ? 2 : D == 64 ? 8 : 4;  // units that the beginning of an item costs, see attn_plan.hpp
     static constexpr int ROW = 2 * D;                  // bytes of a key
     static constexpr int CPR = D / 8;                  // 16-byte chunks of a key
     static constexpr int KPI = 64 / CPR;               // keys of one copy instruction
@@ -130,10 +132,11 @@ struct AttnShape {
 };
 
 // Units of work before each trajectory, prefix[0 .. B], in LDS: a unit is a stage of KT keys for one tile of rows and one
-// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of ceil(len / KT) + ceil(N / KT) units.  Every
+// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) +
+// ceil(N / KT) units.  Every
 // workgroup counts all drafted nodes for itself, eight reads in flight (one after the other they took 17 us for 128 trees of
 // 128 nodes).
-template <int TM, int KT, int THREADS>
+template <int TM, int KT, int THREADS, int START>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -169,7 +172,7 @@ __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *pref
         for (int b0 = 0; b0 < a.B; b0 += 64) {
             const int b = b0 + lane;
             long long x = 0;
-            if (b < a.B) x = item_units(a.len[b], (long long)a.width << a.page_shift, a.N, KT) * tree_items((int)prefix[b + 1], a.per_kv, a.kv_heads, TM);
+            if (b < a.B) x = (START + item_units(a.len[b], (long long)a.width << a.page_shift, a.N, KT)) * tree_items((int)prefix[b + 1], a.per_kv, a.kv_heads, TM);
             for (int off = 1; off < 64; off <<= 1) {
                 const long long y = __shfl_up(x, off);
                 if (lane >= off) x += y;
@@ -209,10 +212,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char *)attn_lds);
 
     long long *sums = (long long *)attn_lds;
-    unit_sums<TM, KT, S::THREADS>(a, sums);
+    unit_sums<TM, KT, S::THREADS, S::START>(a, sums);
     const long long total = sums[a.B];
     if (blockIdx.x == 0 && threadIdx.x == 0) *a.total = total;
-    const long long W = attn_groups(total, a.groups);
+    const long long W = attn_groups(total, a.groups, S::START);
     // neighbours in the order of the work share an XCD (workgroups go round the eight of them in turn) and so its L2
     const int per_xcd = (int)((W + 7) / 8);
     const long long w = (long long)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
@@ -261,26 +264,41 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         if (nodes == 0) { ++b; continue; }             // nothing drafted: no units
         const long long most = (long long)a.width << a.page_shift;
         const int len = __builtin_amdgcn_readfirstlane((int)clamp_length(a.len[b], most));
-        const int per_item = (int)item_units(len, most, a.N, KT), cache_units = (len + KT - 1) / KT;
+        const int units = (int)item_units(len, most, a.N, KT), cache_units = (len + KT - 1) / KT, per_item = units + S::START;
         const int tiles = tree_items(nodes, a.per_kv, 1, TM);
         const int item = (int)((unit - b_start) / per_item);
         // (trajectories begin with different heads: at one time the same head of all of them would use a part of the memory
         // channels, where a token's heads stand side by side)
         const int hk = (item / tiles + b) % a.kv_heads, tile = item % tiles;
         const long long item_start = b_start + (long long)item * per_item;
-        const int u0 = (int)(unit - item_start);
-        const int u1 = (int)(unit_end - item_start < per_item ? unit_end - item_start : per_item);
+        if (unit_end - item_start <= S::START) break;  // the next one's
+        const int u0 = unit - item_start <= S::START ? 0 : (int)(unit - item_start) - S::START;
+        const int u1 = unit_end - item_start < per_item ? (int)(unit_end - item_start) - S::START : units;
         bool leads = false;                            // this share is the second one of its first item
         if (first_item) {
             first_item = false;
-            const long long from = group_of(item_start, total, W);
+            const long long from = first_group(item_start, total, W, S::START);
             leads = u0 > 0 && from == w - 1;
-            if (threadIdx.x == 0)
+            if (threadIdx.x == 0)                      // (every share writes its record: no share ends before its first item begins)
                 a.join[w] = JoinRecord{(int)from, (int)group_of(item_start + per_item - 1, total, W), leads ? min(rows_of_tile(nodes * a.per_kv, tiles), nodes * a.per_kv - tile * rows_of_tile(nodes * a.per_kv, tiles)) : 0, 0};
         }
         const int all_rows = nodes * a.per_kv, tile_rows = rows_of_tile(all_rows, tiles), row0 = tile * tile_rows;
-        const int rows = min(all_rows, row0 + tile_rows), row = row0 + wr * 32 + col;
-        const bool busy = row0 + wr * 32 < rows;       // this wave has rows
+        const int rows = min(all_rows, row0 + tile_rows);
+        // 32 rows for a wave and all keys of a stage; but of five or six such groups the last ones take two waves each, for half of
+        // the keys, so that no SIMD (waves w and w + 4) has four subtiles of a stage where another one has two
+        int wrow = wr, part = 0;
+        bool halved = false, halved_any = false;
+        if constexpr (S::SPLIT) {
+            const int have = (rows - row0 + 31) / 32;
+            halved_any = have == 5 || have == 6;
+            if (halved_any && wave >= 4) {
+                halved = true;
+                wrow = 4 + (wave - 4) % (have - 4);
+                part = (wave - 4) / (have - 4);
+            }
+        }
+        const int row = row0 + wrow * 32 + col;
+        const bool busy = row0 + wrow * 32 < rows && part < 2;  // this wave has rows
         const int my_row = row < rows ? row : rows - 1;
         const int node = list[my_row / a.per_kv], head = hk * a.per_kv + my_row % a.per_kv;
 
@@ -564,15 +582,16 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
             for (int x = 0; x < 16; ++x) even[x] = -__builtin_huge_valf();
             uint32_t before = 0;
-            const int steps = n * SUB;
+            const int steps = halved ? n : n * SUB;             // subtiles of this wave
             auto subtile = [&](int j, const float16v &old, float16v &now) {
                 const bool last = j == steps;                   // (no new keys)
-                if (!last && j % SUB == 0) arrive(j / SUB);
+                const int i = halved ? j : j / SUB, t = halved ? part & 1 : j % SUB;
+                if (!last && (halved || t == 0)) arrive(i);
                 bool all = true;
                 uint32_t word = 0, off = before;
                 if (!last) {
-                    word = counting(j / SUB, j % SUB, all);
-                    off = (j / SUB % S::NBUF) * S::STAGE + j % SUB * 32 * S::ROW;
+                    word = counting(i, t, all);
+                    off = (i % S::NBUF) * S::STAGE + t * 32 * S::ROW;
                 }
                 // (before the first keys: no weight at all, and values that are there)
                 if (busy) step(old, now, off, j == 0 ? off : before, all, word, last);
@@ -586,7 +605,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         if (busy && u1 > cache_units) {
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
             for (int x = 0; x < (a.N + 31) / 32; ++x) {
-                if (x % (KT / 32) / SUB != wk) continue;
+                if (x % (KT / 32) / SUB != wk || (halved && x % SUB != part)) continue;
                 for (uint32_t bits = odd[x]; bits; bits &= bits - 1) {
                     // an infinity or NaN reaches the rows that see its node, whatever its weight
                     const int v = 32 * x + __builtin_ctz(bits);
@@ -606,11 +625,15 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 
         // ---- the key waves' parts joined, then the rows' outputs or this workgroup's part of them ----
         l = other_half_sum(l);
-        if constexpr (S::WK > 1) {
+        constexpr int PARTS = S::SPLIT ? 2 : S::WK;
+        const int key_part = S::SPLIT ? part : wk;
+        if (S::WK > 1 || (S::SPLIT && halved_any)) {
             __syncthreads();
-            float *join = (float *)attn_lds;           // [WK - 1][WR][16 DT + 2][64]
-            if (wk > 0) {
-                float *to = join + ((wk - 1) * S::WR + wr) * (16 * DT + 2) * 64 + lane;
+            float *join = (float *)attn_lds;           // [PARTS - 1][groups of rows][16 DT + 2][64]
+            const int group = S::SPLIT ? wrow - 4 : wr;
+            constexpr int GROUPS = S::SPLIT ? 4 : S::WR;
+            if (key_part > 0 && key_part < PARTS) {
+                float *to = join + ((key_part - 1) * GROUPS + group) * (16 * DT + 2) * 64 + lane;
                 to[0] = m; to[64] = l;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
@@ -618,10 +641,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                     for (int i = 0; i < 16; ++i) to[(2 + 16 * d + i) * 64] = o[d][i];
             }
             __syncthreads();
-            if (wk == 0) {
+            if (key_part == 0 && (!S::SPLIT || halved)) {
                 float next = m;
 #pragma unroll
-                for (int k = 0; k < S::WK - 1; ++k) next = fmaxf(next, join[(k * S::WR + wr) * (16 * DT + 2) * 64 + lane]);
+                for (int k = 0; k < PARTS - 1; ++k) next = fmaxf(next, join[(k * GROUPS + group) * (16 * DT + 2) * 64 + lane]);
                 const float f = __builtin_amdgcn_exp2f(m - next);
                 l *= f;
 #pragma unroll
@@ -629,8 +652,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[d][i] *= f;
 #pragma unroll
-                for (int k = 0; k < S::WK - 1; ++k) {
-                    const float *from = join + (k * S::WR + wr) * (16 * DT + 2) * 64 + lane;
+                for (int k = 0; k < PARTS - 1; ++k) {
+                    const float *from = join + (k * GROUPS + group) * (16 * DT + 2) * 64 + lane;
                     const float g = __builtin_amdgcn_exp2f(from[0] - next);
                     l = fmaf(g, from[64], l);
 #pragma unroll
@@ -641,9 +664,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 m = next;
             }
         }
-        if (wk == 0 && row < rows) {
+        if (key_part == 0 && row < rows) {
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
-            if (u0 == 0 && u1 == per_item) {
+            if (u0 == 0 && u1 == units) {
                 const float r = 1.0f / l;
                 uint16_t *op = a.out + b * a.os[0] + node * a.os[1] + head * a.os[2] + 4 * half;
 #pragma unroll
@@ -654,9 +677,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             } else {
                 // (as the registers stand, so that every store is one run of 1 KiB)
                 float *to = a.part + (2 * w + (u0 == 0)) * (long long)(TM * (D + 2));
-                const int at = wr * 32 + col;
+                const int at = wrow * 32 + col;
                 if (half == 0) { to[at] = m; to[TM + at] = l; }
-                float4v *to4 = (float4v *)(to + 2 * TM) + wr * (4 * DT * 64) + lane;
+                float4v *to4 = (float4v *)(to + 2 * TM) + wrow * (4 * DT * 64) + lane;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -664,7 +687,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 if (leads && half == 0) a.place[w * TM + at] = b * a.os[0] + node * a.os[1] + head * a.os[2];
             }
         }
-        unit = item_start + u1;
+        unit = item_start + S::START + u1;
         if (unit == b_start + (long long)per_item * tiles * fresh_args<TreeAttnArgs>().kv_heads) { b_start = unit; ++b; }
     }
     zero_rows<S>(fresh_args<TreeAttnArgs>());          // (last: the first ones to be done have the time)
@@ -675,7 +698,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 // parts; where there are many parts, a workgroup takes one quarter and its waves share the parts.  Every workgroup sums up the
 // records for itself and takes every gridDim.x-th task.
 constexpr int kJoinShared = 8;        // more parts: the waves share them
-template <int D, int TM, bool F16>
+template <int D, int TM, bool F16, int START>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
 {
     constexpr int Q = D / 32;                          // groups of four elements in a quarter of a lane's
@@ -683,7 +706,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
     __shared__ int tasks[kAttnMaxGroups + 1], wave_sum[4];
     __shared__ float shared[4][4 * Q + 2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int W = (int)attn_groups(*a.total, a.groups), per = (W + 255) / 256;
+    const int W = (int)attn_groups(*a.total, a.groups, START), per = (W + 255) / 256;
     int sum = 0;
     for (int i = 0; i < per; ++i) {
         const int w = threadIdx.x * per + i;
