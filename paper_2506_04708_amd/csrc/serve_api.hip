@@ -62,6 +62,14 @@ bool cache_ok(const stand_cache *c)
            stride_ok(c->slot_stride) && stride_ok(c->head_stride);
 }
 
+// Whether places (x, y) up to these lie less than 2^32 chunks of eight elements from the first one (x, y < 2^31).
+bool spans_chunks(int64_t x, int64_t x_stride, int64_t y, int64_t y_stride)
+{
+    const int64_t most = (int64_t)1 << 32, xs = x_stride / 8, ys = y_stride / 8;
+    if ((x && xs >= most / x) || (y && ys >= most / y)) return false;
+    return x * xs + y * ys < most - 64;
+}
+
 bool strides_ok(const int64_t *s) { return stride_ok(s[0]) && stride_ok(s[1]) && stride_ok(s[2]); }
 
 }  // namespace
@@ -150,6 +158,8 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     const ServeView v = serve_view(h);
     if ((int64_t)table_width * cache->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
     if (v.B > kAttnMaxBatch || rows->q_heads > 65535) return STAND_ELIMIT;
+    // the kernel counts places of a layer in 16-byte chunks, in 32 bits
+    if (!spans_chunks(cache->pages - 1, cache->page_stride, cache->page_size - 1, cache->slot_stride)) return STAND_ELIMIT;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
     TreeAttnArgs a;

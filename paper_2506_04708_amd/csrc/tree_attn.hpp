@@ -107,7 +107,6 @@ struct AttnShape {
     static constexpr int TM = 32 * WR;                 // query rows of a tile
     static constexpr int KT = 32 * WK * SUB;           // keys of a stage
     static constexpr bool ALONE = WR == 1;             // every wave loads the keys that it alone uses
-    static constexpr bool SPLIT = WR == 8 && WK == 1 && SUB == 2;  // groups of rows may be shared by two waves, see the kernel
     static constexpr int NBUF = ALONE ? 2 : 4;         // stages in LDS: two on their way, one in work, one whose values are still read
     static constexpr int START = ALONE ? 2 : D == 64 ? 8 : 4;  // units that the beginning of an item costs, see attn_plan.hpp
     static constexpr int ROW = 2 * D;                  // bytes of a key
@@ -284,21 +283,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         }
         const int all_rows = nodes * a.per_kv, tile_rows = rows_of_tile(all_rows, tiles), row0 = tile * tile_rows;
         const int rows = min(all_rows, row0 + tile_rows);
-        // 32 rows for a wave and all keys of a stage; but of five or six such groups the last ones take two waves each, for half of
-        // the keys, so that no SIMD (waves w and w + 4) has four subtiles of a stage where another one has two
-        int wrow = wr, part = 0;
-        bool halved = false, halved_any = false;
-        if constexpr (S::SPLIT) {
-            const int have = (rows - row0 + 31) / 32;
-            halved_any = have == 5 || have == 6;
-            if (halved_any && wave >= 4) {
-                halved = true;
-                wrow = 4 + (wave - 4) % (have - 4);
-                part = (wave - 4) / (have - 4);
-            }
-        }
-        const int row = row0 + wrow * 32 + col;
-        const bool busy = row0 + wrow * 32 < rows && part < 2;  // this wave has rows
+        const int row = row0 + wr * 32 + col;
+        const bool busy = row0 + wr * 32 < rows;       // this wave has rows
         const int my_row = row < rows ? row : rows - 1;
         const int node = list[my_row / a.per_kv], head = hk * a.per_kv + my_row % a.per_kv;
 
@@ -317,8 +303,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         // ---- the units of this share: cached keys, then the tree's nodes; copies two stages ahead, page numbers two further ----
         const int n = u1 - u0, cached = cache_units - u0;       // units, those (if any) of the cache
         const int32_t *table = a.table + (long long)b * a.width;
+        // (places in the cache are counted in 16-byte chunks: 32 bits reach over 64 GiB of keys or values of a layer)
         const uint16_t *k_pool = a.k_pool + hk * a.pool_head, *v_pool = a.v_pool + hk * a.pool_head;
-        const long long pool_page = a.pool_page, pool_slot = a.pool_slot;
+        const uint32_t pool_page = (uint32_t)(a.pool_page / 8), pool_slot = (uint32_t)(a.pool_slot / 8);
         const int pages = a.pages, page_shift = a.page_shift;
         const int share = wave * S::KW;                         // this wave's keys of a stage (ALONE: those it uses)
         auto load_ids = [&](int i) {
@@ -327,28 +314,37 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             key = key > 0 ? key : 0;
             copy4_async(table + (key >> page_shift), __builtin_amdgcn_readfirstlane(lds0 + S::IDS + wave * 256 + (i & 3) * (S::LOADERS * 256)));
         };
-        auto load_stage = [&](int i) {
+        constexpr int LOADS = S::KW / S::KPI;
+        auto load_cached = [&](int i) {
             const uint32_t buf = lds0 + (i % S::NBUF) * S::STAGE + share * S::ROW;
             const int32_t *id = (const int32_t *)(attn_lds + S::IDS + (i & 3) * (S::LOADERS * 256) + wave * 256);
             const int ch = lane % S::CPR;
+            int page[LOADS];
 #pragma unroll
-            for (int r = 0; r < S::KW / S::KPI; ++r) {
-                const int at = r * S::KPI + lane / S::CPR, in_stage = share + at;
-                const uint16_t *kp, *vp;
-                if (i < cached) {
-                    int key = (u0 + i) * KT + in_stage;
-                    key = key < len ? key : len - 1;            // behind the end: the last key again, weighted with zero
-                    const long long page = clamp_page(id[at], pages);
-                    const long long from = page * pool_page + (key & ((1 << page_shift) - 1)) * pool_slot;
-                    kp = k_pool + from;
-                    vp = v_pool + from;
-                } else {
-                    const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
-                    int v = (i - cached) * KT + in_stage;
-                    v = v < a.N ? v : a.N - 1;
-                    kp = a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2];
-                    vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2];
-                }
+            for (int r = 0; r < LOADS; ++r) page[r] = id[r * S::KPI + lane / S::CPR];
+#pragma unroll
+            for (int r = 0; r < LOADS; ++r) {
+                const int in_stage = share + r * S::KPI + lane / S::CPR;
+                int key = (u0 + i) * KT + in_stage;
+                key = key < len ? key : len - 1;                // behind the end: the last key again, weighted with zero
+                const uint32_t from = (uint32_t)clamp_page(page[r], pages) * pool_page + (uint32_t)(key & ((1 << page_shift) - 1)) * pool_slot;
+                copy16_async(k_pool + 8ull * (from + (ch ^ S::swizzle_k(in_stage))), __builtin_amdgcn_readfirstlane(buf + r * S::KPI * S::ROW));
+                copy16_async(v_pool + 8ull * (from + (ch ^ S::swizzle_v(in_stage))), __builtin_amdgcn_readfirstlane(buf + KT * S::ROW + r * S::KPI * S::ROW));
+            }
+        };
+        auto load_stage = [&](int i) {
+            if (i < cached) {
+                load_cached(i);
+                return;
+            }
+            const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
+            const uint32_t buf = lds0 + (i % S::NBUF) * S::STAGE + share * S::ROW;
+            const int ch = lane % S::CPR;
+            for (int r = 0; r < LOADS; ++r) {
+                const int in_stage = share + r * S::KPI + lane / S::CPR;
+                int v = (i - cached) * KT + in_stage;
+                v = v < a.N ? v : a.N - 1;
+                const uint16_t *kp = a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2], *vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2];
                 copy16_async(kp + ((ch ^ S::swizzle_k(in_stage)) << 3), __builtin_amdgcn_readfirstlane(buf + r * S::KPI * S::ROW));
                 copy16_async(vp + ((ch ^ S::swizzle_v(in_stage)) << 3), __builtin_amdgcn_readfirstlane(buf + KT * S::ROW + r * S::KPI * S::ROW));
             }
@@ -581,23 +577,46 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             float16v even, odd_s;                               // scores of every other subtile: they change places, not registers
 #pragma unroll
             for (int x = 0; x < 16; ++x) even[x] = -__builtin_huge_valf();
+            // (before the first keys there is no weight at all, and values that are there: the first unit's own)
             uint32_t before = 0;
-            const int steps = halved ? n : n * SUB;             // subtiles of this wave
+            // Units whose keys all count and behind which two more cached ones come, without a question asked: branches cost as much
+            // here as arithmetic does.
+            constexpr int AT_ONCE = SUB == 1 ? 2 : 1;           // (an even number of subtiles)
+            const int whole = min(len / KT - u0, min(n, cached) - 2) / AT_ONCE * AT_ONCE;
+            int first = 0;
+            for (; first < whole; first += AT_ONCE) {
+#pragma unroll
+                for (int x = 0; x < AT_ONCE; ++x) {
+                    const int i = first + x;
+                    wait_loads<S::COPIES + 1>();
+                    group_barrier();
+                    if (loads) { load_ids(i + 4); load_cached(i + 2); }
+                    const uint32_t off = (i % S::NBUF) * S::STAGE;
+                    if (busy) {
+#pragma unroll
+                        for (int t = 0; t < SUB; ++t) {
+                            const uint32_t here = off + t * 32 * S::ROW;
+                            if ((x * SUB + t) % 2 == 0) step(even, odd_s, here, before, true, 0u, false);
+                            else step(odd_s, even, here, before, true, 0u, false);
+                            before = here;
+                        }
+                    }
+                }
+            }
+            const int steps = n * SUB;
             auto subtile = [&](int j, const float16v &old, float16v &now) {
                 const bool last = j == steps;                   // (no new keys)
-                const int i = halved ? j : j / SUB, t = halved ? part & 1 : j % SUB;
-                if (!last && (halved || t == 0)) arrive(i);
+                if (!last && j % SUB == 0) arrive(j / SUB);
                 bool all = true;
                 uint32_t word = 0, off = before;
                 if (!last) {
-                    word = counting(i, t, all);
-                    off = (i % S::NBUF) * S::STAGE + t * 32 * S::ROW;
+                    word = counting(j / SUB, j % SUB, all);
+                    off = (j / SUB % S::NBUF) * S::STAGE + j % SUB * 32 * S::ROW;
                 }
-                // (before the first keys: no weight at all, and values that are there)
-                if (busy) step(old, now, off, j == 0 ? off : before, all, word, last);
+                if (busy) step(old, now, off, before, all, word, last);
                 before = off;
             };
-            for (int j = 0; j <= steps; j += 2) {
+            for (int j = first > 0 ? first * SUB : 0; j <= steps; j += 2) {
                 subtile(j, even, odd_s);
                 if (j < steps) subtile(j + 1, odd_s, even);
             }
@@ -605,7 +624,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         if (busy && u1 > cache_units) {
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
             for (int x = 0; x < (a.N + 31) / 32; ++x) {
-                if (x % (KT / 32) / SUB != wk || (halved && x % SUB != part)) continue;
+                if (x % (KT / 32) / SUB != wk) continue;
                 for (uint32_t bits = odd[x]; bits; bits &= bits - 1) {
                     // an infinity or NaN reaches the rows that see its node, whatever its weight
                     const int v = 32 * x + __builtin_ctz(bits);
@@ -625,15 +644,11 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 
         // ---- the key waves' parts joined, then the rows' outputs or this workgroup's part of them ----
         l = other_half_sum(l);
-        constexpr int PARTS = S::SPLIT ? 2 : S::WK;
-        const int key_part = S::SPLIT ? part : wk;
-        if (S::WK > 1 || (S::SPLIT && halved_any)) {
+        if constexpr (S::WK > 1) {
             __syncthreads();
-            float *join = (float *)attn_lds;           // [PARTS - 1][groups of rows][16 DT + 2][64]
-            const int group = S::SPLIT ? wrow - 4 : wr;
-            constexpr int GROUPS = S::SPLIT ? 4 : S::WR;
-            if (key_part > 0 && key_part < PARTS) {
-                float *to = join + ((key_part - 1) * GROUPS + group) * (16 * DT + 2) * 64 + lane;
+            float *join = (float *)attn_lds;           // [WK - 1][WR][16 DT + 2][64]
+            if (wk > 0) {
+                float *to = join + ((wk - 1) * S::WR + wr) * (16 * DT + 2) * 64 + lane;
                 to[0] = m; to[64] = l;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
@@ -641,10 +656,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                     for (int i = 0; i < 16; ++i) to[(2 + 16 * d + i) * 64] = o[d][i];
             }
             __syncthreads();
-            if (key_part == 0 && (!S::SPLIT || halved)) {
+            if (wk == 0) {
                 float next = m;
 #pragma unroll
-                for (int k = 0; k < PARTS - 1; ++k) next = fmaxf(next, join[(k * GROUPS + group) * (16 * DT + 2) * 64 + lane]);
+                for (int k = 0; k < S::WK - 1; ++k) next = fmaxf(next, join[(k * S::WR + wr) * (16 * DT + 2) * 64 + lane]);
                 const float f = __builtin_amdgcn_exp2f(m - next);
                 l *= f;
 #pragma unroll
@@ -652,8 +667,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                     for (int i = 0; i < 16; ++i) o[d][i] *= f;
 #pragma unroll
-                for (int k = 0; k < PARTS - 1; ++k) {
-                    const float *from = join + (k * GROUPS + group) * (16 * DT + 2) * 64 + lane;
+                for (int k = 0; k < S::WK - 1; ++k) {
+                    const float *from = join + (k * S::WR + wr) * (16 * DT + 2) * 64 + lane;
                     const float g = __builtin_amdgcn_exp2f(from[0] - next);
                     l = fmaf(g, from[64], l);
 #pragma unroll
@@ -664,7 +679,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 m = next;
             }
         }
-        if (key_part == 0 && row < rows) {
+        if (wk == 0 && row < rows) {
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
             if (u0 == 0 && u1 == units) {
                 const float r = 1.0f / l;
@@ -677,9 +692,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             } else {
                 // (as the registers stand, so that every store is one run of 1 KiB)
                 float *to = a.part + (2 * w + (u0 == 0)) * (long long)(TM * (D + 2));
-                const int at = wrow * 32 + col;
+                const int at = wr * 32 + col;
                 if (half == 0) { to[at] = m; to[TM + at] = l; }
-                float4v *to4 = (float4v *)(to + 2 * TM) + wrow * (4 * DT * 64) + lane;
+                float4v *to4 = (float4v *)(to + 2 * TM) + wr * (4 * DT * 64) + lane;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
