@@ -86,8 +86,8 @@ auto with_attn_shape(AttnForm f, Call call)
     switch (f) {
     case kAttn32: return call(AttnShape<D, F16, 1, 4, 1>{});
     case kAttn64: return call(AttnShape<D, F16, 2, 2, 1>{});
-    case kAttn128: return call(AttnShape<D, F16, 4, 2, 1>{});
-    default: return call(AttnShape<D, F16, 8, 1, 2>{});
+    case kAttn128: return call(AttnShape<D, F16, 4, D == 64 ? 1 : 2, D == 64 ? 2 : 1>{});
+    default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2>{});
     }
 }
 template <typename Call>

@@ -122,6 +122,7 @@ struct AttnShape {
     static constexpr int MISC = LIST + 2048;
     static constexpr int BYTES = MISC + 256;
     static_assert(KW % KPI == 0 && KW >= KPI && KW <= 64, "a copy instruction brings whole keys of one wave");
+    static_assert(SUB == 1 || SUB == 2, "a step reads the keys of the other one of two subtiles ahead");
     static_assert(!ALONE || LOADERS == WAVES, "every wave loads for itself");
     static_assert((WK - 1) * TM * (D + 2) * 4 <= NBUF * STAGE, "parts of the key waves are joined in the stages' memory");
     // 16-byte chunk c of key k stands at chunk c ^ swizzle(k): reads of one chunk of 16 keys (K) and of four chunks of four
@@ -425,26 +426,32 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             }
         };
         // The same, 32 keys at a time and one step apart: scores of these keys, in whose products' shadow the weights of the keys
-        // before are made; then the products of those with their values, beside the search for these keys' maximum.  A wave issues
-        // in order, so vector instructions between the matrix instructions are what keeps both units busy.
-        auto step = [&](const float16v &old, float16v &t, uint32_t k_off, uint32_t v_off, bool all, uint32_t word, bool last) {
+        // before are made; then the products of those with their values, beside the search for these keys' maximum, which the next
+        // step begins with while its keys are read.  A wave issues in order, so vector instructions between the matrix instructions
+        // are what keeps both units busy.  HAVE: the keys have been read by the step before; NEXT: read those 32 keys further on.
+        uint4v kf[DC];
+        float top = -__builtin_huge_valf();
+        auto step = [&](auto have, auto next, const float16v &old, float16v &t, uint32_t k_off, uint32_t v_off, bool all, uint32_t word) {
             uint32_t ka = k_at + k_off, va = v_at + v_off;
             asm volatile("" : "+v"(ka), "+v"(va));
-            uint4v kf[DC], vf[2][DT];
+            if constexpr (!decltype(have)::value) {
 #pragma unroll
-            for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)(ka ^ (x << 5));
+                for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)(ka ^ (x << 5));
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            top = other_half_max(top) * c;
+            if (__ballot(top > m + 8.0f)) {            // seldom after the first stages: the old maximum will do
+                const float more = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - more);
+                m = more;
+                l *= f;
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+                for (int d = 0; d < DT; ++d)
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    const uint32_t at = (va ^ (d << 6)) + 16 * k * S::ROW;
-                    const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
-                    const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
-                    vf[k][d] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
-                }
-            __builtin_amdgcn_sched_barrier(0);
+                    for (int x = 0; x < 16; ++x) o[d][x] *= f;
+            }
             const float shift = kUp - m;
             constexpr int PER = 16 / DC;               // weights beside a matrix instruction
+            uint4v vf[2 * DT];
             t = float16v{0};
             uint32_t p[8];
             float e[2][PER];
@@ -452,6 +459,14 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             for (int x = 0; x <= DC; ++x) {
                 if (x < DC) {
                     t = mfma32<S::F16>(kf[x], q[x], t);
+                    constexpr int READS = 2 * DT / DC;
+#pragma unroll
+                    for (int y = x * READS; y < (x + 1) * READS; ++y) {
+                        const uint32_t at = (va ^ (y % DT << 6)) + 16 * (y / DT) * S::ROW;
+                        const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
+                        const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
+                        vf[y] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                    }
 #pragma unroll
                     for (int y = 0; y < PER; ++y) e[x & 1][y] = __builtin_amdgcn_exp2f(fmaf(old[x * PER + y], c, shift));
                 }
@@ -471,30 +486,24 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                 for (int x = 0; x < 16; ++x) t[x] = w4 & (1u << (8 * (x / 4) + x % 4)) ? t[x] : -__builtin_huge_valf();
             }
-            float top = t[0];
+            top = t[0];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const uint4v pf = {p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]};
+            for (int y = 0; y < 2 * DT; ++y) {
+                const int k = y / DT;
+                o[y % DT] = mfma32<S::F16>(vf[y], uint4v{p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]}, o[y % DT]);
+                constexpr int EACH = 8 / DT;
 #pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    o[d] = mfma32<S::F16>(vf[k][d], pf, o[d]);
-                    constexpr int EACH = 8 / DT;
+                for (int x = 0; x < EACH; ++x) top = fmaxf(top, t[y * EACH + x]);
+                if constexpr (decltype(next)::value) {
+                    constexpr int READS = DC / (2 * DT);
 #pragma unroll
-                    for (int y = 0; y < EACH; ++y) top = fmaxf(top, t[(k * DT + d) * EACH + y]);
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int x = y * READS; x < (y + 1) * READS; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)((ka ^ (x << 5)) + 32 * S::ROW);
                 }
-            }
-            top = other_half_max(top) * c;
-            if (__ballot(!last && top > m + 8.0f)) {   // seldom after the first stages: the old maximum will do
-                const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - next);
-                m = next;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) o[d][x] *= f;
+                __builtin_amdgcn_sched_barrier(0);
             }
         };
+        using Yes = std::true_type;
+        using No = std::false_type;
         const bool loads = wave < S::LOADERS;
         if (loads) { load_ids(0); load_ids(1); load_ids(2); }
         {
@@ -596,29 +605,29 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                         for (int t = 0; t < SUB; ++t) {
                             const uint32_t here = off + t * 32 * S::ROW;
-                            if ((x * SUB + t) % 2 == 0) step(even, odd_s, here, before, true, 0u, false);
-                            else step(odd_s, even, here, before, true, 0u, false);
+                            if (SUB > 1 && t == 0) step(No{}, Yes{}, even, odd_s, here, before, true, 0u);
+                            else if (SUB > 1) step(Yes{}, No{}, odd_s, even, here, before, true, 0u);
+                            else if (x % 2 == 0) step(No{}, No{}, even, odd_s, here, before, true, 0u);
+                            else step(No{}, No{}, odd_s, even, here, before, true, 0u);
                             before = here;
                         }
                     }
                 }
             }
             const int steps = n * SUB;
-            auto subtile = [&](int j, const float16v &old, float16v &now) {
-                const bool last = j == steps;                   // (no new keys)
+            for (int j = first > 0 ? first * SUB : 0; j <= steps; ++j) {   // (the last one: no new keys)
+                const bool last = j == steps;
                 if (!last && j % SUB == 0) arrive(j / SUB);
+                if (!busy) continue;
                 bool all = true;
                 uint32_t word = 0, off = before;
                 if (!last) {
                     word = counting(j / SUB, j % SUB, all);
                     off = (j / SUB % S::NBUF) * S::STAGE + j % SUB * 32 * S::ROW;
                 }
-                if (busy) step(old, now, off, before, all, word, last);
+                step(No{}, No{}, even, odd_s, off, before, all, word);
+                even = odd_s;
                 before = off;
-            };
-            for (int j = first > 0 ? first * SUB : 0; j <= steps; j += 2) {
-                subtile(j, even, odd_s);
-                if (j < steps) subtile(j + 1, odd_s, even);
             }
         }
         if (busy && u1 > cache_units) {
