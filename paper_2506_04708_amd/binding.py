@@ -6,6 +6,7 @@ the library has not been built, importing this module raises.
 """
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 import torch
@@ -60,19 +61,9 @@ class CacheDesc(C.Structure):
     ]
 
 
-class TreeRows(C.Structure):
-    _fields_ = [
-        ("d_q", C.c_void_p), ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_out", C.c_void_p), ("q_heads", C.c_int32),
-        ("scale", C.c_float), ("q_stride", C.c_int64 * 3), ("k_stride", C.c_int64 * 3), ("v_stride", C.c_int64 * 3),
-        ("out_stride", C.c_int64 * 3),
-    ]
-
-
-class CacheRows(C.Structure):
-    _fields_ = [
-        ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("rows", C.c_int32), ("layer_stride", C.c_int64),
-        ("batch_stride", C.c_int64), ("row_stride", C.c_int64), ("head_stride", C.c_int64),
-    ]
+# stand_tree_rows and stand_cache_rows, filled in anew by every call (a ctypes structure takes three times as long)
+_TREE_ROWS = struct.Struct("@4Pif12q")
+_CACHE_ROWS = struct.Struct("@2Pi4x4q")
 
 
 class PagesDesc(C.Structure):
@@ -242,6 +233,7 @@ class PagedCache:
         assert k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device
         assert k.is_cuda and k.dtype in _HALF and k.stride(4) == 1
         self.k, self.v = k, v
+        self.dtype, self.index, (self.layers, self.pages, self.page_size, self.heads, self.dim) = k.dtype, k.get_device(), k.shape
         self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), _HALF[k.dtype], *k.shape, *k.stride()[:4])
         self.ref = C.addressof(self.desc)
 
@@ -286,6 +278,9 @@ class Stand:
         self.W = self.D + 1
         self.logits_dtype = logits_dtype
         self.device = torch.device("cuda", device)
+        self._tree_rows = C.create_string_buffer(_TREE_ROWS.size)
+        self._cache_rows = C.create_string_buffer(_CACHE_ROWS.size)
+        self._work_bytes = {}   # of an attention, by its heads and type
 
     def close(self):
         if getattr(self, "h", None):
@@ -417,8 +412,9 @@ class Stand:
         return mask, pos
 
     def _here(self, *tensors):
+        index = self.device.index
         for t in tensors:
-            assert t is None or t.device == self.device, "tensor on %s, handle on %s" % (t.device, self.device)
+            assert t is None or t.get_device() == index, "tensor on %s, handle on %s" % (t.device, self.device)
 
     def _stream(self):
         # the caller's stream on the handle's device, whichever device is the current one
@@ -427,34 +423,40 @@ class Stand:
     def tree_attention(self, cache, layer, length, table, draft_tok, q, k, v, scale=None, out=None):
         """Attention of the drafted nodes over the cache's first length[b] tokens and their own ancestors: q [B, N, heads, d],
         k, v [B, N, kv heads, d] (slices of a fused projection are fine) -> out, like q."""
-        B, N, H, d = q.shape
-        G = cache.k.shape[3]
+        B, N, H, d = shape = q.shape
         if out is None:
-            out = torch.empty((B, N, H, d), dtype=q.dtype, device=q.device)
-        assert (B, N) == (self.B, self.N) and k.shape == v.shape == (B, N, G, d) and out.shape == q.shape and d == cache.k.shape[4]
-        assert q.dtype == k.dtype == v.dtype == out.dtype == cache.k.dtype
-        assert q.stride(3) == k.stride(3) == v.stride(3) == out.stride(3) == 1
-        assert length.shape == (B,) and table.dim() == 2 and table.shape[0] == B and draft_tok.shape == (B, N)
-        self._here(cache.k, length, table, draft_tok, q, k, v, out)
-        s3 = C.c_int64 * 3
-        rows = TreeRows(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), H, d ** -0.5 if scale is None else scale,
-                        s3(*q.stride()[:3]), s3(*k.stride()[:3]), s3(*v.stride()[:3]), s3(*out.stride()[:3]))
-        need = self._lib.stand_tree_attention_work(self.h, cache.ref, H)
+            out = torch.empty(shape, dtype=q.dtype, device=q.device)
+        assert B == self.B and N == self.N and d == cache.dim and k.shape == v.shape == (B, N, cache.heads, d) and out.shape == shape
+        assert cache.dtype is q.dtype and cache.dtype is k.dtype and cache.dtype is v.dtype and cache.dtype is out.dtype
+        (q0, q1, q2, q3), (k0, k1, k2, k3), (v0, v1, v2, v3), (o0, o1, o2, o3) = q.stride(), k.stride(), v.stride(), out.stride()
+        assert q3 == k3 == v3 == o3 == 1
+        rows, width = table.shape
+        assert rows == B and length.shape == (B,) and draft_tok.shape == (B, N) and cache.index == self.device.index
+        self._here(length, table, draft_tok, q, k, v, out)
+        buf = self._tree_rows
+        _TREE_ROWS.pack_into(buf, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), H, d ** -0.5 if scale is None else scale,
+                             q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2)
+        key = (H, cache.heads, d, cache.desc.dtype)
+        need = self._work_bytes.get(key)
+        if need is None:
+            need = self._work_bytes[key] = self._lib.stand_tree_attention_work(self.h, cache.ref, H)
         # (torch's allocator hands this memory on in the order of the stream, and keeps a captured graph's apart)
         work = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
-        _check(self._lib.stand_tree_attention(self.h, cache.ref, layer, _dptr(length, torch.int32), _dptr(table, torch.int32), table.shape[1],
-                                              _dptr(draft_tok, torch.int32), C.addressof(rows), work.data_ptr(), need, self._stream()), self.h)
+        _check(self._lib.stand_tree_attention(self.h, cache.ref, layer, _dptr(length, torch.int32), _dptr(table, torch.int32), width,
+                                              _dptr(draft_tok, torch.int32), C.addressof(buf), work.data_ptr(), need, self._stream()), self.h)
         return out
 
     def cache_commit(self, cache, k, v, slots, row=None, count=None):
         """Rows k, v [layers, B, rows, kv heads, d] into the cache: row[b][j] (None: j) to slots[b][j], j < count[b] (None: all)."""
-        L, _, _, G, d = cache.k.shape
-        assert k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype == cache.k.dtype and k.stride(4) == 1
-        assert k.dim() == 5 and (k.shape[0], k.shape[1], k.shape[3], k.shape[4]) == (L, self.B, G, d)
-        assert slots.dim() == 2 and slots.shape[0] == self.B and (row is None or row.shape == slots.shape) and (count is None or count.shape == (self.B,))
-        self._here(cache.k, k, v, slots, row, count)
-        rows = CacheRows(k.data_ptr(), v.data_ptr(), k.shape[2], *k.stride()[:4])
-        _check(self._lib.stand_cache_commit(self.h, cache.ref, C.addressof(rows), _dptr(slots, torch.int64), slots.shape[1],
+        layers, B, rows, heads, d = k.shape
+        stride = k.stride()
+        assert k.shape == v.shape and stride == v.stride() and stride[4] == 1 and cache.dtype is k.dtype and cache.dtype is v.dtype
+        assert layers == cache.layers and B == self.B and heads == cache.heads and d == cache.dim and cache.index == self.device.index
+        assert slots.dim() == 2 and slots.shape[0] == B and (row is None or row.shape == slots.shape) and (count is None or count.shape == (B,))
+        self._here(k, v, slots, row, count)
+        buf = self._cache_rows
+        _CACHE_ROWS.pack_into(buf, 0, k.data_ptr(), v.data_ptr(), rows, *stride[:4])
+        _check(self._lib.stand_cache_commit(self.h, cache.ref, C.addressof(buf), _dptr(slots, torch.int64), slots.shape[1],
                                             _dptr(row, torch.int32), _dptr(count, torch.int32), self._stream()), self.h)
 
     def cache_pages(self, pages, add=None, room=None, slots=None, missing=None, out=None):

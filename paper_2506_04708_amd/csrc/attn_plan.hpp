@@ -15,7 +15,6 @@
 namespace stand {
 
 constexpr int kAttnMaxBatch = 4096;   // trajectories of a call: their unit sums are made in LDS
-constexpr int kAttnMaxGroups = 2048;  // workgroups of a launch: their records are summed up in LDS
 STAND_BOTH long long clamp_length(long long len, long long most) { return len < 0 ? 0 : (len > most ? most : len); }
 STAND_BOTH int clamp_page(int page, int pages) { return page < 0 ? 0 : (page >= pages ? pages - 1 : page); }
 

@@ -108,10 +108,9 @@ int attn_launch_groups(int cus)
         if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)tree_attn_kernel<S>, S::THREADS, S::BYTES) != hipSuccess) return 1;
         return std::max(n, 1);
     }();
-    return std::max(8, std::min(cus * per_cu, kAttnMaxGroups) / 8 * 8);
+    return std::max(8, cus * per_cu / 8 * 8);
 }
-// Workspace: units, records, places, parts.
-constexpr uint64_t kAttnHead = 256;
+// Workspace: records, places, parts.
 template <typename S>
 uint64_t attn_part_bytes(int cus)
 {
@@ -123,11 +122,10 @@ hipError_t attn_launch(TreeAttnArgs &a, int cus, hipStream_t s)
 {
     static_assert(S::BYTES <= 160 * 1024, "LDS of a compute unit");
     a.groups = attn_launch_groups<S>(cus);
-    a.join = (JoinRecord *)((char *)a.total + kAttnHead);
     a.place = (long long *)(a.join + a.groups);
     a.part = (float *)(a.place + (size_t)a.groups * S::TM);
     tree_attn_kernel<S><<<dim3((unsigned)a.groups), dim3(S::THREADS), S::BYTES, s>>>(a);
-    tree_attn_join_kernel<S::D, S::TM, S::F16, S::START><<<dim3(4u * (unsigned)cus), dim3(256), 0, s>>>(a);
+    tree_attn_join_kernel<S::D, S::TM, S::F16><<<dim3((unsigned)a.groups, S::WR), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -138,7 +136,7 @@ extern "C" uint64_t stand_tree_attention_work(const stand_handle *h, const stand
     if (!h || !cache_ok(cache) || q_heads < 1 || q_heads % cache->kv_heads) return 0;
     const ServeView v = serve_view(const_cast<stand_handle *>(h));
     const AttnForm f = attn_form((int64_t)v.N * (q_heads / cache->kv_heads));
-    return kAttnHead + with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, f, [&](auto s) { return attn_part_bytes<decltype(s)>(v.cus); });
+    return with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, f, [&](auto s) { return attn_part_bytes<decltype(s)>(v.cus); });
 }
 
 extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, int32_t layer, const int32_t *d_len,
@@ -169,7 +167,7 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     a.v_pool = (const uint16_t *)cache->d_v + layer * cache->layer_stride;
     a.len = d_len; a.table = d_table; a.draft_tok = d_draft_tok;
     a.anc = (const uint32_t *)v.anc; a.anc_words = 2 * v.anc_words;      // (little endian: words of 32 nodes)
-    a.total = (long long *)d_work;
+    a.join = (JoinRecord *)d_work;
     for (int i = 0; i < 3; ++i) {
         a.qs[i] = rows->q_stride[i]; a.ks[i] = rows->k_stride[i]; a.vs[i] = rows->v_stride[i]; a.os[i] = rows->out_stride[i];
     }

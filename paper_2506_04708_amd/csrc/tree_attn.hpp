@@ -7,7 +7,7 @@
 
 namespace stand {
 
-// What the workgroup leaves whose share begins inside an item that the one before it began: who has the parts.
+// What a workgroup leaves whose share begins inside an item: who has the item's parts.  rows 0: nothing to join.
 struct JoinRecord { int first, last, rows, unused; };
 
 struct TreeAttnArgs {
@@ -15,7 +15,6 @@ struct TreeAttnArgs {
     uint16_t *out;
     const int32_t *len, *table, *draft_tok;
     const uint32_t *anc;                             // [N][anc_words] bit sets in 32-bit words
-    long long *total;                                // workspace: units of the call
     JoinRecord *join;                                // workspace: [groups], then the rows' places in out, [groups][rows of a tile]
     long long *place;
     float *part;                                     // workspace: [2 * groups][rows of a tile][D + 2]
@@ -140,6 +139,7 @@ template <int TM, int KT, int THREADS, int START>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int first_len = a.len[lane < a.B ? lane : 0];    // (asked for before it is needed)
     for (int b = threadIdx.x; b <= a.B; b += THREADS) prefix[b] = 0;
     __syncthreads();
     int p2 = 1;
@@ -172,7 +172,7 @@ __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *pref
         for (int b0 = 0; b0 < a.B; b0 += 64) {
             const int b = b0 + lane;
             long long x = 0;
-            if (b < a.B) x = (START + item_units(a.len[b], (long long)a.width << a.page_shift, a.N, KT)) * tree_items((int)prefix[b + 1], a.per_kv, a.kv_heads, TM);
+            if (b < a.B) x = (START + item_units(b0 ? a.len[b] : first_len, (long long)a.width << a.page_shift, a.N, KT)) * tree_items((int)prefix[b + 1], a.per_kv, a.kv_heads, TM);
             for (int off = 1; off < 64; off <<= 1) {
                 const long long y = __shfl_up(x, off);
                 if (lane >= off) x += y;
@@ -214,8 +214,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
     long long *sums = (long long *)attn_lds;
     unit_sums<TM, KT, S::THREADS, S::START>(a, sums);
     const long long total = sums[a.B];
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.total = total;
     const long long W = attn_groups(total, a.groups, S::START);
+    if (threadIdx.x == 0 && (long long)blockIdx.x >= W) a.join[blockIdx.x] = JoinRecord{0, 0, 0, 0};   // (no share has this number)
     // neighbours in the order of the work share an XCD (workgroups go round the eight of them in turn) and so its L2
     const int per_xcd = (int)((W + 7) / 8);
     const long long w = (long long)(blockIdx.x % 8) * per_xcd + blockIdx.x / 8;
@@ -279,8 +279,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             first_item = false;
             const long long from = first_group(item_start, total, W, S::START);
             leads = u0 > 0 && from == w - 1;
-            if (threadIdx.x == 0)                      // (every share writes its record: no share ends before its first item begins)
-                a.join[w] = JoinRecord{(int)from, (int)group_of(item_start + per_item - 1, total, W), leads ? min(rows_of_tile(nodes * a.per_kv, tiles), nodes * a.per_kv - tile * rows_of_tile(nodes * a.per_kv, tiles)) : 0, 0};
+            if (threadIdx.x == 0) {                    // (every share comes here: none ends before its first item begins)
+                const int each = rows_of_tile(nodes * a.per_kv, tiles);
+                a.join[w] = JoinRecord{(int)from, (int)group_of(item_start + per_item - 1, total, W), u0 > 0 ? min(each, nodes * a.per_kv - tile * each) : 0, 0};
+            }
         }
         const int all_rows = nodes * a.per_kv, tile_rows = rows_of_tile(all_rows, tiles), row0 = tile * tile_rows;
         const int rows = min(all_rows, row0 + tile_rows);
@@ -717,119 +719,94 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
     zero_rows<S>(fresh_args<TreeAttnArgs>());          // (last: the first ones to be done have the time)
 }
 
-// Rows of items that several workgroups took: their parts joined, 32 rows (those of one wave) at a time and in the layout of its
-// registers: lane l has the row l % 32 and every second group of four elements.  Each wave takes a quarter of the elements of all
-// parts; where there are many parts, a workgroup takes one quarter and its waves share the parts.  Every workgroup sums up the
-// records for itself and takes every gridDim.x-th task.
-constexpr int kJoinShared = 8;        // more parts: the waves share them
-template <int D, int TM, bool F16, int START>
+// Rows of items that several workgroups took: their parts joined, 32 rows (those of one wave) by a workgroup and in the layout of
+// a wave's registers: lane l has the row l % 32 and every second group of four elements.  The workgroups of the item's second
+// share take a quarter of the elements with each wave; where there are many parts, those of eight shares take an eighth each and
+// their waves the parts in turn.
+constexpr int kJoinShared = 8;        // more parts: shared
+template <int D, int TM, bool F16>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
 {
-    constexpr int Q = D / 32;                          // groups of four elements in a quarter of a lane's
+    constexpr int GROUPS = D / 8;                      // groups of four elements of a lane
+    constexpr int Q = GROUPS / 4, E = GROUPS / 8;      // a quarter of them, an eighth
     constexpr long long kSlot = TM * (D + 2);
-    __shared__ int tasks[kAttnMaxGroups + 1], wave_sum[4];
-    __shared__ float shared[4][4 * Q + 2][64];
+    __shared__ float shared[4][4 * E + 2][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int W = (int)attn_groups(*a.total, a.groups, START), per = (W + 255) / 256;
-    int sum = 0;
-    for (int i = 0; i < per; ++i) {
-        const int w = threadIdx.x * per + i;
-        if (w < W) {
-            const JoinRecord r = a.join[w];
-            sum += (r.rows + 31) / 32 * (r.last - r.first + 1 > kJoinShared ? 4 : 1);
-            tasks[w + 1] = sum;
-        }
-    }
-    int before = sum;
-    for (int off = 1; off < 64; off <<= 1) {
-        const int y = __shfl_up(before, off);
-        if (lane >= off) before += y;
-    }
-    if (lane == 63) wave_sum[wave] = before;
-    __syncthreads();
-    before -= sum;
-    for (int k = 0; k < wave; ++k) before += wave_sum[k];
-    for (int i = 0; i < per; ++i)
-        if (threadIdx.x * per + i < W) tasks[threadIdx.x * per + i + 1] += before;
-    if (threadIdx.x == 0) tasks[0] = 0;
-    __syncthreads();
-    const int total = W > 0 ? tasks[W] : 0;
-    for (int task = blockIdx.x; task < total; task += gridDim.x) {
-        int lo = 0, hi = W - 1;                        // the record: last one with tasks[] <= task
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) / 2;
-            if (tasks[mid] <= task) lo = mid; else hi = mid - 1;
-        }
-        const int w = __builtin_amdgcn_readfirstlane(lo), sub = task - tasks[w];
-        const JoinRecord r = a.join[w];
-        const bool share = r.last - r.first + 1 > kJoinShared;
-        const int wr = share ? sub / 4 : sub, quarter = share ? sub % 4 : wave;
-        const int step = share ? 4 : 1, from = share ? r.first + wave : r.first;
-        const int at = wr * 32 + (lane & 31);
-        const long long place = at < r.rows ? a.place[(long long)w * TM + at] : 0;
-        float4v acc[Q];
-        float top = -1e38f, l = 0.0f;
+    const int w = blockIdx.x, wr = blockIdx.y, at = wr * 32 + (lane & 31);
+    const JoinRecord r = a.join[w];
+    if (wr * 32 >= r.rows) return;
+    const int turn = w - r.first - 1;                  // 0: the item's second share
+    const bool share = r.last - r.first + 1 > kJoinShared;
+    if (turn >= (share ? 8 : 1)) return;
+    const int row = at < r.rows ? at : r.rows - 1;
+    const long long place = a.place[(r.first + 1ll) * TM + row];
+    uint16_t *o = a.out + place + 4 * (lane >> 5);
+    auto store = [&](int j, float4v x, float l) {      // group j: elements 32 (j / 4) + 8 (j % 4) + 4 (lane / 32) and the three behind
+        if (at < r.rows) *(uint2 *)(o + 32 * (j / 4) + 8 * (j % 4)) = uint2{pack2<F16>(x[0] / l, x[1] / l), pack2<F16>(x[2] / l, x[3] / l)};
+    };
+    auto gather = [&](auto n, int group, int from, int step, float4v *acc, float &top, float &l) {
+        constexpr int COUNT = decltype(n)::value, AT_ONCE = 16 / COUNT;
 #pragma unroll
-        for (int i = 0; i < Q; ++i) acc[i] = float4v{0, 0, 0, 0};
-        for (int g0 = from; g0 <= r.last; g0 += 4 * step) {
-            float m[4], x[4];
-            float4v p[4][Q];
+        for (int i = 0; i < COUNT; ++i) acc[i] = float4v{0, 0, 0, 0};
+        for (int g0 = from; g0 <= r.last; g0 += AT_ONCE * step) {
+            float m[AT_ONCE], x[AT_ONCE];
+            float4v p[AT_ONCE][COUNT];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {              // (past the last one: that one again, with no weight)
+            for (int k = 0; k < AT_ONCE; ++k) {        // (past the last one: that one again, with no weight)
                 const int g = min(g0 + k * step, r.last);
                 const float *slot = a.part + (2 * g + (g == r.first)) * kSlot;
                 m[k] = slot[at]; x[k] = slot[TM + at];
 #pragma unroll
-                for (int i = 0; i < Q; ++i) p[k][i] = ((const float4v *)(slot + 2 * TM))[(wr * (4 * Q) + quarter * Q + i) * 64 + lane];
+                for (int i = 0; i < COUNT; ++i) p[k][i] = ((const float4v *)(slot + 2 * TM))[(wr * GROUPS + group + i) * 64 + lane];
             }
             float best = top;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) best = fmaxf(best, m[k]);
+            for (int k = 0; k < AT_ONCE; ++k) best = fmaxf(best, m[k]);
             const float f = __builtin_amdgcn_exp2f(top - best);
             top = best;
             l *= f;
 #pragma unroll
-            for (int i = 0; i < Q; ++i) acc[i] = acc[i] * f;
+            for (int i = 0; i < COUNT; ++i) acc[i] = acc[i] * f;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
+            for (int k = 0; k < AT_ONCE; ++k) {
                 if (g0 + k * step > r.last) continue;
                 const float y = __builtin_amdgcn_exp2f(m[k] - best);
                 l = fmaf(y, x[k], l);
 #pragma unroll
-                for (int i = 0; i < Q; ++i)
+                for (int i = 0; i < COUNT; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e) acc[i][e] = fmaf(y, p[k][i][e], acc[i][e]);
             }
         }
-        if (share) {
-            __syncthreads();                           // (the task before is done with them)
-            shared[wave][4 * Q][lane] = top;
-            shared[wave][4 * Q + 1][lane] = l;
+    };
+    float top = -1e38f, l = 0.0f;
+    if (!share) {
+        float4v acc[Q];
+        gather(std::integral_constant<int, Q>{}, wave * Q, r.first, 1, acc, top, l);
 #pragma unroll
-            for (int i = 0; i < 4 * Q; ++i) shared[wave][i][lane] = acc[i / 4][i % 4];
-            __syncthreads();
-            if (wave > 0) continue;
-            const float best = fmaxf(fmaxf(shared[0][4 * Q][lane], shared[1][4 * Q][lane]), fmaxf(shared[2][4 * Q][lane], shared[3][4 * Q][lane]));
-            l = 0.0f;
-#pragma unroll
-            for (int i = 0; i < Q; ++i) acc[i] = float4v{0, 0, 0, 0};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float f = __builtin_amdgcn_exp2f(shared[k][4 * Q][lane] - best);
-                l = fmaf(f, shared[k][4 * Q + 1][lane], l);
-#pragma unroll
-                for (int i = 0; i < 4 * Q; ++i) acc[i / 4][i % 4] = fmaf(f, shared[k][i][lane], acc[i / 4][i % 4]);
-            }
-        }
-        if (at >= r.rows) continue;
-        // group j of a lane's: elements 32 (j / 4) + 8 (j % 4) + 4 (lane / 32) and the three behind
-        uint16_t *o = a.out + place + 4 * (lane >> 5);
-#pragma unroll
-        for (int i = 0; i < Q; ++i) {
-            const int j = quarter * Q + i;
-            *(uint2 *)(o + 32 * (j / 4) + 8 * (j % 4)) = uint2{pack2<F16>(acc[i][0] / l, acc[i][1] / l), pack2<F16>(acc[i][2] / l, acc[i][3] / l)};
-        }
+        for (int i = 0; i < Q; ++i) store(wave * Q + i, acc[i], l);
+        return;
     }
+    float4v acc[E];
+    gather(std::integral_constant<int, E>{}, turn * E, r.first + wave, 4, acc, top, l);
+    shared[wave][4 * E][lane] = top;
+    shared[wave][4 * E + 1][lane] = l;
+#pragma unroll
+    for (int i = 0; i < 4 * E; ++i) shared[wave][i][lane] = acc[i / 4][i % 4];
+    __syncthreads();
+    if (wave >= E) return;
+    // wave i: its group of the eighth, over the four waves' parts
+    const float best = fmaxf(fmaxf(shared[0][4 * E][lane], shared[1][4 * E][lane]), fmaxf(shared[2][4 * E][lane], shared[3][4 * E][lane]));
+    float4v x = {0, 0, 0, 0};
+    l = 0.0f;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const float f = __builtin_amdgcn_exp2f(shared[k][4 * E][lane] - best);
+        l = fmaf(f, shared[k][4 * E + 1][lane], l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = fmaf(f, shared[k][4 * wave + e][lane], x[e]);
+    }
+    store(turn * E + wave, x, l);
 }
 
 }  // namespace stand
