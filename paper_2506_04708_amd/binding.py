@@ -278,8 +278,6 @@ class Stand:
         self.W = self.D + 1
         self.logits_dtype = logits_dtype
         self.device = torch.device("cuda", device)
-        self._tree_rows = C.create_string_buffer(_TREE_ROWS.size)
-        self._cache_rows = C.create_string_buffer(_CACHE_ROWS.size)
         self._work_bytes = {}   # of an attention, by its heads and type
 
     def close(self):
@@ -433,9 +431,8 @@ class Stand:
         rows, width = table.shape
         assert rows == B and length.shape == (B,) and draft_tok.shape == (B, N) and cache.index == self.device.index
         self._here(length, table, draft_tok, q, k, v, out)
-        buf = self._tree_rows
-        _TREE_ROWS.pack_into(buf, 0, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), H, d ** -0.5 if scale is None else scale,
-                             q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2)
+        desc = _TREE_ROWS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), H, d ** -0.5 if scale is None else scale,
+                               q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2)
         key = (H, cache.heads, d, cache.desc.dtype)
         need = self._work_bytes.get(key)
         if need is None:
@@ -443,7 +440,7 @@ class Stand:
         # (torch's allocator hands this memory on in the order of the stream, and keeps a captured graph's apart)
         work = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
         _check(self._lib.stand_tree_attention(self.h, cache.ref, layer, _dptr(length, torch.int32), _dptr(table, torch.int32), width,
-                                              _dptr(draft_tok, torch.int32), C.addressof(buf), work.data_ptr(), need, self._stream()), self.h)
+                                              _dptr(draft_tok, torch.int32), desc, work.data_ptr(), need, self._stream()), self.h)
         return out
 
     def cache_commit(self, cache, k, v, slots, row=None, count=None):
@@ -454,9 +451,8 @@ class Stand:
         assert layers == cache.layers and B == self.B and heads == cache.heads and d == cache.dim and cache.index == self.device.index
         assert slots.dim() == 2 and slots.shape[0] == B and (row is None or row.shape == slots.shape) and (count is None or count.shape == (B,))
         self._here(k, v, slots, row, count)
-        buf = self._cache_rows
-        _CACHE_ROWS.pack_into(buf, 0, k.data_ptr(), v.data_ptr(), rows, *stride[:4])
-        _check(self._lib.stand_cache_commit(self.h, cache.ref, C.addressof(buf), _dptr(slots, torch.int64), slots.shape[1],
+        desc = _CACHE_ROWS.pack(k.data_ptr(), v.data_ptr(), rows, *stride[:4])
+        _check(self._lib.stand_cache_commit(self.h, cache.ref, desc, _dptr(slots, torch.int64), slots.shape[1],
                                             _dptr(row, torch.int32), _dptr(count, torch.int32), self._stream()), self.h)
 
     def cache_pages(self, pages, add=None, room=None, slots=None, missing=None, out=None):

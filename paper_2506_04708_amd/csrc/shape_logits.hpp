@@ -222,8 +222,8 @@ __global__ __launch_bounds__(kShapeThreads) void shape_logits_kernel(ShapeArgs a
 #pragma unroll
                     for (int e = 0; e < 8; ++e) {
                         const float times = (float)(c[e] & (kPromptFlag - 1)), z = x[k][e];
-                        // the quotient to half a step: one correction with the exact remainder
-                        const float q = z * inverse, p = fmaf(fmaf(-q, rho, z), inverse, q);
+                        // the quotient to half a step: one correction with the exact remainder (there is none of an infinity)
+                        const float q = z * inverse, p = q < __builtin_huge_valf() ? fmaf(fmaf(-q, rho, z), inverse, q) : q;
                         float y = z > 0.0f ? p : z * rho;
                         y = y - often * times;
                         y = times > 0.0f ? y - present : y;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(kShapeThreads) void shape_logits_kernel(ShapeArgs a
 // Tokens into the counts: the prompt's set a flag, generated ones are added.
 __global__ __launch_bounds__(256) void count_tokens_kernel(int32_t *count, const int32_t *tok, const int32_t *len, int V, int width, int prompt)
 {
-    const int b = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;
+    const int b = blockIdx.y, j = blockIdx.x * 256 + threadIdx.x;   // (width is at most 2^30)
     if (j >= width || (len && j >= len[b])) return;
     const int v = tok[(long long)b * width + j];
     if (v < 0 || v >= V) return;
