@@ -1,13 +1,13 @@
 // serve_api.hip -- host side of the operators around a verification (include/stand.h): argument checks and launches.
 // Nothing here allocates, waits or keeps state between calls; everything a call needs comes with it.
-#include "../../include/stand.h"
 #include "cache_ops.hpp"
+#include "serve_checks.hpp"
 #include "serve_view.hpp"
 #include "shape_logits.hpp"
 #include "tree_attn.hpp"
 
 #include <algorithm>
-#include <cmath>
+#include <atomic>
 
 using namespace stand;
 
@@ -43,39 +43,6 @@ int bad_device(const ServeView &v, hipError_t e)
     return STAND_EHIP;
 }
 
-bool aligned16(const void *p) { return ((uintptr_t)p & 15u) == 0; }
-bool stride_ok(int64_t s) { return s >= 0 && s % 8 == 0 && s < ((int64_t)1 << 48); }
-int log2_of(int64_t x)
-{
-    int s = 0;
-    while (((int64_t)1 << s) < x) ++s;
-    return s;
-}
-bool power_of_two(int64_t x) { return x > 0 && (x & (x - 1)) == 0; }
-bool page_size_ok(int32_t p) { return power_of_two(p) && p <= STAND_MAX_PAGE; }
-
-bool cache_ok(const stand_cache *c)
-{
-    return c && c->d_k && c->d_v && aligned16(c->d_k) && aligned16(c->d_v) && (c->dtype == STAND_BF16 || c->dtype == STAND_F16) &&
-           c->layers >= 1 && c->pages >= 1 && page_size_ok(c->page_size) && c->kv_heads >= 1 && c->kv_heads <= 4096 &&
-           (c->head_dim == 64 || c->head_dim == 128) && stride_ok(c->layer_stride) && stride_ok(c->page_stride) &&
-           stride_ok(c->slot_stride) && stride_ok(c->head_stride);
-}
-
-// Whether places (x, y) up to these lie less than 2^32 chunks of eight elements from the first one (x, y < 2^31).
-bool spans_chunks(int64_t x, int64_t x_stride, int64_t y, int64_t y_stride)
-{
-    const int64_t most = (int64_t)1 << 32, xs = x_stride / 8, ys = y_stride / 8;
-    if ((x && xs >= most / x) || (y && ys >= most / y)) return false;
-    return x * xs + y * ys < most - 64;
-}
-
-bool strides_ok(const int64_t *s) { return stride_ok(s[0]) && stride_ok(s[1]) && stride_ok(s[2]); }
-
-}  // namespace
-
-namespace {
-
 // The form of the attention kernel a call takes, by the rows that share a key/value head.
 enum AttnForm { kAttn32, kAttn64, kAttn128, kAttn256 };
 AttnForm attn_form(int64_t rows) { return rows <= 32 ? kAttn32 : rows <= 64 ? kAttn64 : rows <= 128 ? kAttn128 : kAttn256; }
@@ -97,31 +64,40 @@ auto with_attn_shape(int head_dim, bool f16, AttnForm f, Call call)
     return f16 ? with_attn_shape<128, true>(f, call) : with_attn_shape<128, false>(f, call);
 }
 
-// Workgroups launched: as many as the device holds at once, a multiple of its eight XCDs.
+// Workgroups of a launch: as many as the device holds at once, a multiple of its eight XCDs; 0: the device refused.  (Above
+// 64 KiB dynamic LDS has to be asked for, on every device.)
+constexpr int kMaxDevices = 64;
 template <typename S>
-int attn_launch_groups(int cus)
+int attn_groups_of(const ServeView &v)
 {
-    static const int per_cu = [] {
-        int n = 0;
-        // (above 64 KiB dynamic LDS has to be asked for)
-        if (hipFuncSetAttribute((const void *)tree_attn_kernel<S>, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES) != hipSuccess) return 1;
-        if (hipOccupancyMaxActiveBlocksPerMultiprocessor(&n, (const void *)tree_attn_kernel<S>, S::THREADS, S::BYTES) != hipSuccess) return 1;
-        return std::max(n, 1);
-    }();
-    return std::max(8, cus * per_cu / 8 * 8);
+    static_assert(S::BYTES <= 160 * 1024, "LDS of a compute unit");
+    static std::atomic<int> known[kMaxDevices];
+    const int at = v.device < kMaxDevices ? v.device : -1;
+    int per_cu = at < 0 ? 0 : known[at].load(std::memory_order_relaxed);
+    if (per_cu == 0) {
+        const DeviceScope scope(v.device);
+        const void *kernel = (const void *)tree_attn_kernel<S>;
+        hipError_t e = scope.e;
+        if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
+        if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kernel, S::THREADS, S::BYTES);
+        if (e != hipSuccess || per_cu < 1) {
+            *v.last_hip = (int)e;
+            return 0;
+        }
+        if (at >= 0) known[at].store(per_cu, std::memory_order_relaxed);
+    }
+    return std::max(8, v.cus * per_cu / 8 * 8);
 }
 // Workspace: records, places, parts.
 template <typename S>
-uint64_t attn_part_bytes(int cus)
+uint64_t attn_work_bytes(int groups)
 {
-    return (uint64_t)attn_launch_groups<S>(cus) * (sizeof(JoinRecord) + S::TM * 8 + 2 * S::TM * (S::D + 2) * 4);
+    return (uint64_t)groups * (sizeof(JoinRecord) + S::TM * 8 + 2 * S::TM * (S::D + 2) * 4);
 }
 
 template <typename S>
-hipError_t attn_launch(TreeAttnArgs &a, int cus, hipStream_t s)
+hipError_t attn_launch(TreeAttnArgs &a, hipStream_t s)
 {
-    static_assert(S::BYTES <= 160 * 1024, "LDS of a compute unit");
-    a.groups = attn_launch_groups<S>(cus);
     a.place = (long long *)(a.join + a.groups);
     a.part = (float *)(a.place + (size_t)a.groups * S::TM);
     tree_attn_kernel<S><<<dim3((unsigned)a.groups), dim3(S::THREADS), S::BYTES, s>>>(a);
@@ -133,33 +109,21 @@ hipError_t attn_launch(TreeAttnArgs &a, int cus, hipStream_t s)
 
 extern "C" uint64_t stand_tree_attention_work(const stand_handle *h, const stand_cache *cache, int32_t q_heads)
 {
-    if (!h || !cache_ok(cache) || q_heads < 1 || q_heads % cache->kv_heads) return 0;
+    if (!h || !cache_ok(cache) || !heads_ok(cache, q_heads)) return 0;
     const ServeView v = serve_view(const_cast<stand_handle *>(h));
     const AttnForm f = attn_form((int64_t)v.N * (q_heads / cache->kv_heads));
-    return with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, f, [&](auto s) { return attn_part_bytes<decltype(s)>(v.cus); });
+    return with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, f,
+                           [&](auto s) { return attn_work_bytes<decltype(s)>(attn_groups_of<decltype(s)>(v)); });
 }
 
 extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, int32_t layer, const int32_t *d_len,
                                     const int32_t *d_table, int32_t table_width, const int32_t *d_draft_tok,
                                     const stand_tree_rows *rows, void *d_work, uint64_t work_bytes, void *stream)
 {
-    if (!h || !cache_ok(cache) || !rows || !d_len || !d_table || !d_draft_tok || !d_work) return STAND_EINVAL;
-    if (layer < 0 || layer >= cache->layers || table_width < 1) return STAND_EINVAL;
-    if (!rows->d_q || !rows->d_k || !rows->d_v || !rows->d_out) return STAND_EINVAL;
-    if (!aligned16(rows->d_q) || !aligned16(rows->d_k) || !aligned16(rows->d_v) || !aligned16(rows->d_out) || !aligned16(d_work))
-        return STAND_EINVAL;
-    if (!strides_ok(rows->q_stride) || !strides_ok(rows->k_stride) || !strides_ok(rows->v_stride) || !strides_ok(rows->out_stride))
-        return STAND_EINVAL;
-    if (rows->q_heads < 1 || rows->q_heads % cache->kv_heads) return STAND_EINVAL;
-    if (!(rows->scale > 0.0f) || !std::isfinite(rows->scale)) return STAND_EINVAL;
-    if (work_bytes < stand_tree_attention_work(h, cache, rows->q_heads)) return STAND_EINVAL;
+    if (!h) return STAND_EINVAL;
     const ServeView v = serve_view(h);
-    if ((int64_t)table_width * cache->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
-    if (v.B > kAttnMaxBatch || rows->q_heads > 65535) return STAND_ELIMIT;
-    // the kernel counts places of a layer in 16-byte chunks, in 32 bits
-    if (!spans_chunks(cache->pages - 1, cache->page_stride, cache->page_size - 1, cache->slot_stride)) return STAND_ELIMIT;
-    const DeviceScope scope(v.device);
-    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    const int refused = check_tree_attention(v.B, cache, layer, d_len, d_table, table_width, d_draft_tok, rows, d_work);
+    if (refused) return refused;
     TreeAttnArgs a;
     a.q = (const uint16_t *)rows->d_q; a.k_new = (const uint16_t *)rows->d_k; a.v_new = (const uint16_t *)rows->d_v;
     a.out = (uint16_t *)rows->d_out;
@@ -174,21 +138,25 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     a.pool_page = cache->page_stride; a.pool_slot = cache->slot_stride; a.pool_head = cache->head_stride;
     a.scale = rows->scale; a.B = v.B; a.N = v.N; a.kv_heads = cache->kv_heads; a.per_kv = rows->q_heads / cache->kv_heads;
     a.width = table_width; a.pages = cache->pages; a.page_shift = log2_of(cache->page_size);
-    const hipError_t e = with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, attn_form((int64_t)v.N * a.per_kv),
-                                         [&](auto s) { return attn_launch<decltype(s)>(a, v.cus, (hipStream_t)stream); });
-    if (e == hipSuccess) return STAND_OK;
-    *v.last_hip = (int)e;
-    return STAND_EHIP;
+    return with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, attn_form((int64_t)v.N * a.per_kv), [&](auto s) {
+        using S = decltype(s);
+        a.groups = attn_groups_of<S>(v);
+        if (a.groups == 0) return STAND_EHIP;
+        if (work_bytes < attn_work_bytes<S>(a.groups)) return STAND_EINVAL;
+        const DeviceScope scope(v.device);
+        if (scope.e != hipSuccess) return bad_device(v, scope.e);
+        const hipError_t e = attn_launch<S>(a, (hipStream_t)stream);
+        return e == hipSuccess ? STAND_OK : bad_device(v, e);
+    });
 }
 
 extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots,
                                   int32_t width, const int32_t *d_row, const int32_t *d_count, void *stream)
 {
-    if (!h || !cache_ok(cache) || !rows || !rows->d_k || !rows->d_v || !d_slots || width < 1 || rows->rows < 1) return STAND_EINVAL;
-    if (!aligned16(rows->d_k) || !aligned16(rows->d_v)) return STAND_EINVAL;
-    if (!stride_ok(rows->layer_stride) || !stride_ok(rows->batch_stride) || !stride_ok(rows->row_stride) || !stride_ok(rows->head_stride))
-        return STAND_EINVAL;
+    if (!h) return STAND_EINVAL;
     const ServeView v = serve_view(h);
+    const int refused = check_cache_commit(v.B, cache, rows, d_slots, width);
+    if (refused) return refused;
     CommitArgs a;
     a.words = cache->head_dim / 8;
     a.heads = cache->kv_heads;
@@ -196,7 +164,6 @@ extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, con
     const int row_words = a.heads * a.words;
     a.per_group = (1024 + row_words - 1) / row_words;
     const int64_t groups = (width + (int64_t)a.per_group - 1) / a.per_group;
-    if (v.B > 65535 || cache->layers > 65535 || groups * 256 > UINT32_MAX) return STAND_ELIMIT;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
     a.k_rows = (const uint4 *)rows->d_k; a.v_rows = (const uint4 *)rows->d_v;
@@ -215,13 +182,10 @@ extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, con
 extern "C" int stand_cache_pages(stand_handle *h, const stand_pages *p, const int32_t *d_add, const int32_t *d_room, int64_t *d_slots,
                                  int32_t slot_width, int32_t *d_missing, const stand_pages *out, void *stream)
 {
-    if (!h || !p || !out || !p->d_table || !p->d_ring || !p->d_length || !p->d_held || !p->d_mark || !d_missing) return STAND_EINVAL;
-    if (!out->d_length || !out->d_held || !out->d_mark) return STAND_EINVAL;
-    if (out->d_table != p->d_table || out->d_ring != p->d_ring || out->width != p->width || out->pages != p->pages || out->page_size != p->page_size)
-        return STAND_EINVAL;
-    if (p->width < 1 || p->pages < 1 || !page_size_ok(p->page_size) || slot_width < 0 || (slot_width > 0 && !d_slots)) return STAND_EINVAL;
-    if ((int64_t)p->width * p->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
+    if (!h) return STAND_EINVAL;
     const ServeView v = serve_view(h);
+    const int refused = check_cache_pages(v.B, p, d_slots, slot_width, d_missing, out);
+    if (refused) return refused;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
     PagesArgs a;
@@ -258,11 +222,12 @@ extern "C" int stand_shape_logits(stand_handle *h, const void *d_logits, void *d
                                   const float *d_penalty, const int32_t *d_bias_id, const float *d_bias, int32_t bias_width,
                                   const uint32_t *d_allow, void *d_work, uint64_t work_bytes, void *stream)
 {
-    if (!h || !d_logits || !d_out || !d_draft_tok || bias_width < 0 || (bias_width > 0 && (!d_bias_id || !d_bias))) return STAND_EINVAL;
-    if (d_allow && (!d_work || work_bytes < stand_shape_logits_work(h))) return STAND_EINVAL;
+    if (!h) return STAND_EINVAL;
     const ServeView v = serve_view(h);
+    const int refused = check_shape_logits(v.B, v.logits_dtype, d_logits, d_out, d_draft_tok, d_bias_id, d_bias, bias_width);
+    if (refused) return refused;
+    if (d_allow && (!d_work || work_bytes < stand_shape_logits_work(h))) return STAND_EINVAL;
     const bool f32 = v.logits_dtype == STAND_F32;
-    if (((uintptr_t)d_logits | (uintptr_t)d_out) & (f32 ? 3u : 1u)) return STAND_EINVAL;
     ShapeArgs a;
     a.x = d_logits; a.out = d_out; a.draft_tok = d_draft_tok; a.count = d_count; a.penalty = d_penalty; a.bias_id = d_bias_id; a.bias = d_bias;
     a.allow = d_allow; a.anc = v.anc; a.anc_words = v.anc_words; a.N = v.N; a.V = v.V; a.M = bias_width; a.words = (v.V + 31) / 32;
@@ -273,7 +238,7 @@ extern "C" int stand_shape_logits(stand_handle *h, const void *d_logits, void *d
     while (a.nodes_per_group > 1 && spans * v.B * ((v.N + a.nodes_per_group - 1) / a.nodes_per_group) < 2048) a.nodes_per_group /= 2;
     a.node_groups = (v.N + a.nodes_per_group - 1) / a.nodes_per_group;
     a.spans = (int)spans;
-    if (v.B > 65535 || spans * a.node_groups * v.B > (int64_t)(UINT32_MAX / kShapeThreads)) return STAND_ELIMIT;
+    if (spans * a.node_groups * v.B > (int64_t)(UINT32_MAX / kShapeThreads)) return STAND_ELIMIT;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
     const dim3 grid((unsigned)(spans * a.node_groups * v.B));
@@ -286,10 +251,11 @@ extern "C" int stand_shape_logits(stand_handle *h, const void *d_logits, void *d
 extern "C" int stand_count_tokens(stand_handle *h, int32_t *d_count, const int32_t *d_tok, const int32_t *d_len, int32_t width,
                                   int32_t prompt, void *stream)
 {
-    if (!h || !d_count || !d_tok || width < 1) return STAND_EINVAL;
+    if (!h) return STAND_EINVAL;
     const ServeView v = serve_view(h);
+    const int refused = check_count_tokens(v.B, d_count, d_tok, width);
+    if (refused) return refused;
     const int64_t groups = ((int64_t)width + 255) / 256;
-    if (v.B > 65535) return STAND_ELIMIT;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
     count_tokens_kernel<<<dim3((unsigned)groups, (unsigned)v.B), dim3(256), 0, (hipStream_t)stream>>>(d_count, d_tok, d_len, v.V, width, prompt);
