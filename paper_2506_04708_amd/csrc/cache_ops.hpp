@@ -59,11 +59,15 @@ struct PagesArgs {
     int32_t *length_out, *held_out, *missing;
     long long *mark_out, *slots;
     int B, width, pages, page_shift, slot_width, default_room;
-    int per_group;              // consecutive trajectories of a workgroup, at most kPagesThreads
+    int per_group;              // consecutive trajectories of a workgroup, at most kPagesMine
     int what;                   // kPagesTables | kPagesState
 };
 constexpr int kPagesTables = 1, kPagesState = 2;
-constexpr int kPagesThreads = 256;
+constexpr int kPagesThreads = 512;   // (256: 11.6 us for 512 trajectories with 4000 slots each, 1024: 14.8, this: 10.5)
+constexpr int kPagesMine = 64;       // trajectories of a workgroup: 1024 of them have all
+constexpr int kPagesGroups = 1024;
+constexpr int kPagesKept = 2;        // of a thread's trajectories, in registers
+constexpr int kPagesFirst = 8;       // a step takes one page or two of a trajectory
 
 struct PagesDemand { long long len; int need, held, ask, give, room; };
 
@@ -91,10 +95,10 @@ __device__ __forceinline__ PagesDemand pages_demand(const PagesArgs &a, int b)
 __global__ __launch_bounds__(kPagesThreads) void cache_pages_kernel(PagesArgs a)
 {
     struct Mine { long long len, before, back; int need, held, now, ask, give, room; };
-    __shared__ Mine mine[kPagesThreads];
-    __shared__ long long wave_ask[4], wave_give[4];
+    __shared__ Mine mine[kPagesMine];
+    __shared__ long long wave_ask[kPagesThreads / 64], wave_give[kPagesThreads / 64];
     __shared__ unsigned long long granted;
-    __shared__ int most_ask, most_give;
+    __shared__ int most;
     const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
     const long long taken = a.mark[0], given = a.mark[1];
     long long avail = given - taken;
@@ -102,11 +106,16 @@ __global__ __launch_bounds__(kPagesThreads) void cache_pages_kernel(PagesArgs a)
     const int chunk = (a.B + kPagesThreads - 1) / kPagesThreads, c0 = t * chunk, c1 = min(a.B, c0 + chunk);
     const int b0 = blockIdx.x * a.per_group, b1 = min(a.B, b0 + a.per_group);
 
-    // sums before this thread's trajectories
+    // sums before this thread's trajectories; what the first ones ask for is kept
     long long ask = 0, give = 0;
-    PagesDemand d;
-    for (int b = c0; b < c1; ++b) {
-        d = pages_demand(a, b);
+    PagesDemand kept[kPagesKept];
+#pragma unroll
+    for (int q = 0; q < kPagesKept; ++q) kept[q] = pages_demand(a, min(c0 + q, a.B - 1));
+#pragma unroll
+    for (int q = 0; q < kPagesKept; ++q)
+        if (c0 + q < c1) { ask += kept[q].ask; give += kept[q].give; }
+    for (int b = c0 + kPagesKept; b < c1; ++b) {
+        const PagesDemand d = pages_demand(a, b);
         ask += d.ask; give += d.give;
     }
     long long up_ask = ask, up_give = give;
@@ -115,33 +124,32 @@ __global__ __launch_bounds__(kPagesThreads) void cache_pages_kernel(PagesArgs a)
         if (lane >= off) { up_ask += x; up_give += y; }
     }
     if (lane == 63) { wave_ask[wave] = up_ask; wave_give[wave] = up_give; }
-    if (t == 0) { granted = 0; most_ask = 0; most_give = 0; }
+    if (t == 0) { granted = 0; most = 0; }
     __syncthreads();
     long long before = up_ask - ask, back = up_give - give;
     for (int k = 0; k < wave; ++k) { before += wave_ask[k]; back += wave_give[k]; }
 
     // what becomes of each
     const bool state = a.what & kPagesState;
-    const long long all_given = wave_give[0] + wave_give[1] + wave_give[2] + wave_give[3];
-    for (int b = c0; b < c1; ++b) {
+    long long all_given = 0;
+    for (int k = 0; k < kPagesThreads / 64; ++k) all_given += wave_give[k];
+    auto settle = [&](int b, const PagesDemand &d) {
         const bool ours = b >= b0 && b < b1;
-        if (!ours && !state) {
-            if (chunk > 1) { d = pages_demand(a, b); before += d.ask; back += d.give; }
-            continue;
-        }
-        if (chunk > 1) d = pages_demand(a, b);
         const bool ok = d.need <= d.held || (d.need <= a.width && before + d.ask <= avail);
         const int now = ok ? d.need : d.held;
-        if (ok && d.ask) atomicMax(&granted, (unsigned long long)(before + d.ask));
+        if (state && blockIdx.x == 0 && ok && d.ask) atomicMax(&granted, (unsigned long long)(before + d.ask));
         if (ours && (a.what & kPagesTables)) {
             a.missing[b] = ok ? 0 : d.need - d.held;
             mine[b - b0] = Mine{d.len, before, back, d.need, d.held, now, ok ? d.ask : 0, d.give, d.room};
-            if (ok && d.ask) atomicMax(&most_ask, d.ask);
-            if (d.give) atomicMax(&most_give, d.give);
+            if (ok && d.ask + d.give > kPagesFirst) atomicMax(&most, d.ask + d.give);
         }
-        if (state && gridDim.x == 1 && (a.what & kPagesTables) == 0) { a.length_out[b] = (int)d.len; a.held_out[b] = now; }
+        if (state && !(a.what & kPagesTables)) { a.length_out[b] = (int)d.len; a.held_out[b] = now; }
         before += d.ask; back += d.give;
-    }
+    };
+#pragma unroll
+    for (int q = 0; q < kPagesKept; ++q)
+        if (c0 + q < c1) settle(c0 + q, kept[q]);
+    for (int b = c0 + kPagesKept; b < c1; ++b) settle(b, pages_demand(a, b));
     __syncthreads();
     if (state && t == 0 && blockIdx.x == 0) { a.mark_out[0] = taken + (long long)granted; a.mark_out[1] = given + all_given; }
     if (!(a.what & kPagesTables)) return;
@@ -153,29 +161,55 @@ __global__ __launch_bounds__(kPagesThreads) void cache_pages_kernel(PagesArgs a)
         return (unsigned)(x < P ? x : x - P < P ? x - P : x % P);
     };
     const int n = b1 - b0;
-    auto each = [&](int width, auto &&f) {                     // f(trajectory, j), j < width, over the workgroup's threads
-        if (width >= 64)
-            for (int k = 0; k < n; ++k)
-                for (int j = t; j < width; j += kPagesThreads) f(k, j);
-        else
-            for (int x = t; x < n * width; x += kPagesThreads) f(x / width, x % width);
+    // A trajectory either takes pages or gives some back: from one place in the ring or the table to one in the other.
+    auto from = [&](int k, const Mine &m, int i) {
+        return m.ask ? a.ring + ring_at(taken_at, m.before + i) : a.table + (long long)(b0 + k) * a.width + m.need + i;
     };
-    each(most_ask, [&](int k, int i) {
+    auto to = [&](int k, const Mine &m, int i) {
+        return m.ask ? a.table + (long long)(b0 + k) * a.width + m.held + i : a.ring + ring_at(given_at, m.back + i);
+    };
+    // the first few of all trajectories at once, a thread each; the rest of those that move many by teams of threads
+    for (int x = t; x < n * kPagesFirst; x += kPagesThreads) {
+        const int k = x / kPagesFirst, i = x % kPagesFirst;
         const Mine &m = mine[k];
-        if (i < m.ask) a.table[(long long)(b0 + k) * a.width + m.held + i] = a.ring[ring_at(taken_at, m.before + i)];
-    });
-    each(most_give, [&](int k, int i) {
-        const Mine &m = mine[k];
-        if (i < m.give) a.ring[ring_at(given_at, m.back + i)] = a.table[(long long)(b0 + k) * a.width + m.need + i];
-    });
-    each(a.slot_width, [&](int k, int j) {
+        if (i < m.ask + m.give) *to(k, m, i) = *from(k, m, i);
+    }
+    int team = kPagesThreads;
+    while (team > 64 && team * n > kPagesThreads) team /= 2;
+    const int at = t & (team - 1);
+    if (most)
+        for (int k = t / team; k < n; k += kPagesThreads / team) {
+            const Mine &m = mine[k];
+            const int count = m.ask + m.give;
+            for (int i0 = kPagesFirst + at; i0 < count; i0 += 4 * team) {
+                int32_t page[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) page[u] = i0 + u * team < count ? *from(k, m, i0 + u * team) : 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (i0 + u * team < count) *to(k, m, i0 + u * team) = page[u];
+            }
+        }
+    auto slot_of = [&](int k, int j) {
         const Mine &m = mine[k];
         const long long pos = m.len + j, pg = pos >> a.page_shift;
-        long long slot = -1;
-        if (j < m.room && pg < m.now)
-            slot = (long long)(pg < m.held ? a.table[(long long)(b0 + k) * a.width + pg] : a.ring[ring_at(taken_at, m.before + pg - m.held)]) * ps + (pos & (ps - 1));
-        a.slots[(long long)(b0 + k) * a.slot_width + j] = slot;
-    });
+        if (j >= m.room || pg >= m.now) return -1ll;
+        const int page = pg < m.held ? a.table[(long long)(b0 + k) * a.width + pg] : a.ring[ring_at(taken_at, m.before + pg - m.held)];
+        return (long long)page * ps + (pos & (ps - 1));
+    };
+    long long *slots = a.slots + (long long)b0 * a.slot_width;
+    if (a.slot_width < 64)
+        for (int x = t; x < n * a.slot_width; x += kPagesThreads) slots[x] = slot_of(x / a.slot_width, x % a.slot_width);
+    else
+        for (int k = t / team; k < n; k += kPagesThreads / team)
+            for (int j0 = at; j0 < a.slot_width; j0 += 4 * team) {
+                long long slot[4];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) slot[u] = j0 + u * team < a.slot_width ? slot_of(k, j0 + u * team) : 0;
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+                    if (j0 + u * team < a.slot_width) slots[(long long)k * a.slot_width + j0 + u * team] = slot[u];
+            }
     if (state)
         for (int k = t; k < n; k += kPagesThreads) { a.length_out[b0 + k] = (int)mine[k].len; a.held_out[b0 + k] = mine[k].now; }
 }

@@ -196,10 +196,11 @@ extern "C" int stand_cache_pages(stand_handle *h, const stand_pages *p, const in
     a.B = v.B; a.width = p->width; a.pages = p->pages; a.page_shift = log2_of(p->page_size); a.slot_width = slot_width;
     a.default_room = v.D + 1;
     // One workgroup where that is little work (up to 64 trajectories with 4096 slots: the state is then written behind its own
-    // reads); else up to 1024 of them.
+    // reads); else one for each trajectory, up to 1024 of them.
     const bool aside = out->d_length != p->d_length && out->d_held != p->d_held && out->d_mark != p->d_mark;
     const int64_t slots = (int64_t)v.B * slot_width;
-    int64_t groups = v.B <= 64 && slots <= 4096 ? 1 : std::min<int64_t>(v.B, 1024);
+    static_assert(kServeMaxBatch <= kPagesMine * kPagesGroups, "a workgroup's trajectories stand in LDS");
+    int64_t groups = v.B <= kPagesMine && slots <= 4096 ? 1 : std::min<int64_t>(v.B, kPagesGroups);
     a.per_group = (int)((v.B + groups - 1) / groups);
     groups = (v.B + a.per_group - 1) / a.per_group;
     a.what = groups == 1 || aside ? kPagesTables | kPagesState : kPagesTables;
