@@ -247,7 +247,7 @@ class Pages:
         self.page_size, self.table, self.ring, self.length, self.held, self.mark = page_size, table, ring, length, held, mark
         self.desc = PagesDesc(*[_dptr(t, torch.int32) for t in (table, ring, length, held)], _dptr(mark, torch.int64),
                               table.shape[1], ring.shape[0], page_size)
-        self.ref = C.addressof(self.desc)
+        self.ref, self.index = C.addressof(self.desc), table.get_device()
 
     @classmethod
     def new(cls, batch, pages, page_size, width, device="cuda"):
@@ -278,6 +278,7 @@ class Stand:
         self.W = self.D + 1
         self.logits_dtype = logits_dtype
         self.device = torch.device("cuda", device)
+        self._index = device
         self._work_bytes = {}   # of an attention, by its heads and type
 
     def close(self):
@@ -409,14 +410,16 @@ class Stand:
         _check(self._lib.stand_tree_packing(self.h, _dptr(mask), _dptr(pos), _stream_ptr_up()), self.h)
         return mask, pos
 
-    def _here(self, *tensors):
-        index = self.device.index
-        for t in tensors:
-            assert t is None or t.get_device() == index, "tensor on %s, handle on %s" % (t.device, self.device)
+    def _arg(self, t, dtype):
+        """Pointer of a contiguous tensor on the handle's device (None: none)."""
+        if t is None:
+            return None
+        assert t.dtype is dtype and t.get_device() == self._index and t.is_contiguous(), (t.dtype, dtype, t.device)
+        return t.data_ptr()
 
     def _stream(self):
         # the caller's stream on the handle's device, whichever device is the current one
-        return _stream_of(self.device.index)
+        return _stream_of(self._index)
 
     def tree_attention(self, cache, layer, length, table, draft_tok, q, k, v, scale=None, out=None):
         """Attention of the drafted nodes over the cache's first length[b] tokens and their own ancestors: q [B, N, heads, d],
@@ -429,18 +432,18 @@ class Stand:
         (q0, q1, q2, q3), (k0, k1, k2, k3), (v0, v1, v2, v3), (o0, o1, o2, o3) = q.stride(), k.stride(), v.stride(), out.stride()
         assert q3 == k3 == v3 == o3 == 1
         rows, width = table.shape
-        assert rows == B and length.shape == (B,) and draft_tok.shape == (B, N) and cache.index == self.device.index
-        self._here(length, table, draft_tok, q, k, v, out)
+        assert rows == B and length.shape == (B,) and draft_tok.shape == (B, N)
+        assert self._index == cache.index == q.get_device() == k.get_device() == v.get_device() == out.get_device()
         desc = _TREE_ROWS.pack(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), H, d ** -0.5 if scale is None else scale,
                                q0, q1, q2, k0, k1, k2, v0, v1, v2, o0, o1, o2)
         key = (H, cache.heads, d, cache.desc.dtype)
         need = self._work_bytes.get(key)
-        if need is None:
+        if not need:
             need = self._work_bytes[key] = self._lib.stand_tree_attention_work(self.h, cache.ref, H)
         # (torch's allocator hands this memory on in the order of the stream, and keeps a captured graph's apart)
         work = torch.empty(max(need, 16), dtype=torch.uint8, device=self.device)
-        _check(self._lib.stand_tree_attention(self.h, cache.ref, layer, _dptr(length, torch.int32), _dptr(table, torch.int32), width,
-                                              _dptr(draft_tok, torch.int32), desc, work.data_ptr(), need, self._stream()), self.h)
+        _check(self._lib.stand_tree_attention(self.h, cache.ref, layer, self._arg(length, torch.int32), self._arg(table, torch.int32), width,
+                                              self._arg(draft_tok, torch.int32), desc, work.data_ptr(), need, self._stream()), self.h)
         return out
 
     def cache_commit(self, cache, k, v, slots, row=None, count=None):
@@ -448,12 +451,12 @@ class Stand:
         layers, B, rows, heads, d = k.shape
         stride = k.stride()
         assert k.shape == v.shape and stride == v.stride() and stride[4] == 1 and cache.dtype is k.dtype and cache.dtype is v.dtype
-        assert layers == cache.layers and B == self.B and heads == cache.heads and d == cache.dim and cache.index == self.device.index
+        assert layers == cache.layers and B == self.B and heads == cache.heads and d == cache.dim
         assert slots.dim() == 2 and slots.shape[0] == B and (row is None or row.shape == slots.shape) and (count is None or count.shape == (B,))
-        self._here(k, v, slots, row, count)
+        assert self._index == cache.index == k.get_device() == v.get_device()
         desc = _CACHE_ROWS.pack(k.data_ptr(), v.data_ptr(), rows, *stride[:4])
-        _check(self._lib.stand_cache_commit(self.h, cache.ref, desc, _dptr(slots, torch.int64), slots.shape[1],
-                                            _dptr(row, torch.int32), _dptr(count, torch.int32), self._stream()), self.h)
+        _check(self._lib.stand_cache_commit(self.h, cache.ref, desc, self._arg(slots, torch.int64), slots.shape[1],
+                                            self._arg(row, torch.int32), self._arg(count, torch.int32), self._stream()), self.h)
 
     def cache_pages(self, pages, add=None, room=None, slots=None, missing=None, out=None):
         """Moves lengths on by add, takes and gives back pages for room more tokens (None: a whole path); slots [B, any] and
@@ -463,9 +466,9 @@ class Stand:
         out = pages if out is None else out
         assert pages.table.shape[0] == self.B and missing.shape == (self.B,) and (slots is None or (slots.dim() == 2 and slots.shape[0] == self.B))
         assert (add is None or add.shape == (self.B,)) and (room is None or room.shape == (self.B,))
-        self._here(pages.table, out.table, add, room, slots, missing)
-        _check(self._lib.stand_cache_pages(self.h, pages.ref, _dptr(add, torch.int32), _dptr(room, torch.int32), _dptr(slots, torch.int64),
-                                           0 if slots is None else slots.shape[1], _dptr(missing, torch.int32), out.ref, self._stream()), self.h)
+        assert self._index == pages.index == out.index
+        _check(self._lib.stand_cache_pages(self.h, pages.ref, self._arg(add, torch.int32), self._arg(room, torch.int32), self._arg(slots, torch.int64),
+                                           0 if slots is None else slots.shape[1], self._arg(missing, torch.int32), out.ref, self._stream()), self.h)
         return missing
 
     def shape_logits(self, logits, out, draft_tok, count=None, penalty=None, bias_id=None, bias=None, allow=None):
@@ -477,19 +480,18 @@ class Stand:
         assert penalty is None or penalty.shape == (self.B, 3)
         assert (bias_id is None) == (bias is None) and (bias is None or bias.shape == bias_id.shape == (self.B, M))
         assert allow is None or allow.shape == (self.B, self.N, (self.V + 31) // 32)
-        self._here(logits, out, draft_tok, count, penalty, bias_id, bias, allow)
+        assert self._index == logits.get_device() == out.get_device()
         work = None if allow is None else torch.empty(self.B * self.N, dtype=torch.uint8, device=self.device)
-        _check(self._lib.stand_shape_logits(self.h, self._logits_ptr(logits), self._logits_ptr(out), _dptr(draft_tok, torch.int32),
-                                            _dptr(count, torch.int32), _dptr(penalty, torch.float32), _dptr(bias_id, torch.int32),
-                                            _dptr(bias, torch.float32), M, _dptr(allow, torch.int32), _dptr(work), self.B * self.N,
-                                            self._stream()), self.h)
+        _check(self._lib.stand_shape_logits(self.h, self._logits_ptr(logits), self._logits_ptr(out), self._arg(draft_tok, torch.int32),
+                                            self._arg(count, torch.int32), self._arg(penalty, torch.float32), self._arg(bias_id, torch.int32),
+                                            self._arg(bias, torch.float32), M, self._arg(allow, torch.int32),
+                                            None if work is None else work.data_ptr(), self.B * self.N, self._stream()), self.h)
         return out
 
     def count_tokens(self, count, tok, length=None, prompt=False):
         """Tokens tok [B, any] (the first length[b] of them) into count [B, V]: generated ones, or the prompt's."""
         assert count.shape == (self.B, self.V) and tok.dim() == 2 and tok.shape[0] == self.B and (length is None or length.shape == (self.B,))
-        self._here(count, tok, length)
-        _check(self._lib.stand_count_tokens(self.h, _dptr(count, torch.int32), _dptr(tok, torch.int32), _dptr(length, torch.int32),
+        _check(self._lib.stand_count_tokens(self.h, self._arg(count, torch.int32), self._arg(tok, torch.int32), self._arg(length, torch.int32),
                                             tok.shape[1], int(prompt), self._stream()), self.h)
 
     def record_slots(self, rows_per_trajectory, orders):
