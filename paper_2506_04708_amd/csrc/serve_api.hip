@@ -43,9 +43,15 @@ int bad_device(const ServeView &v, hipError_t e)
     return STAND_EHIP;
 }
 
-// The form of the attention kernel a call takes, by the rows that share a key/value head.
-enum AttnForm { kAttn32, kAttn64, kAttn128, kAttn256 };
-AttnForm attn_form(int64_t rows) { return rows <= 32 ? kAttn32 : rows <= 64 ? kAttn64 : rows <= 128 ? kAttn128 : kAttn256; }
+// The form of the attention kernel a call takes, by the rows that share a key/value head, as if all nodes were drafted.
+//   up to 32: four waves on different keys, each loading its own without a barrier (32 trees of 17 .. 32 rows, d 64: 44 us, with
+//     tiles of 256 rows 51; up to 64 rows it would be behind: 90 us instead of 74, d 128);
+//   up to 64: two waves of rows on each half of a stage's keys (32 trees, d 128: 72 us, with tiles of 256 rows 75; d 64: 42 and
+//     49 us);
+//   above: eight waves of rows with d 128, 256 of them (four waves of rows on halves of the keys took the same times, 85 .. 89 us,
+//     with 128 rows); with d 64 four, whose two workgroups share a compute unit (128 trees of 128 nodes: 190 us, eight: 207).
+enum AttnForm { kAttn32, kAttn64, kAttnMore };
+AttnForm attn_form(int64_t rows) { return rows <= 32 ? kAttn32 : rows <= 64 ? kAttn64 : kAttnMore; }
 
 template <int D, bool F16, typename Call>
 auto with_attn_shape(AttnForm f, Call call)
@@ -53,7 +59,6 @@ auto with_attn_shape(AttnForm f, Call call)
     switch (f) {
     case kAttn32: return call(AttnShape<D, F16, 1, 4, 1>{});
     case kAttn64: return call(AttnShape<D, F16, 2, 2, 1>{});
-    case kAttn128: return call(AttnShape<D, F16, 4, D == 64 ? 1 : 2, D == 64 ? 2 : 1>{});
     default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2>{});
     }
 }

@@ -1,4 +1,30 @@
 // tree_attn.hpp -- attention of the nodes of a drafted tree over a paged key/value cache and over their own ancestors.
+//
+// For a row (one node, one query head) and the keys t that it sees, c = scale * log2(e):
+//     out = sum_t w_t value_t / sum_t w_t,    w_t = 2^(c * query . key_t - m)
+// in one pass over the keys with a running m; any m gives the same quotient.  m is raised only where a score passes it by more
+// than 8: weights are then at most 2^8, sums stay far inside fp32, and the outputs are scaled anew a few times per row instead of
+// at every maximum.  Weights are rounded to the cache's type for the matrix cores and summed as rounded, so that numerator and
+// denominator err together.  Scores, m, sums and outputs are fp32.
+//
+// Rows: drafted nodes are numbered through (a third of a tree is not drafted, and is not computed), and all query heads of a
+// key/value head share its keys, so a tile has up to 256 rows of (node, head) that read a key once.  A wave has 32 of them.  It
+// computes S^T = K Q^T with 32x32x16 products, so that a lane has one row and 16 of 32 keys: maximum and sum need one exchange
+// between two lanes, and the weights stand where the second product O^T = V^T P^T wants its right operand, with the keys in
+// another order; the values are read in that order (transposed by the LDS reads).  Nothing but keys and values passes through LDS.
+//
+// Keys come in stages of 64 or 128 by asynchronous copies, page numbers two stages ahead of them, into a swizzled layout that
+// both products read without bank conflicts.  Four stages of memory: two on their way, one in work, one whose values are
+// still read.
+//
+// Work: trajectories differ in length a hundredfold, so tiles are cut by units of a stage, equal shares for every workgroup the
+// chip holds (attn_plan.hpp); items that were cut are joined by a second kernel.  No atomics: the same call gives the same bits.
+//
+// Bound: decoding by HBM (2.04 GB of cache in 353 us, 5.8 TB/s; a torch copy reaches 4.9 counting both ways); larger trees by
+// what a wave issues between its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128:
+// 125 us for 70 GFLOP, 565 TFLOP/s on rows as they are, where a large matrix product reaches 1211); alone on a SIMD a step of 32
+// keys takes a wave 404 ns, of which its 16 matrix instructions are 262.  Short calls are bound by the chain lengths -> shares ->
+// nodes -> page numbers -> keys, each a trip to memory: 11.5 us, and 3.8 us for the join.
 #pragma once
 #include "attn_plan.hpp"
 #include "wave_ops.hpp"
@@ -97,6 +123,7 @@ __device__ __forceinline__ void group_barrier()
     asm volatile("" ::: "memory");
 }
 
+// A form of the kernel: WR waves with 32 rows each times WK waves with SUB * 32 keys of a stage each.
 template <int D_, bool F16_, int WR_, int WK_, int SUB_>
 struct AttnShape {
     static constexpr int D = D_, WR = WR_, WK = WK_, SUB = SUB_;
@@ -107,7 +134,9 @@ struct AttnShape {
     static constexpr int KT = 32 * WK * SUB;           // keys of a stage
     static constexpr bool ALONE = WR == 1;             // every wave loads the keys that it alone uses
     static constexpr int NBUF = ALONE ? 2 : 4;         // stages in LDS: two on their way, one in work, one whose values are still read
-    static constexpr int START = ALONE ? 2 : D == 64 ? 8 : 4;  // units that the beginning of an item costs, see attn_plan.hpp
+    // units that the beginning of an item costs, see attn_plan.hpp (half and twice as many: 216 and 233 us instead of 214 for 128
+    // trees of 128 nodes with heads of 64, 178 and 175 instead of 173 for 32 trees of 64 with heads of 128)
+    static constexpr int START = ALONE ? 2 : D == 64 ? 8 : 4;
     static constexpr int ROW = 2 * D;                  // bytes of a key
     static constexpr int CPR = D / 8;                  // 16-byte chunks of a key
     static constexpr int KPI = 64 / CPR;               // keys of one copy instruction
@@ -131,10 +160,9 @@ struct AttnShape {
 };
 
 // Units of work before each trajectory, prefix[0 .. B], in LDS: a unit is a stage of KT keys for one tile of rows and one
-// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) +
-// ceil(N / KT) units.  Every
-// workgroup counts all drafted nodes for itself, eight reads in flight (one after the other they took 17 us for 128 trees of
-// 128 nodes).
+// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) + ceil(N / KT) units.
+// Every workgroup counts all drafted nodes for itself, eight reads in flight (one after the other they took 17 us for 128 trees
+// of 128 nodes).
 template <int TM, int KT, int THREADS, int START>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
 {
@@ -521,8 +549,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             load_stage(0);
             if (n > 1) { load_ids(3); load_stage(1); }
         }
-        uint32_t *odd = (uint32_t *)(attn_lds + S::MISC);       // [N / 32]: nodes with a value that is no finite number
-        if (threadIdx.x < 32) odd[threadIdx.x] = 0;
+        uint32_t *wild = (uint32_t *)(attn_lds + S::MISC);      // [N / 32]: nodes with a value that is no finite number
+        if (threadIdx.x < 32) wild[threadIdx.x] = 0;
         // A unit that has come: everyone's copies are there, two units ahead are on their way, the tree's values are finite.
         // -> the keys of this wave's subtile t that count for this lane's query: bits, `all` of them.
         auto arrive = [&](int i) {
@@ -552,7 +580,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 if (found) {
                     *vp = vw;
                     const int v = (i - cached) * KT + x / S::CPR;
-                    if (v < a.N) atomicOr(&odd[v / 32], 1u << (v & 31));
+                    if (v < a.N) atomicOr(&wild[v / 32], 1u << (v & 31));
                 }
             }
             __syncthreads();
@@ -585,7 +613,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
         } else {
-            float16v even, odd_s;                               // scores of every other subtile: they change places, not registers
+            float16v even, odd;                               // scores of every other subtile: they change places, not registers
 #pragma unroll
             for (int x = 0; x < 16; ++x) even[x] = -__builtin_huge_valf();
             // (before the first keys there is no weight at all, and values that are there: the first unit's own)
@@ -607,10 +635,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                         for (int t = 0; t < SUB; ++t) {
                             const uint32_t here = off + t * 32 * S::ROW;
-                            if (SUB > 1 && t == 0) step(No{}, Yes{}, even, odd_s, here, before, true, 0u);
-                            else if (SUB > 1) step(Yes{}, No{}, odd_s, even, here, before, true, 0u);
-                            else if (x % 2 == 0) step(No{}, No{}, even, odd_s, here, before, true, 0u);
-                            else step(No{}, No{}, odd_s, even, here, before, true, 0u);
+                            if (SUB > 1 && t == 0) step(No{}, Yes{}, even, odd, here, before, true, 0u);
+                            else if (SUB > 1) step(Yes{}, No{}, odd, even, here, before, true, 0u);
+                            else if (x % 2 == 0) step(No{}, No{}, even, odd, here, before, true, 0u);
+                            else step(No{}, No{}, odd, even, here, before, true, 0u);
                             before = here;
                         }
                     }
@@ -627,8 +655,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                     word = counting(j / SUB, j % SUB, all);
                     off = (j / SUB % S::NBUF) * S::STAGE + j % SUB * 32 * S::ROW;
                 }
-                step(No{}, No{}, even, odd_s, off, before, all, word);
-                even = odd_s;
+                step(No{}, No{}, even, odd, off, before, all, word);
+                even = odd;
                 before = off;
             }
         }
@@ -636,7 +664,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
             for (int x = 0; x < (a.N + 31) / 32; ++x) {
                 if (x % (KT / 32) / SUB != wk) continue;
-                for (uint32_t bits = odd[x]; bits; bits &= bits - 1) {
+                for (uint32_t bits = wild[x]; bits; bits &= bits - 1) {
                     // an infinity or NaN reaches the rows that see its node, whatever its weight
                     const int v = 32 * x + __builtin_ctz(bits);
                     const bool sees = (a.anc[(long long)node * a.anc_words + x] >> (v & 31)) & 1u;
@@ -719,10 +747,11 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
     zero_rows<S>(fresh_args<TreeAttnArgs>());          // (last: the first ones to be done have the time)
 }
 
-// Rows of items that several workgroups took: their parts joined, 32 rows (those of one wave) by a workgroup and in the layout of
+// Rows of items that several workgroups took: their parts joined (weights 2^(m - largest m)), 32 rows (those of one wave) by a workgroup and in the layout of
 // a wave's registers: lane l has the row l % 32 and every second group of four elements.  The workgroups of the item's second
 // share take a quarter of the elements with each wave; where there are many parts, those of eight shares take an eighth each and
-// their waves the parts in turn.
+// their waves the parts in turn.  Bound by the trip record -> place -> parts: 3.8 us for a short tree, 13.5 us for the 17 MB of
+// parts of 32 trees of 64 nodes (256 workgroups' shares, each up to two parts of 256 rows).
 constexpr int kJoinShared = 8;        // more parts: shared
 template <int D, int TM, bool F16>
 __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
