@@ -373,7 +373,8 @@ int stand_read_rows(const void *d_src, uint64_t row_bytes, uint64_t rows, uint32
  *
  * The calls take tree, batch, vocabulary, type of the logits and device from the handle, read nothing else of it and change
  * nothing in it; they allocate nothing, keep nothing, and may be captured into a graph.  The caller's current device is
- * the same after a call.  Up to 65 535 trajectories, 4096 for the attention (STAND_ELIMIT above).
+ * the same after a call.  Up to 65 535 trajectories, 4096 for the attention (STAND_ELIMIT above); widths of tables, slots and lists
+ * are at most 2^30 (STAND_EINVAL above).
  *
  * Trees: the root's keys and values are those of the last committed token, which is not in the cache yet: a cache of n
  * tokens holds the positions 0 .. n-1 and node u stands at position n + depth(u) (stand_tree_packing's d_pos).  The rows of
@@ -414,7 +415,10 @@ typedef struct {
  * rows off a node's path and behind a length is never used, whatever it is (a NaN included).  d_draft_tok [B][N] is what
  * stand_draft / stand_step gave.  Token t of trajectory b is in page d_table[b][t / page_size], d_table: [B][table_width].
  * A length below 0 counts as 0, one above table_width * page_size (at most STAND_MAX_CACHED) as that; a page outside the cache is never
- * read (what is read instead is not specified).  A tree of one node is the ordinary attention of single tokens.
+ * read (what is read instead is not specified).  A tree of one node is the ordinary attention of single tokens.  Where a value
+ * that a row sees is infinite or NaN, that element of its output is one of the two (which is not specified); a score that is
+ * neither finite nor -infinity makes the row NaN.  A drafted node's ancestors are drafted.
+ *   Keys (and values) of one layer span less than 64 GiB (STAND_ELIMIT).
  *   Products are summed in fp32, the weights p are rounded to the cache's type for the product with the values (relative error
  * 2^-9 in bf16, 2^-12 in fp16 each, at most half a step) and summed as rounded; the result is rounded once.
  *   d_work: 16-byte aligned device memory of stand_tree_attention_work bytes, used from the call's start to its end on the
