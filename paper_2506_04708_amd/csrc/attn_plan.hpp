@@ -23,29 +23,37 @@ STAND_BOTH long long item_units(long long len, long long most, int nodes_of_tree
 {
     return (clamp_length(len, most) + keys - 1) / keys + (nodes_of_tree + keys - 1) / keys;
 }
-// Items of a trajectory with `drafted` nodes: per_kv query heads share a key/value head, a tile has `tile_rows` rows.
-STAND_BOTH int tree_items(int drafted, int per_kv, int kv_heads, int tile_rows)
+// A head's rows (drafted nodes times query heads that share its keys) are full tiles and what is left.  What a unit of a tile
+// costs: `heavy`, or `light` where the tile fills no more than half of the waves.
+STAND_BOTH int tile_weight(int rows, int tile_rows, int heavy, int light) { return 2 * rows > tile_rows ? heavy : light; }
+// The weights of all tiles of a head together.
+STAND_BOTH long long head_weight(int rows, int tile_rows, int heavy, int light)
 {
-    return (drafted * per_kv + tile_rows - 1) / tile_rows * kv_heads;
+    const int left = rows % tile_rows;
+    return (long long)(rows / tile_rows) * heavy + (left ? tile_weight(left, tile_rows, heavy, light) : 0);
 }
-// Rows of each of a head's tiles but the last: equal ones, in whole waves.
-STAND_BOTH int rows_of_tile(int rows, int tiles) { return ((rows + tiles - 1) / tiles + 31) / 32 * 32; }
 // What an item costs beside its units (nodes, queries, page numbers and first keys to wait for) counts as `start` units at its
 // beginning, so that shares of many short items are no longer than others.  A share that would begin or end among them begins
-// or ends at the item's beginning instead.
-// Workgroups that get a share, of `groups` launched: no share is shorter than start + 2.
-STAND_BOTH long long attn_groups(long long total, int groups, int start)
+// or ends at the item's beginning instead, one that would begin or end inside a unit does at the unit's beginning.
+// Units of an item that lie before a place of the work, places counted from the item's beginning.
+STAND_BOTH long long units_before(long long place, int weight, int start, long long units)
 {
-    const long long w = total / (start + 2);
+    const long long u = place / weight - start;
+    return u < 0 ? 0 : (u > units ? units : u);
+}
+// Workgroups that get a share, of `groups` launched: no share is shorter than start + 2 units of the heaviest kind.
+STAND_BOTH long long attn_groups(long long total, int groups, int start, int heavy)
+{
+    const long long w = total / (heavy * (start + 2));
     return w >= groups ? groups : w > 0 ? w : total > 0;
 }
 STAND_BOTH long long group_start(long long w, long long total, long long W) { return w * total / W; }
-// The last workgroup whose share would begin at or before a unit.
-STAND_BOTH long long group_of(long long unit, long long total, long long W) { return ((unit + 1) * W - 1) / total; }
+// The last workgroup whose share would begin at or before a place.
+STAND_BOTH long long group_of(long long place, long long total, long long W) { return ((place + 1) * W - 1) / total; }
 // The workgroup that has an item's first part.
-STAND_BOTH long long first_group(long long item_start, long long total, long long W, int start)
+STAND_BOTH long long first_group(long long item_start, long long total, long long W, int start, int weight)
 {
-    return group_of(item_start + start, total, W);
+    return group_of(item_start + (long long)(start + 1) * weight - 1, total, W);
 }
 
 }  // namespace stand

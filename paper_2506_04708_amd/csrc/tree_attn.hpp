@@ -137,6 +137,9 @@ struct AttnShape {
     // units that the beginning of an item costs, see attn_plan.hpp (half and twice as many: 216 and 233 us instead of 214 for 128
     // trees of 128 nodes with heads of 64, 178 and 175 instead of 173 for 32 trees of 64 with heads of 128)
     static constexpr int START = ALONE ? 2 : D == 64 ? 8 : 4;
+    // cost of a unit whose waves of rows share the SIMDs, and of one with a wave each, which its keys' way into LDS bounds (336 rows
+    // of 32 trees, a tile of 256 and one of 80: 133 us; by 2 : 1 142, 5 : 4 136, two tiles of 168 rows 141)
+    static constexpr int HEAVY = WR == 8 ? 3 : 1, LIGHT = WR == 8 ? 2 : 1;
     static constexpr int ROW = 2 * D;                  // bytes of a key
     static constexpr int CPR = D / 8;                  // 16-byte chunks of a key
     static constexpr int KPI = 64 / CPR;               // keys of one copy instruction
@@ -163,9 +166,10 @@ struct AttnShape {
 // key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) + ceil(N / KT) units.
 // Every workgroup counts all drafted nodes for itself, eight reads in flight (one after the other they took 17 us for 128 trees
 // of 128 nodes).
-template <int TM, int KT, int THREADS, int START>
+template <typename S>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
 {
+    constexpr int THREADS = S::THREADS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int first_len = a.len[lane < a.B ? lane : 0];    // (asked for before it is needed)
     for (int b = threadIdx.x; b <= a.B; b += THREADS) prefix[b] = 0;
@@ -200,7 +204,7 @@ __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *pref
         for (int b0 = 0; b0 < a.B; b0 += 64) {
             const int b = b0 + lane;
             long long x = 0;
-            if (b < a.B) x = (START + item_units(b0 ? a.len[b] : first_len, (long long)a.width << a.page_shift, a.N, KT)) * tree_items((int)prefix[b + 1], a.per_kv, a.kv_heads, TM);
+            if (b < a.B) x = (S::START + item_units(b0 ? a.len[b] : first_len, (long long)a.width << a.page_shift, a.N, S::KT)) * head_weight((int)prefix[b + 1] * a.per_kv, S::TM, S::HEAVY, S::LIGHT) * a.kv_heads;
             for (int off = 1; off < 64; off <<= 1) {
                 const long long y = __shfl_up(x, off);
                 if (lane >= off) x += y;
@@ -240,9 +244,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
     const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char *)attn_lds);
 
     long long *sums = (long long *)attn_lds;
-    unit_sums<TM, KT, S::THREADS, S::START>(a, sums);
+    unit_sums<S>(a, sums);
     const long long total = sums[a.B];
-    const long long W = attn_groups(total, a.groups, S::START);
+    const long long W = attn_groups(total, a.groups, S::START, S::HEAVY);
     if (threadIdx.x == 0 && (long long)blockIdx.x >= W) a.join[blockIdx.x] = JoinRecord{0, 0, 0, 0};   // (no share has this number)
     // neighbours in the order of the work share an XCD (workgroups go round the eight of them in turn) and so its L2
     const int per_xcd = (int)((W + 7) / 8);
@@ -293,27 +297,26 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         const long long most = (long long)a.width << a.page_shift;
         const int len = __builtin_amdgcn_readfirstlane((int)clamp_length(a.len[b], most));
         const int units = (int)item_units(len, most, a.N, KT), cache_units = (len + KT - 1) / KT, per_item = units + S::START;
-        const int tiles = tree_items(nodes, a.per_kv, 1, TM);
-        const int item = (int)((unit - b_start) / per_item);
+        const int all_rows = nodes * a.per_kv, full = all_rows / TM;
+        const long long per_head = per_item * head_weight(all_rows, TM, S::HEAVY, S::LIGHT);
+        const int heads_before = (int)((unit - b_start) / per_head);
+        const long long head_start = b_start + heads_before * per_head;
+        const int tile = min((int)((unit - head_start) / (S::HEAVY * per_item)), full);
+        const int row0 = tile * TM, rows = min(all_rows, row0 + TM), weight = tile_weight(rows - row0, TM, S::HEAVY, S::LIGHT);
         // (trajectories begin with different heads: at one time the same head of all of them would use a part of the memory
         // channels, where a token's heads stand side by side)
-        const int hk = (item / tiles + b) % a.kv_heads, tile = item % tiles;
-        const long long item_start = b_start + (long long)item * per_item;
-        if (unit_end - item_start <= S::START) break;  // the next one's
-        const int u0 = unit - item_start <= S::START ? 0 : (int)(unit - item_start) - S::START;
-        const int u1 = unit_end - item_start < per_item ? (int)(unit_end - item_start) - S::START : units;
+        const int hk = (heads_before + b) % a.kv_heads;
+        const long long item_start = head_start + (long long)tile * S::HEAVY * per_item, item_end = item_start + (long long)weight * per_item;
+        const int u0 = (int)units_before(unit - item_start, weight, S::START, units), u1 = (int)units_before(unit_end - item_start, weight, S::START, units);
+        if (u1 == 0) break;                            // the next one's
         bool leads = false;                            // this share is the second one of its first item
         if (first_item) {
             first_item = false;
-            const long long from = first_group(item_start, total, W, S::START);
+            const long long from = first_group(item_start, total, W, S::START, weight);
             leads = u0 > 0 && from == w - 1;
-            if (threadIdx.x == 0) {                    // (every share comes here: none ends before its first item begins)
-                const int each = rows_of_tile(nodes * a.per_kv, tiles);
-                a.join[w] = JoinRecord{(int)from, (int)group_of(item_start + per_item - 1, total, W), u0 > 0 ? min(each, nodes * a.per_kv - tile * each) : 0, 0};
-            }
+            if (threadIdx.x == 0)                      // (every share comes here: none ends before its first item begins)
+                a.join[w] = JoinRecord{(int)from, (int)group_of(item_end - 1, total, W), u0 > 0 ? rows - row0 : 0, 0};
         }
-        const int all_rows = nodes * a.per_kv, tile_rows = rows_of_tile(all_rows, tiles), row0 = tile * tile_rows;
-        const int rows = min(all_rows, row0 + tile_rows);
         const int row = row0 + wr * 32 + col;
         const bool busy = row0 + wr * 32 < rows;       // this wave has rows
         const int my_row = row < rows ? row : rows - 1;
@@ -741,8 +744,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 if (leads && half == 0) a.place[w * TM + at] = b * a.os[0] + node * a.os[1] + head * a.os[2];
             }
         }
-        unit = item_start + S::START + u1;
-        if (unit == b_start + (long long)per_item * tiles * fresh_args<TreeAttnArgs>().kv_heads) { b_start = unit; ++b; }
+        if (u1 < units) break;
+        unit = item_end;
+        if (unit == b_start + per_head * fresh_args<TreeAttnArgs>().kv_heads) { b_start = unit; ++b; }
     }
     zero_rows<S>(fresh_args<TreeAttnArgs>());          // (last: the first ones to be done have the time)
 }

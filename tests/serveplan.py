@@ -11,12 +11,13 @@ _SRC = """
 using namespace stand;
 extern "C" {
 int64_t units(int64_t len, int64_t most, int nodes, int keys) { return item_units(len, most, nodes, keys); }
-int items(int drafted, int per_kv, int heads, int rows) { return tree_items(drafted, per_kv, heads, rows); }
-int tile_rows(int rows, int tiles) { return rows_of_tile(rows, tiles); }
-int64_t groups(int64_t total, int launched, int start) { return attn_groups(total, launched, start); }
+int64_t head(int rows, int tile, int heavy, int light) { return head_weight(rows, tile, heavy, light); }
+int weight(int rows, int tile, int heavy, int light) { return tile_weight(rows, tile, heavy, light); }
+int64_t before(int64_t place, int weight, int start, int64_t units) { return units_before(place, weight, start, units); }
+int64_t groups(int64_t total, int launched, int start, int heavy) { return attn_groups(total, launched, start, heavy); }
 int64_t begin(int64_t w, int64_t total, int64_t W) { return group_start(w, total, W); }
 int64_t owner(int64_t unit, int64_t total, int64_t W) { return group_of(unit, total, W); }
-int64_t first(int64_t item, int64_t total, int64_t W, int start) { return first_group(item, total, W, start); }
+int64_t first(int64_t item, int64_t total, int64_t W, int start, int weight) { return first_group(item, total, W, start, weight); }
 int page(int p, int pages) { return clamp_page(p, pages); }
 int64_t length(int64_t len, int64_t most) { return clamp_length(len, most); }
 int attention(int64_t B, const stand_cache *c, int layer, const int32_t *len, const int32_t *table, int width, const int32_t *tok,
@@ -64,8 +65,9 @@ def lib():
                             os.path.join(ROOT, "paper_2506_04708_amd", "csrc"), "-o", so, src], check=True)
             _lib = C.CDLL(so)
         i, l, p = C.c_int, C.c_int64, C.c_void_p
-        for name, args, res in (("units", [l, l, i, i], l), ("items", [i, i, i, i], i), ("tile_rows", [i, i], i), ("groups", [l, i, i], l),
-                                ("begin", [l, l, l], l), ("owner", [l, l, l], l), ("first", [l, l, l, i], l), ("page", [i, i], i),
+        for name, args, res in (("units", [l, l, i, i], l), ("head", [i, i, i, i], l), ("weight", [i, i, i, i], i),
+                                ("before", [l, i, i, l], l), ("groups", [l, i, i, i], l),
+                                ("begin", [l, l, l], l), ("owner", [l, l, l], l), ("first", [l, l, l, i, i], l), ("page", [i, i], i),
                                 ("length", [l, l], l), ("attention", [l, p, i, p, p, i, p, p, p], i), ("commit", [l, p, p, p, i], i),
                                 ("cache_pages", [l, p, p, i, p, p], i), ("shape", [l, i, p, p, p, p, p, i], i), ("count", [l, p, p, i], i)):
             f = getattr(_lib, name)

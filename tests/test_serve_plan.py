@@ -23,76 +23,66 @@ def trajectories(rng, kind):
 
 
 @pytest.mark.parametrize("kind", ["short", "any"])
-@pytest.mark.parametrize("tile,keys,start", [(32, 128, 2), (64, 64, 4), (128, 64, 4), (256, 64, 4), (128, 64, 8)])
-def test_shares_cover_every_unit_once(kind, tile, keys, start):
+@pytest.mark.parametrize("tile,keys,start,heavy,light", [(32, 128, 2, 1, 1), (64, 64, 4, 1, 1), (256, 64, 4, 3, 2), (256, 64, 4, 2, 1), (128, 64, 8, 1, 1)])
+def test_shares_cover_every_unit_once(kind, tile, keys, start, heavy, light):
     """The kernel's walk over its shares, unit by unit, and what the join does with the parts."""
-    L, rng = serveplan.lib(), random.Random(tile + start)
+    L, rng = serveplan.lib(), random.Random(tile + start + heavy)
     for rep in range(60):
         lens, drafted, N, per, heads, most = trajectories(rng, kind)
         launched = rng.choice([8, 256, 512, 1024])
-        sums, items = [0], []                                  # of trajectories; (first unit, units) of every item
+        items, total = [], 0                                   # (first place, units, weight) of every item
         for n, t in zip(lens, drafted):
             u = L.units(n, most, N, keys)
             assert u == -(-min(max(n, 0), most) // keys) + -(-N // keys) and u >= 1
-            count = L.items(t, per, heads, tile)
-            assert count == -(-t * per // tile) * heads
-            items += [(sums[-1] + k * (u + start), u) for k in range(count)]
-            sums.append(sums[-1] + count * (u + start))
-        total = sums[-1]
-        W = L.groups(total, launched, start)
+            tiles = [min(tile, t * per - r) for r in range(0, t * per, tile)]
+            weights = [L.weight(r, tile, heavy, light) for r in tiles]
+            assert weights == [heavy if r > tile // 2 else light for r in tiles] and L.head(t * per, tile, heavy, light) == sum(weights)
+            assert heavy in weights[:-1] or len(weights) < 2
+            for _ in range(heads):
+                for w in weights:
+                    items.append((total, u, w))
+                    total += w * (u + start)
+        W = L.groups(total, launched, start, heavy)
         assert 0 <= W <= launched and (W > 0) == (total > 0)
         if not total:
             continue
         done, records = {}, {}
         starts = [L.begin(w, total, W) for w in range(W + 1)]
         assert starts[0] == 0 and starts[-1] == total
-        by_start = {s: (k, u) for k, (s, u) in enumerate(items)}
-        order = sorted(by_start)
         at = 0
         for w in range(W):
-            unit, end = starts[w], starts[w + 1]
-            assert end - unit >= start + 2 or W == 1
-            assert L.owner(unit, total, W) == w and L.owner(end - 1, total, W) == w
-            while at + 1 < len(order) and order[at + 1] <= unit:
+            place, end = starts[w], starts[w + 1]
+            assert end - place >= heavy * (start + 2) or W == 1
+            assert L.owner(place, total, W) == w and L.owner(end - 1, total, W) == w
+            while at + 1 < len(items) and items[at + 1][0] <= place:
                 at += 1
-            k, first_item = at, True
-            while unit < end and k < len(order):
-                s = order[k]
-                item, u = by_start[s]
-                if end - s <= start:
+            for k in range(at, len(items)):
+                s, u, weight = items[k]
+                u0, u1 = L.before(place - s, weight, start, u), L.before(end - s, weight, start, u)
+                if s >= end or u1 == 0:
                     break
-                u0 = 0 if unit - s <= start else unit - s - start
-                u1 = end - s - start if end - s < u + start else u
                 assert 0 <= u0 < u1 <= u
-                if first_item:
-                    records[w] = (item, L.first(s, total, W, start), L.owner(s + u + start - 1, total, W), u0 > 0)
-                first_item = False
-                done.setdefault(item, []).append((u0, u1, w))
-                unit = s + start + u1
-                k += 1
+                if w not in records:
+                    records[w] = (k, L.first(s, total, W, start, weight), L.owner(s + weight * (u + start) - 1, total, W), u0 > 0)
+                done.setdefault(k, []).append((u0, u1, w))
+                if u1 < u:
+                    break
+                place = s + weight * (u + start)
+                if place >= end:
+                    break
             assert w in records                                # (every share leaves its record)
         assert len(done) == len(items)
-        for item, (s, u) in enumerate(items):
-            parts = done[item]
+        for k, (s, u, weight) in enumerate(items):
+            parts = done[k]
             assert [p[0] for p in parts] == [0] + [p[1] for p in parts[:-1]] and parts[-1][1] == u
             if len(parts) > 1:                                 # joined by the second share's record, from all of the shares
                 ws = [p[2] for p in parts]
                 assert ws == list(range(ws[0], ws[-1] + 1))
                 for w in ws[1:]:
-                    assert records[w] == (item, ws[0], ws[-1], True)
-        for w, (item, a, b, cut) in records.items():
+                    assert records[w] == (k, ws[0], ws[-1], True)
+        for w, (k, a, b, cut) in records.items():
             if not cut:                                        # nothing to join by this one
-                assert done[item][0][2] == w
-
-
-def test_rows_of_tiles():
-    L = serveplan.lib()
-    for rows in list(range(1, 700)) + [7168, 65535]:
-        for tile in (32, 64, 128, 256):
-            tiles = -(-rows // tile)
-            each = L.tile_rows(rows, tiles)
-            assert each % 32 == 0 and each <= tile and each * tiles >= rows
-            assert (tiles - 1) * each < rows                   # no tile without a row
+                assert done[k][0][2] == w
 
 
 def test_bad_pages_and_lengths_are_replaced():
