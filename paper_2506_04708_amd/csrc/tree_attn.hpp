@@ -134,8 +134,8 @@ struct AttnShape {
     static constexpr int KT = 32 * WK * SUB;           // keys of a stage
     static constexpr bool ALONE = WR == 1;             // every wave loads the keys that it alone uses
     static constexpr int NBUF = ALONE ? 2 : 4;         // stages in LDS: two on their way, one in work, one whose values are still read
-    // units that the beginning of an item costs, see attn_plan.hpp (half and twice as many: 216 and 233 us instead of 214 for 128
-    // trees of 128 nodes with heads of 64, 178 and 175 instead of 173 for 32 trees of 64 with heads of 128)
+    // units that the beginning of an item costs, see attn_plan.hpp (128 trees of 128 nodes with heads of 64: 169 us, with 6 170, with 12
+    // 173; 32 trees of 64 with heads of 128: 132 us, with 2 138, with 6 133, with 8 135)
     static constexpr int START = ALONE ? 2 : D == 64 ? 8 : 4;
     // cost of a unit whose waves of rows share the SIMDs, and of one with a wave each, which its keys' way into LDS bounds (336 rows
     // of 32 trees, a tile of 256 and one of 80: 133 us; by 2 : 1 142, 5 : 4 136, two tiles of 168 rows 141)

@@ -173,7 +173,8 @@ def test_two_captured_loops_at_once(binding):
 
 # ---- every form of the attention kernel ---------------------------------------------------------------------------------
 
-FORMS = [(1, 1, 1), (16, 2, 1), (32, 2, 1), (33, 1, 1), (64, 1, 1), (64, 2, 1), (33, 7, 1), (130, 4, 2), (64, 8, 2)]   # N, heads, kv heads
+FORMS = [(1, 1, 1), (16, 2, 1), (32, 2, 1), (33, 1, 1), (64, 1, 1), (64, 2, 1), (33, 7, 1), (130, 4, 2), (64, 8, 2),   # N, heads, kv heads
+         (130, 3, 1), (130, 4, 1)]                  # a full tile and a small one, a full one and most of one
 
 
 @pytest.mark.parametrize("d,dtype", [(64, BF), (64, HF), (128, BF), (128, HF)])
