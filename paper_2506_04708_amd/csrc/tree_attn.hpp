@@ -143,18 +143,17 @@ struct AttnShape {
     static constexpr int ROW = 2 * D;                  // bytes of a key
     static constexpr int CPR = D / 8;                  // 16-byte chunks of a key
     static constexpr int KPI = 64 / CPR;               // keys of one copy instruction
-    static constexpr int LOADERS = ALONE ? WAVES : WAVES >= 8 && KT / KPI >= 8 ? 8 : 4;  // waves that load (WAVES >= 4)
-    static constexpr int KW = KT / LOADERS;            // keys that each of them loads per stage
+    static constexpr int KW = KT / WAVES;              // keys that a wave loads per stage
     static constexpr int COPIES = 2 * KW / KPI;
     static constexpr int STAGE = 2 * KT * ROW;
     static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
-    static constexpr int IDS = NBUF * STAGE > SUMS ? NBUF * STAGE : SUMS;  // LDS: stages (unit sums before them) | page ids [4][LOADERS][64] | node list | scratch
-    static constexpr int LIST = IDS + 4 * LOADERS * 256;
+    // LDS: stages (unit sums before them) | page numbers or ancestors, [8 stages][WAVES][64] | node list | values that are not finite
+    static constexpr int IDS = NBUF * STAGE > SUMS ? NBUF * STAGE : SUMS;
+    static constexpr int LIST = IDS + 8 * WAVES * 256;
     static constexpr int MISC = LIST + 2048;
-    static constexpr int BYTES = MISC + 256;
+    static constexpr int BYTES = MISC + WAVES * 128;
     static_assert(KW % KPI == 0 && KW >= KPI && KW <= 64, "a copy instruction brings whole keys of one wave");
     static_assert(SUB == 1 || SUB == 2, "a step reads the keys of the other one of two subtiles ahead");
-    static_assert(!ALONE || LOADERS == WAVES, "every wave loads for itself");
     static_assert((WK - 1) * TM * (D + 2) * 4 <= NBUF * STAGE, "parts of the key waves are joined in the stages' memory");
     // 16-byte chunk c of key k stands at chunk c ^ swizzle(k): reads of one chunk of 16 keys (K) and of four chunks of four
     // keys (V) touch every bank once
@@ -342,16 +341,23 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         const uint32_t pool_page = (uint32_t)(a.pool_page / 8), pool_slot = (uint32_t)(a.pool_slot / 8);
         const int pages = a.pages, page_shift = a.page_shift;
         const int share = wave * S::KW;                         // this wave's keys of a stage (ALONE: those it uses)
+        // page numbers of a stage's keys; of the tree's stages the words of this wave's rows' ancestors
         auto load_ids = [&](int i) {
-            int key = (u0 + i) * KT + share + lane % S::KW;
-            key = key < len ? key : len - 1;
-            key = key > 0 ? key : 0;
-            copy4_async(table + (key >> page_shift), __builtin_amdgcn_readfirstlane(lds0 + S::IDS + wave * 256 + (i & 3) * (S::LOADERS * 256)));
+            const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + S::IDS + wave * 256 + (i & 7) * (S::WAVES * 256));
+            if (i < cached) {
+                int key = (u0 + i) * KT + share + lane % S::KW;
+                key = key < len ? key : len - 1;
+                copy4_async(table + (key >> page_shift), to);
+            } else {
+                const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
+                const int v = (i - cached) * KT + (wk * SUB + half % SUB) * 32;
+                copy4_async(a.anc + (long long)node * a.anc_words + (v < a.N ? v / 32 : 0), to);
+            }
         };
         constexpr int LOADS = S::KW / S::KPI;
         auto load_cached = [&](int i) {
             const uint32_t buf = lds0 + (i % S::NBUF) * S::STAGE + share * S::ROW;
-            const int32_t *id = (const int32_t *)(attn_lds + S::IDS + (i & 3) * (S::LOADERS * 256) + wave * 256);
+            const int32_t *id = (const int32_t *)(attn_lds + S::IDS + (i & 7) * (S::WAVES * 256) + wave * 256);
             const int ch = lane % S::CPR;
             int page[LOADS];
 #pragma unroll
@@ -537,8 +543,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         };
         using Yes = std::true_type;
         using No = std::false_type;
-        const bool loads = wave < S::LOADERS;
-        if (loads) { load_ids(0); load_ids(1); load_ids(2); }
+        load_ids(0); load_ids(1); load_ids(2);
         {
             const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2] + 8 * half;
 #pragma unroll
@@ -548,45 +553,43 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             for (int i = 0; i < DC; ++i) asm volatile("" : "+v"(q[i]));
         }
         wait_loads<0>();
-        if (loads) {
-            load_stage(0);
-            if (n > 1) { load_ids(3); load_stage(1); }
-        }
-        uint32_t *wild = (uint32_t *)(attn_lds + S::MISC);      // [N / 32]: nodes with a value that is no finite number
-        if (threadIdx.x < 32) wild[threadIdx.x] = 0;
+        load_stage(0);
+        if (n > 1) { load_ids(3); load_stage(1); }
+        uint32_t *wild = (uint32_t *)(attn_lds + S::MISC);      // [WAVES][32]: nodes with a value that is no finite number, found by a wave
+        if (lane < 32) wild[wave * 32 + lane] = 0;
         // A unit that has come: everyone's copies are there, two units ahead are on their way, the tree's values are finite.
         // -> the keys of this wave's subtile t that count for this lane's query: bits, `all` of them.
         auto arrive = [&](int i) {
             if (i + 1 < n) wait_loads<S::COPIES + 1>();         // (the unit's own copies are all older than the newest that many)
             else wait_loads<0>();
+            if (i >= cached) {
+                // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
+                // zeros here, by the wave that loaded them, and the rows that see them get them added below.
+                const uint32_t at = lds0 + (i % S::NBUF) * S::STAGE + KT * S::ROW + share * S::ROW;
+                const int n_nodes = fresh_args<TreeAttnArgs>().N;
+                for (int x = lane; x < S::KW * S::CPR; x += 64) {
+                    lds_uint4v *vp = (lds_uint4v *)(uintptr_t)(at + x * 16);
+                    uint4v vw = *vp;
+                    constexpr uint32_t kExp = S::F16 ? 0x7C00u : 0x7F80u;
+                    bool found = false;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool lo = (vw[e] & kExp) == kExp, hi = ((vw[e] >> 16) & kExp) == kExp;
+                        found |= lo | hi;
+                        vw[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+                    }
+                    if (found) {
+                        *vp = vw;
+                        const int v = (i - cached) * KT + share + x / S::CPR;
+                        if (v < n_nodes) atomicOr(&wild[wave * 32 + v / 32], 1u << (v & 31));
+                    }
+                }
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            }
             if constexpr (!S::ALONE) {
                 group_barrier();                                // ... and everyone is done with the unit two before
-                if (loads && i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
+                if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
-            if (i < cached) return;
-            // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
-            // zeros here, and the rows that see them get them added below.
-            const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
-            const uint32_t off = (i % S::NBUF) * S::STAGE;
-            __syncthreads();
-            for (int x = threadIdx.x; x < KT * S::CPR; x += S::THREADS) {
-                lds_uint4v *vp = (lds_uint4v *)(uintptr_t)(lds0 + off + KT * S::ROW + x * 16);
-                uint4v vw = *vp;
-                constexpr uint32_t kExp = S::F16 ? 0x7C00u : 0x7F80u;
-                bool found = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const bool lo = (vw[e] & kExp) == kExp, hi = ((vw[e] >> 16) & kExp) == kExp;
-                    found |= lo | hi;
-                    vw[e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
-                }
-                if (found) {
-                    *vp = vw;
-                    const int v = (i - cached) * KT + x / S::CPR;
-                    if (v < a.N) atomicOr(&wild[v / 32], 1u << (v & 31));
-                }
-            }
-            __syncthreads();
         };
         auto counting = [&](int i, int t, bool &all) {
             const int first = wk * SUB * 32 + t * 32;           // the subtile's first key in the unit
@@ -598,9 +601,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             }
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
             const int v = (i - cached) * KT + first;            // a node sees its ancestors and itself
-            uint32_t word = busy && v < a.N ? a.anc[(long long)node * a.anc_words + v / 32] : 0u;
-            asm volatile("" : "+v"(word));                      // (waited for here: elsewhere it would be a wait for the copies too)
-            return word;
+            const uint32_t word = ((const uint32_t *)(attn_lds + S::IDS + (i & 7) * (S::WAVES * 256) + wave * 256))[t * 32 + col];
+            return busy && v < a.N ? word : 0u;
         };
         if constexpr (S::ALONE) {
             for (int i = 0; i < n; ++i) {
@@ -632,7 +634,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                     const int i = first + x;
                     wait_loads<S::COPIES + 1>();
                     group_barrier();
-                    if (loads) { load_ids(i + 4); load_cached(i + 2); }
+                    load_ids(i + 4);
+                    load_cached(i + 2);
                     const uint32_t off = (i % S::NBUF) * S::STAGE;
                     if (busy) {
 #pragma unroll
@@ -667,7 +670,11 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
             for (int x = 0; x < (a.N + 31) / 32; ++x) {
                 if (x % (KT / 32) / SUB != wk) continue;
-                for (uint32_t bits = wild[x]; bits; bits &= bits - 1) {
+                uint32_t bits = wild[wave * 32 + x];
+                if constexpr (!S::ALONE)                        // (who alone uses its keys has found all there is in them)
+#pragma unroll
+                    for (int y = 0; y < S::WAVES; ++y) bits |= wild[y * 32 + x];
+                for (; bits; bits &= bits - 1) {
                     // an infinity or NaN reaches the rows that see its node, whatever its weight
                     const int v = 32 * x + __builtin_ctz(bits);
                     const bool sees = (a.anc[(long long)node * a.anc_words + x] >> (v & 31)) & 1u;

@@ -204,6 +204,13 @@ def test_forms_with_values_that_are_not_finite(binding, N, H, G, d, dtype):
     assert not bool(torch.isfinite(got[0, drafted][:, :per, 5]).any())
     got[0, :, :per, 5] = clean[0, :, :per, 5]
     assert bool(((got - clean).abs() <= tol).all())
+    leaf = max(u for u in range(N) if t.tok[1, u] >= 0)      # nobody sees it but itself
+    t.v[1, leaf, 0, 7], t.v[1, leaf, G - 1, 9] = float("-inf"), float("nan")
+    got = t.h.tree_attention(**t.on_gpu()).cpu().double()
+    assert not bool(torch.isfinite(got[1, leaf, :per, 7]).any()) and bool(torch.isnan(got[1, leaf, (G - 1) * per:, 9]).all())
+    got[0, :, :per, 5], got[1, leaf, :per, 7], got[1, leaf, (G - 1) * per:, 9] = (
+        clean[0, :, :per, 5], clean[1, leaf, :per, 7], clean[1, leaf, (G - 1) * per:, 9])
+    assert bool(((got - clean).abs() <= tol).all())
 
 
 def test_attention_of_nothing_drafted(binding):
