@@ -15,6 +15,11 @@
 namespace stand {
 
 constexpr int kAttnMaxBatch = 4096;   // trajectories of a call: their unit sums are made in LDS
+// a / b of numbers that are not negative.  (A division of 64 bits costs the GPU half a microsecond, and these mostly fit 32.)
+STAND_BOTH long long quotient(long long a, long long b)
+{
+    return (unsigned long long)(a | b) >> 32 ? a / b : (long long)((unsigned)a / (unsigned)b);
+}
 STAND_BOTH long long clamp_length(long long len, long long most) { return len < 0 ? 0 : (len > most ? most : len); }
 STAND_BOTH int clamp_page(int page, int pages) { return page < 0 ? 0 : (page >= pages ? pages - 1 : page); }
 
@@ -38,18 +43,19 @@ STAND_BOTH long long head_weight(int rows, int tile_rows, int heavy, int light)
 // Units of an item that lie before a place of the work, places counted from the item's beginning.
 STAND_BOTH long long units_before(long long place, int weight, int start, long long units)
 {
-    const long long u = place / weight - start;
+    if (place < 0) return 0;
+    const long long u = quotient(place, weight) - start;
     return u < 0 ? 0 : (u > units ? units : u);
 }
 // Workgroups that get a share, of `groups` launched: no share is shorter than start + 2 units of the heaviest kind.
 STAND_BOTH long long attn_groups(long long total, int groups, int start, int heavy)
 {
-    const long long w = total / (heavy * (start + 2));
+    const long long w = quotient(total, heavy * (start + 2));
     return w >= groups ? groups : w > 0 ? w : total > 0;
 }
-STAND_BOTH long long group_start(long long w, long long total, long long W) { return w * total / W; }
+STAND_BOTH long long group_start(long long w, long long total, long long W) { return quotient(w * total, W); }
 // The last workgroup whose share would begin at or before a place.
-STAND_BOTH long long group_of(long long place, long long total, long long W) { return ((place + 1) * W - 1) / total; }
+STAND_BOTH long long group_of(long long place, long long total, long long W) { return quotient((place + 1) * W - 1, total); }
 // The workgroup that has an item's first part.
 STAND_BOTH long long first_group(long long item_start, long long total, long long W, int start, int weight)
 {

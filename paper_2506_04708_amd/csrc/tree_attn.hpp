@@ -163,40 +163,51 @@ struct AttnShape {
 
 // Units of work before each trajectory, prefix[0 .. B], in LDS: a unit is a stage of KT keys for one tile of rows and one
 // key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) + ceil(N / KT) units.
-// Every workgroup counts all drafted nodes for itself, eight reads in flight (one after the other they took 17 us for 128 trees
-// of 128 nodes).
+// Every workgroup counts all drafted nodes for itself, up to 16 reads of a wave in flight.
 template <typename S>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
 {
     constexpr int THREADS = S::THREADS;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int first_len = a.len[lane < a.B ? lane : 0];    // (asked for before it is needed)
-    for (int b = threadIdx.x; b <= a.B; b += THREADS) prefix[b] = 0;
-    __syncthreads();
-    int p2 = 1;
-    while (p2 < a.N && p2 < 64) p2 <<= 1;
-    // a wave counts 64 / p2 trajectories at once, or 64 nodes of one
-    const int at_once = 64 / p2, per_b = (a.N + 63) / 64, rounds = (a.B + at_once - 1) / at_once * per_b;
-    const int turn = (int)(blockIdx.x * 5u % (unsigned)rounds);   // (not all of them the same line of the L2 at one time)
-    for (int i0 = wave; i0 < rounds; i0 += THREADS / 64 * 8) {
-        int tok[8];
+    if (threadIdx.x == 0) prefix[0] = 0;
+    int lg = 0;
+    while (1 << lg < a.N && lg < 6) ++lg;
+    // a wave counts 64 >> lg trajectories at once, or 64 nodes of one after the other
+    const int sub = lane & ((1 << lg) - 1), turns = (a.B + (64 >> lg) - 1) >> (6 - lg);
+    const int ahead = (int)(blockIdx.x * 5u % (unsigned)turns);   // (not all of them the same line of the L2 at one time)
+    constexpr int WAVES = THREADS / 64;
+    auto count = [&](auto at_a_time) {
+        constexpr int K = decltype(at_a_time)::value;
+        for (int x0 = wave; x0 < turns; x0 += WAVES * K) {
+            int n[K] = {}, b[K];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int x = i0 + k * (THREADS / 64), i = x + turn < rounds ? x + turn : x + turn - rounds;
-            const int b = i / per_b * at_once + lane / p2, u = i % per_b * 64 + lane % p2;
-            const bool there = x < rounds && b < a.B && u < a.N;
-            const int v = a.draft_tok[there ? (long long)b * a.N + u : 0];   // (read by all: a branch would wait for each)
-            tok[k] = there ? v : -1;
-        }
+            for (int k = 0; k < K; ++k) {
+                const int x = x0 + k * WAVES, g = x + ahead < turns ? x + ahead : x + ahead - turns;
+                b[k] = x < turns ? (g << (6 - lg)) + (lane >> lg) : a.B;
+            }
+            for (int u = sub; u - sub < a.N; u += 64) {
+                int tok[K];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) {
-            const int x = i0 + k * (THREADS / 64), i = x + turn < rounds ? x + turn : x + turn - rounds;
-            const int b = i / per_b * at_once + lane / p2;
-            const unsigned long long bits = __ballot(tok[k] >= 0) >> (lane & ~(p2 - 1));
-            const int count = __popcll(p2 == 64 ? bits : bits & ((1ull << p2) - 1));
-            if (x < rounds && count && lane % p2 == 0) atomicAdd((unsigned long long *)&prefix[b + 1], (unsigned long long)count);
+                for (int k = 0; k < K; ++k) {
+                    const bool there = b[k] < a.B && u < a.N;
+                    const int v = a.draft_tok[there ? b[k] * a.N + u : 0];   // (read by all: a branch would wait for each)
+                    tok[k] = there ? v : -1;
+                }
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    const unsigned long long bits = __ballot(tok[k] >= 0) >> (lane - sub);
+                    n[k] += __popcll(lg == 6 ? bits : bits & ((1ull << (1 << lg)) - 1));
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < K; ++k)
+                if (sub == 0 && b[k] < a.B) prefix[b[k] + 1] = n[k];
         }
-    }
+    };
+    if (turns <= WAVES) count(std::integral_constant<int, 1>{});
+    else if (turns <= 8 * WAVES) count(std::integral_constant<int, 8>{});
+    else count(std::integral_constant<int, 16>{});
     __syncthreads();
     if (wave == 0) {
         long long base = 0;
@@ -221,13 +232,14 @@ template <typename S>
 __device__ __forceinline__ void zero_rows(const TreeAttnArgs &a)
 {
     const int lane = threadIdx.x & 63;
-    const long long all = (long long)a.B * a.N, r0 = all * blockIdx.x / a.groups, r1 = all * (blockIdx.x + 1) / a.groups;
-    for (long long x = r0; x < r1; x += 64) {
+    const unsigned all = a.B * a.N, each = (all + a.groups - 1) / a.groups, r0 = min(all, blockIdx.x * each), r1 = min(all, r0 + each);
+    for (unsigned x = r0; x < r1; x += 64) {
         unsigned long long gone = __ballot(x + lane < r1 && a.draft_tok[x + lane < r1 ? x + lane : r0] < 0);
         for (; gone; gone &= gone - 1) {
-            const long long r = x + __builtin_ctzll(gone);
+            const unsigned r = x + __builtin_ctzll(gone), b = r / (unsigned)a.N;
+            uint16_t *row = a.out + b * a.os[0] + (r - b * a.N) * a.os[1];
             for (int i = threadIdx.x; i < a.kv_heads * a.per_kv * S::CPR; i += S::THREADS)
-                *(uint4v *)(a.out + (r / a.N) * a.os[0] + (r % a.N) * a.os[1] + (i / S::CPR) * a.os[2] + i % S::CPR * 8) = uint4v{0, 0, 0, 0};
+                *(uint4v *)(row + (i / S::CPR) * a.os[2] + i % S::CPR * 8) = uint4v{0, 0, 0, 0};
         }
     }
 }
@@ -281,12 +293,18 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         uint16_t *list = (uint16_t *)(attn_lds + S::LIST);
         if (listed != b) {
             int base = 0;
-            for (int u0 = 0; u0 < a.N; u0 += 64) {
-                const int u = u0 + lane;
-                const bool there = u < a.N && a.draft_tok[(long long)b * a.N + u] >= 0;
-                const unsigned long long bits = __ballot(there);
-                if (wave == 0 && there) list[base + __popcll(bits & ((1ull << lane) - 1))] = (uint16_t)u;
-                base += __popcll(bits);
+            for (int u0 = 0; u0 < a.N; u0 += 256) {
+                int tok[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) tok[k] = a.draft_tok[b * a.N + min(u0 + 64 * k + lane, a.N - 1)];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int u = u0 + 64 * k + lane;
+                    const bool there = u < a.N && tok[k] >= 0;
+                    const unsigned long long bits = __ballot(there);
+                    if (wave == 0 && there) list[base + __popcll(bits & ((1ull << lane) - 1))] = (uint16_t)u;
+                    base += __popcll(bits);
+                }
             }
             nodes = __builtin_amdgcn_readfirstlane(base);
             listed = b;
@@ -298,9 +316,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         const int units = (int)item_units(len, most, a.N, KT), cache_units = (len + KT - 1) / KT, per_item = units + S::START;
         const int all_rows = nodes * a.per_kv, full = all_rows / TM;
         const long long per_head = per_item * head_weight(all_rows, TM, S::HEAVY, S::LIGHT);
-        const int heads_before = (int)((unit - b_start) / per_head);
+        const int heads_before = (int)quotient(unit - b_start, per_head);
         const long long head_start = b_start + heads_before * per_head;
-        const int tile = min((int)((unit - head_start) / (S::HEAVY * per_item)), full);
+        const int tile = min((int)quotient(unit - head_start, S::HEAVY * per_item), full);
         const int row0 = tile * TM, rows = min(all_rows, row0 + TM), weight = tile_weight(rows - row0, TM, S::HEAVY, S::LIGHT);
         // (trajectories begin with different heads: at one time the same head of all of them would use a part of the memory
         // channels, where a token's heads stand side by side)
