@@ -17,14 +17,15 @@
 // both products read without bank conflicts.  Four stages of memory: two on their way, one in work, one whose values are
 // still read.
 //
-// Work: trajectories differ in length a hundredfold, so tiles are cut by units of a stage, equal shares for every workgroup the
-// chip holds (attn_plan.hpp); items that were cut are joined by a second kernel.  No atomics: the same call gives the same bits.
+// Work: trajectories differ in length a hundredfold, so tiles are cut by units of a stage, equal shares (by the units' costs) for
+// every workgroup the chip holds (attn_plan.hpp); items that were cut are joined by a second kernel.  No sum is made by atomics:
+// the same call gives the same bits.
 //
-// Bound: decoding by HBM (2.04 GB of cache in 353 us, 5.8 TB/s; a torch copy reaches 4.9 counting both ways); larger trees by
+// Bound: decoding by HBM (2.04 GB of cache in 346 us, 5.9 TB/s; a torch copy reaches 4.9 counting both ways); larger trees by
 // what a wave issues between its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128:
-// 125 us for 70 GFLOP, 565 TFLOP/s on rows as they are, where a large matrix product reaches 1211); alone on a SIMD a step of 32
+// 131 us for 70 GFLOP, 540 TFLOP/s on rows as they are, where a large matrix product reaches 1211); alone on a SIMD a step of 32
 // keys takes a wave 404 ns, of which its 16 matrix instructions are 262.  Short calls are bound by the chain lengths -> shares ->
-// nodes -> page numbers -> keys, each a trip to memory: 11.5 us, and 3.8 us for the join.
+// nodes -> page numbers -> keys, each a trip to memory: 10.1 us, and 2.3 us for the join.
 #pragma once
 #include "attn_plan.hpp"
 #include "wave_ops.hpp"
@@ -163,7 +164,7 @@ struct AttnShape {
 
 // Units of work before each trajectory, prefix[0 .. B], in LDS: a unit is a stage of KT keys for one tile of rows and one
 // key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) + ceil(N / KT) units.
-// Every workgroup counts all drafted nodes for itself, up to 16 reads of a wave in flight.
+// Every workgroup counts all drafted nodes for itself, up to 16 reads of a wave in flight (128 trees of 128 nodes: 7 us).
 template <typename S>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
 {
@@ -779,7 +780,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 // Rows of items that several workgroups took: their parts joined (weights 2^(m - largest m)), 32 rows (those of one wave) by a workgroup and in the layout of
 // a wave's registers: lane l has the row l % 32 and every second group of four elements.  The workgroups of the item's second
 // share take a quarter of the elements with each wave; where there are many parts, those of eight shares take an eighth each and
-// their waves the parts in turn.  Bound by the trip record -> place -> parts: 3.8 us for a short tree, 13.5 us for the 17 MB of
+// their waves the parts in turn.  Bound by the trip record -> place -> parts: 2.3 us for a short tree, 14 us for the 17 MB of
 // parts of 32 trees of 64 nodes (256 workgroups' shares, each up to two parts of 256 rows).
 constexpr int kJoinShared = 8;        // more parts: shared
 template <int D, int TM, bool F16>
