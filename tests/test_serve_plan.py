@@ -52,7 +52,7 @@ def test_shares_cover_every_unit_once(kind, tile, keys, start, heavy, light):
         at = 0
         for w in range(W):
             place, end = starts[w], starts[w + 1]
-            assert end - place >= heavy * (start + 2) or W == 1
+            assert end - place >= heavy * (start + 1) or W == 1
             assert L.owner(place, total, W) == w and L.owner(end - 1, total, W) == w
             while at + 1 < len(items) and items[at + 1][0] <= place:
                 at += 1
