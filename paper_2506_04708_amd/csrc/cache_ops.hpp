@@ -5,6 +5,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "commit_plan.hpp"
+
 namespace stand {
 
 // ---- rows into the cache ------------------------------------------------------------------------------------------------
@@ -21,27 +23,28 @@ struct CommitArgs {
     long long pool_layer, pool_page, pool_slot, pool_head;
     long long slot_count;
     int B, rows, width, page_shift, heads, words;           // words: 16-byte words of one head's row
-    int per_group;              // positions a workgroup copies
+    int per_group;              // positions a workgroup copies at a time
 };
 
-__global__ __launch_bounds__(256) void cache_commit_kernel(CommitArgs a)
+__global__ __launch_bounds__(kCommitThreads) void cache_commit_kernel(CommitArgs a)
 {
     const int b = blockIdx.y, layer = blockIdx.z;
-    int n = a.count ? a.count[b] : a.width;
-    n = n < a.width ? n : a.width;
-    const int j0 = blockIdx.x * a.per_group, j1 = min(n, j0 + a.per_group);
+    const int n = commit_positions(a.count ? a.count[b] : a.width, a.width);
     const int row_words = a.heads * a.words;
-    for (int i = threadIdx.x; i < (j1 - j0) * row_words; i += 256) {
-        const int j = j0 + i / row_words, w = i % row_words;
-        const int head = w / a.words, e = w % a.words;
-        const long long slot = a.slots[(long long)b * a.width + j];
-        const int r = a.row ? a.row[(long long)b * a.width + j] : j;
-        if (slot < 0 || slot >= a.slot_count || r < 0 || r >= a.rows) continue;
-        const long long src = layer * a.src_layer + b * a.src_batch + r * a.src_row + head * a.src_head + e;
-        const long long dst = layer * a.pool_layer + (slot >> a.page_shift) * a.pool_page +
-                              (slot & ((1ll << a.page_shift) - 1)) * a.pool_slot + head * a.pool_head + e;
-        a.k_pool[dst] = a.k_rows[src];
-        a.v_pool[dst] = a.v_rows[src];
+    for (unsigned j0 = blockIdx.x * (unsigned)a.per_group; j0 < (unsigned)n; j0 += gridDim.x * (unsigned)a.per_group) {
+        const int words = commit_words(n, j0, a.per_group, row_words);
+        for (int i = threadIdx.x; i < words; i += kCommitThreads) {
+            const int j = (int)j0 + i / row_words, w = i % row_words;
+            const int head = w / a.words, e = w % a.words;
+            const long long slot = a.slots[(long long)b * a.width + j];
+            const int r = a.row ? a.row[(long long)b * a.width + j] : j;
+            if (slot < 0 || slot >= a.slot_count || r < 0 || r >= a.rows) continue;
+            const long long src = layer * a.src_layer + b * a.src_batch + r * a.src_row + head * a.src_head + e;
+            const long long dst = layer * a.pool_layer + (slot >> a.page_shift) * a.pool_page +
+                                  (slot & ((1ll << a.page_shift) - 1)) * a.pool_slot + head * a.pool_head + e;
+            a.k_pool[dst] = a.k_rows[src];
+            a.v_pool[dst] = a.v_rows[src];
+        }
     }
 }
 

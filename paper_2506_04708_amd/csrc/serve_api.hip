@@ -165,10 +165,8 @@ extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, con
     CommitArgs a;
     a.words = cache->head_dim / 8;
     a.heads = cache->kv_heads;
-    // a workgroup copies at least four words a thread, where there are as many
-    const int row_words = a.heads * a.words;
-    a.per_group = (1024 + row_words - 1) / row_words;
-    const int64_t groups = (width + (int64_t)a.per_group - 1) / a.per_group;
+    a.per_group = commit_per_group(a.heads * a.words);
+    const int64_t groups = commit_groups(width, a.per_group);
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
     a.k_rows = (const uint4 *)rows->d_k; a.v_rows = (const uint4 *)rows->d_v;
@@ -180,7 +178,7 @@ extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, con
     a.page_shift = log2_of(cache->page_size);
     a.slot_count = (long long)cache->pages << a.page_shift;
     a.B = v.B; a.rows = rows->rows; a.width = width;
-    cache_commit_kernel<<<dim3((unsigned)groups, (unsigned)v.B, (unsigned)cache->layers), dim3(256), 0, (hipStream_t)stream>>>(a);
+    cache_commit_kernel<<<dim3((unsigned)groups, (unsigned)v.B, (unsigned)cache->layers), dim3(kCommitThreads), 0, (hipStream_t)stream>>>(a);
     return launched(v);
 }
 

@@ -1,0 +1,46 @@
+"""The host side of the operators around a verification, without a GPU: how a commit's positions are shared out."""
+import ctypes as C
+
+import pytest
+
+from tests import servehost
+
+I, U, L, P = C.c_int, C.c_uint, C.c_int64, C.c_void_p
+
+
+@pytest.fixture(scope="module")
+def commit():
+    return servehost.build("""
+#include "commit_plan.hpp"
+using namespace stand;
+extern "C" {
+int per_group(int row_words) { return commit_per_group(row_words); }
+int64_t groups(int width, int per) { return commit_groups(width, per); }
+int positions(int count, int width) { return commit_positions(count, width); }
+int words(int n, unsigned j0, int per, int row_words) { return commit_words(n, j0, per, row_words); }
+}""", dict(per_group=([I], I), groups=([I, I], L), positions=([I, I], I), words=([I, U, I, I], I)))
+
+
+# kv heads * 16-byte words of a head's row: the smallest, ordinary ones, the largest that a cache may have
+ROW_WORDS = [8, 16, 24, 64, 128, 512, 1024, 1040, 65536]
+
+
+@pytest.mark.parametrize("row_words", ROW_WORDS)
+def test_a_commit_copies_what_was_counted_and_nothing_else(commit, row_words):
+    """At every position where a 32-bit product of positions and words could wrap, for every count."""
+    per = commit.per_group(row_words)
+    assert per >= 1 and (per == 1 or (per - 1) * row_words < 1024)
+    wraps = [k * 2 ** 31 // row_words + e for k in (1, 2, 3) for e in (-per, -1, 0, 1, per)]
+    for width in [1, 2, per, per + 1, 4099, 2 ** 24 + 5, 2 ** 30]:
+        for count in [-2 ** 31, -2 ** 31 + 1, -1, 0, 1, per, 7, width - 1, width, width + 1, 2 ** 31 - 1]:
+            n = commit.positions(count, width)
+            assert n == min(max(count, 0), width)
+            step = commit.groups(width, per) * per
+            assert 1 <= commit.groups(width, per) < 2 ** 32 / 256        # threads of a launch's dimension
+            last = (width - 1) // per * per
+            for j0 in {0, per, last} | {x // per * per for x in wraps + [n - 1, n, n + per]}:
+                if not 0 <= j0 <= last:
+                    continue
+                assert commit.words(n, j0, per, row_words) == min(max(n - j0, 0), per) * row_words, (width, count, j0)
+            # a workgroup's next position: behind the last one it is past the end of every row, in 32 bits without a sign too
+            assert n + step < 2 ** 32 and (step >= width or commit.groups(width, per) == (2 ** 32 - 1) // 256)
