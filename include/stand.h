@@ -404,7 +404,7 @@ typedef struct {
     const void *d_q, *d_k, *d_v; /* [B][N][q_heads | kv_heads | kv_heads][head_dim] */
     void *d_out;                 /* [B][N][q_heads][head_dim] */
     int32_t q_heads;             /* a multiple of kv_heads; query head i reads head i / (q_heads / kv_heads) */
-    float scale;                 /* of the scores, > 0 (usually head_dim ^ -0.5) */
+    float scale;                 /* of the scores, > 0 and at most 2^127 (usually head_dim ^ -0.5) */
     int64_t q_stride[3], k_stride[3], v_stride[3], out_stride[3];
 } stand_tree_rows;
 
@@ -416,8 +416,9 @@ typedef struct {
  * stand_draft / stand_step gave.  Token t of trajectory b is in page d_table[b][t / page_size], d_table: [B][table_width].
  * A length below 0 counts as 0, one above table_width * page_size (at most STAND_MAX_CACHED) as that; a page outside the cache is never
  * read (what is read instead is not specified).  A tree of one node is the ordinary attention of single tokens.  Where a value
- * that a row sees is infinite or NaN, that element of its output is one of the two (which is not specified); a score that is
- * neither finite nor -infinity makes the row NaN.  A drafted node's ancestors are drafted.
+ * that a row sees is infinite or NaN, that element of its output is one of the two (which is not specified); a product
+ * query . key (summed in fp32, before the scale) that is neither finite nor -infinity makes the row NaN, and so does a row of nothing
+ * but -infinity; finite ones of any size do not.  A drafted node's ancestors are drafted.
  *   Keys (and values) of one layer span less than 64 GiB (STAND_ELIMIT).
  *   Products are summed in fp32, the weights p are rounded to the cache's type for the product with the values (relative error
  * 2^-9 in bf16, 2^-12 in fp16 each, at most half a step) and summed as rounded; the result is rounded once.

@@ -50,7 +50,7 @@ inline int check_tree_attention(int64_t B, const stand_cache *cache, int32_t lay
     if (!strides_ok(rows->q_stride) || !strides_ok(rows->k_stride) || !strides_ok(rows->v_stride) || !strides_ok(rows->out_stride))
         return STAND_EINVAL;
     if (!heads_ok(cache, rows->q_heads)) return STAND_EINVAL;
-    if (!(rows->scale > 0.0f) || !std::isfinite(rows->scale)) return STAND_EINVAL;
+    if (!(rows->scale > 0.0f && rows->scale <= 0x1p127f)) return STAND_EINVAL;   // (its product with log2(e) is a number)
     if ((int64_t)table_width * cache->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
     if (B > kAttnMaxBatch || rows->q_heads > 65535) return STAND_ELIMIT;
     // the kernel counts places of a layer in 16-byte chunks, in 32 bits

@@ -1,11 +1,13 @@
 // tree_attn.hpp -- attention of the nodes of a drafted tree over a paged key/value cache and over their own ancestors.
 //
 // For a row (one node, one query head) and the keys t that it sees, c = scale * log2(e):
-//     out = sum_t w_t value_t / sum_t w_t,    w_t = 2^(c * query . key_t - m)
-// in one pass over the keys with a running m; any m gives the same quotient.  m is raised only where a score passes it by more
+//     out = sum_t w_t value_t / sum_t w_t,    w_t = 2^(c * (s_t - m)),    s_t = query . key_t
+// in one pass over the keys with a running m; any m gives the same quotient.  m is raised only where c * s passes c * m by more
 // than 8: weights are then at most 2^8, sums stay far inside fp32, and the outputs are scaled anew a few times per row instead of
-// at every maximum.  Weights are rounded to the cache's type for the matrix cores and summed as rounded, so that numerator and
-// denominator err together.  Scores, m, sums and outputs are fp32.
+// at every maximum.  The exponent is one fused operation, c * s - (c * m rounded): the rounding is the same for all keys of a row,
+// but where |c * m| passes 2^22 it would be a large number, so such rows take m from their scores first (raise_row).  Weights are
+// rounded to the cache's type for the matrix cores and summed as rounded, so that numerator and denominator err together.  Scores,
+// m, sums and outputs are fp32.
 //
 // Rows: drafted nodes are numbered through (a third of a tree is not drafted, and is not computed), and all query heads of a
 // key/value head share its keys, so a tile has up to 256 rows of (node, head) that read a key once.  A wave has 32 of them.  It
@@ -99,6 +101,46 @@ __device__ __forceinline__ float other_half_sum(float x)
 {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// What a row's weights are made with.  c and rise = 8 / c are the call's.
+struct Exponent { float c, rise; };
+__device__ __forceinline__ Exponent exponent_of(float scale)
+{
+    const float c = scale * 1.4426950408889634f;
+    return Exponent{c, 8.0f / c};
+}
+// weights are at most 2^8 (where the running maximum is left behind); fp16 ones are scaled up so that few are subnormal
+template <bool F16> constexpr float kUp = F16 ? 6.0f : 0.0f;
+constexpr float kFarRow = 4194304.0f;   // 2^22: c * m is rounded by at most a quarter
+constexpr float kLowest = -3.402823466e+38f;
+
+// The running maximum m of a lane's row before the products with the values of the scores s[0 .. NS), whose largest one is `top`:
+// -> the shift of their exponents, c * s + shift.  m is raised, and the sum l and outputs o are scaled, where `top` passes it by more
+// than `rise`; m begins at -infinity.  Rows with |c * m| > 2^22 (nothing but -infinity seen among them) come here with every stage
+// and get differences s - m for scores.  Seldom after the first stages: the old maximum will do.
+template <bool F16, int NS, int DT>
+__device__ __forceinline__ float raise_row(const Exponent &e, float top, float &m, float &l, float16v (&o)[DT], float16v *const (&s)[NS])
+{
+    float shift = fmaf(-m, e.c, kUp<F16>);
+    if (__ballot(top > m + e.rise || fabsf(shift) > kFarRow)) {
+        const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(next > m ? (m - next) * e.c : 0.0f);
+        m = next;
+        l *= f;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[d][x] *= f;
+        shift = fmaf(-m, e.c, kUp<F16>);
+        const bool far = fabsf(shift) > kFarRow;
+        const float from = far && m > -__builtin_huge_valf() ? m : 0.0f;
+        shift = far ? kUp<F16> : shift;
+#pragma unroll
+        for (int k = 0; k < NS; ++k)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) (*s[k])[x] -= from;
+    }
+    return shift;
 }
 
 // Asynchronous copies from global memory to LDS: lane l's 16 (4) bytes go to `to` + 16 l (4 l).  They have no result register;
@@ -281,9 +323,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
     long long b_start = sums[b];
     int listed = -1, nodes = 0;
     bool first_item = true;
-    const float c = a.scale * 1.4426950408889634f;
-    // weights are at most 2^8 (where the running maximum is left behind); fp16 ones are scaled up so that few are subnormal
-    constexpr float kUp = S::F16 ? 6.0f : 0.0f;
+    const Exponent ex = exponent_of(a.scale);
+    const float c = ex.c;
 
     const int B = a.B;
     while (unit < unit_end && b < B) {
@@ -343,7 +384,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         float16v o[DT];
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = float16v{0};
-        float m = -1e38f, l = 0.0f;                    // running maximum (scaled scores, base 2) and sum of the weights
+        float m = -__builtin_huge_valf(), l = 0.0f;    // running maximum of the products with the keys, sum of the weights
 
         // this lane's first fragments inside a stage (chunk 0 of the keys, elements 0 .. 31 of the values); the others differ
         // in address bits that the swizzle only flips
@@ -457,17 +498,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             for (int t = 0; t < SUB; ++t)
 #pragma unroll
                 for (int x = 0; x < 16; ++x) top = fmaxf(top, s[t][x]);
-            top = other_half_max(top) * c;
-            if (__ballot(top > m + 8.0f)) {            // seldom after the first stages: the old maximum will do
-                const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - next);
-                m = next;
-                l *= f;
+            float16v *of[SUB];
 #pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) o[d][x] *= f;
-            }
-            const float shift = kUp - m;
+            for (int t = 0; t < SUB; ++t) of[t] = &s[t];
+            const float shift = raise_row<S::F16>(ex, other_half_max(top), m, l, o, of);
 #pragma unroll
             for (int t = 0; t < SUB; ++t) {
                 uint32_t p[8];
@@ -489,7 +523,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         // are what keeps both units busy.  HAVE: the keys have been read by the step before; NEXT: read those 32 keys further on.
         uint4v kf[DC];
         float top = -__builtin_huge_valf();
-        auto step = [&](auto have, auto next, const float16v &old, float16v &t, uint32_t k_off, uint32_t v_off, bool all, uint32_t word) {
+        auto step = [&](auto have, auto next, float16v &old, float16v &t, uint32_t k_off, uint32_t v_off, bool all, uint32_t word) {
             uint32_t ka = k_at + k_off, va = v_at + v_off;
             asm volatile("" : "+v"(ka), "+v"(va));
             if constexpr (!decltype(have)::value) {
@@ -497,17 +531,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)(ka ^ (x << 5));
                 __builtin_amdgcn_sched_barrier(0);
             }
-            top = other_half_max(top) * c;
-            if (__ballot(top > m + 8.0f)) {            // seldom after the first stages: the old maximum will do
-                const float more = fmaxf(m, top), f = __builtin_amdgcn_exp2f(m - more);
-                m = more;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) o[d][x] *= f;
-            }
-            const float shift = kUp - m;
+            float16v *const of[1] = {&old};
+            const float shift = raise_row<S::F16>(ex, other_half_max(top), m, l, o, of);
             constexpr int PER = 16 / DC;               // weights beside a matrix instruction
             uint4v vf[2 * DT];
             t = float16v{0};
@@ -712,6 +737,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 
         // ---- the key waves' parts joined, then the rows' outputs or this workgroup's part of them ----
         l = other_half_sum(l);
+        m = fmaxf(m, kLowest);                         // (nothing seen: differences of maxima are numbers)
         if constexpr (S::WK > 1) {
             __syncthreads();
             float *join = (float *)attn_lds;           // [WK - 1][WR][16 DT + 2][64]
@@ -728,7 +754,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 float next = m;
 #pragma unroll
                 for (int k = 0; k < S::WK - 1; ++k) next = fmaxf(next, join[(k * S::WR + wr) * (16 * DT + 2) * 64 + lane]);
-                const float f = __builtin_amdgcn_exp2f(m - next);
+                const float f = __builtin_amdgcn_exp2f((m - next) * c);
                 l *= f;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
@@ -737,7 +763,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                 for (int k = 0; k < S::WK - 1; ++k) {
                     const float *from = join + (k * S::WR + wr) * (16 * DT + 2) * 64 + lane;
-                    const float g = __builtin_amdgcn_exp2f(from[0] - next);
+                    const float g = __builtin_amdgcn_exp2f((from[0] - next) * c);
                     l = fmaf(g, from[64], l);
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
@@ -777,7 +803,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
     zero_rows<S>(fresh_args<TreeAttnArgs>());          // (last: the first ones to be done have the time)
 }
 
-// Rows of items that several workgroups took: their parts joined (weights 2^(m - largest m)), 32 rows (those of one wave) by a workgroup and in the layout of
+// Rows of items that several workgroups took: their parts joined (weights 2^(c * (m - largest m))), 32 rows (those of one wave) by a workgroup and in the layout of
 // a wave's registers: lane l has the row l % 32 and every second group of four elements.  The workgroups of the item's second
 // share take a quarter of the elements with each wave; where there are many parts, those of eight shares take an eighth each and
 // their waves the parts in turn.  Bound by the trip record -> place -> parts: 2.3 us for a short tree, 14 us for the 17 MB of
@@ -793,6 +819,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int w = blockIdx.x, wr = blockIdx.y, at = wr * 32 + (lane & 31);
     const JoinRecord r = a.join[w];
+    const float c = exponent_of(a.scale).c;
     if (wr * 32 >= r.rows) return;
     const int turn = w - r.first - 1;                  // 0: the item's second share
     const bool share = r.last - r.first + 1 > kJoinShared;
@@ -821,7 +848,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
             float best = top;
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) best = fmaxf(best, m[k]);
-            const float f = __builtin_amdgcn_exp2f(top - best);
+            const float f = __builtin_amdgcn_exp2f((top - best) * c);
             top = best;
             l *= f;
 #pragma unroll
@@ -829,7 +856,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
                 if (g0 + k * step > r.last) continue;
-                const float y = __builtin_amdgcn_exp2f(m[k] - best);
+                const float y = __builtin_amdgcn_exp2f((m[k] - best) * c);
                 l = fmaf(y, x[k], l);
 #pragma unroll
                 for (int i = 0; i < COUNT; ++i)
@@ -838,7 +865,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
             }
         }
     };
-    float top = -1e38f, l = 0.0f;
+    float top = kLowest, l = 0.0f;
     if (!share) {
         float4v acc[Q];
         gather(std::integral_constant<int, Q>{}, wave * Q, r.first, 1, acc, top, l);
@@ -860,7 +887,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
     l = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const float f = __builtin_amdgcn_exp2f(shared[k][4 * E][lane] - best);
+        const float f = __builtin_amdgcn_exp2f((shared[k][4 * E][lane] - best) * c);
         l = fmaf(f, shared[k][4 * E + 1][lane], l);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = fmaf(f, shared[k][4 * wave + e][lane], x[e]);

@@ -37,3 +37,112 @@ def test_commit_of_wide_tables(binding, G, d, width):
         assert torch.equal(pool[0], want[0]) and torch.equal(pool[1], want[1]), counts
         for b, j, r, s in at:
             slots[b, j] = 3
+
+
+def hard_attention(t):
+    """(outputs, truth values [B, N, H]) of rows whose largest score is so far above the others that its value alone is the
+    output: by more than twice what sums in fp32 may be off, and by 40 more, below which no weight changes a rounding."""
+    B, N, H, d = t.q.shape
+    per = H // t.k.shape[2]
+    out, sure = torch.zeros((B, N, H, d), dtype=t.q.dtype), torch.zeros((B, N, H), dtype=torch.bool)
+    for b, n in enumerate(t.lens):
+        pos = torch.arange(n)
+        at = torch.from_numpy(t.table[b]).long()[pos // t.page]
+        for u in range(N):
+            if t.tok[b, u] < 0:
+                continue
+            own, v = [], u
+            while v >= 0:
+                own.append(v)
+                v = int(t.parent[v])
+            for i in range(H):
+                g = i // per
+                K = torch.cat([t.kp[t.layer][at, pos % t.page, g], t.k[b, own, g]]).double()
+                V = torch.cat([t.vp[t.layer][at, pos % t.page, g], t.v[b, own, g]])
+                q = t.q[b, u, i].double()
+                s = K @ q * t.scale
+                off = (K.abs() @ q.abs()) * t.scale * (d + 8) * 2.0 ** -24
+                top = int(s.argmax())
+                rest = torch.cat([s[:top] + off[:top], s[top + 1:] + off[top + 1:]])
+                out[b, u, i] = V[top]
+                sure[b, u, i] = len(rest) == 0 or bool(s[top] - off[top] > rest.max() + 40)
+    return out, sure
+
+
+def far(t, sign, size):
+    """Every product of a query and a key gets this sign and about this size; some queries are as they were."""
+    root = (size / t.q.shape[3]) ** 0.5
+    for x, s in ((t.q, sign), (t.k, 1.0), (t.kp, 1.0)):
+        y = torch.where(x == 0, torch.ones_like(x), x.abs()).double().clamp(0.5, 1.0 if size > 1e38 else 4.0)
+        x.copy_((y * root * s).to(x.dtype))
+    return t
+
+
+@pytest.mark.parametrize("N,H,G,lens", [(1, 4, 1, [300, 0, 3, 5000]), (16, 4, 1, [300, 0, 1]), (16, 14, 1, [700, 33, 0]), (33, 1, 1, [2000, 1])])
+@pytest.mark.parametrize("d,dtype,sign,size,scale", [
+    (128, BF, -1.0, 1.5e38, 1.0),      # scores are finite, and less than -1e38
+    (64, BF, -1.0, 2.0e38, 1.6),       # ... also where their product with log2(e) is not
+    (64, BF, 1.0, 2.0e38, 1.6),
+    (128, BF, 1.0, 1e12, 1.0),         # far above what a difference of rounded products would keep inside the range
+    (64, HF, -1.0, 1.6e9, 1.0),
+    (128, HF, 1.0, 1.6e9, 1.0),
+])
+def test_attention_of_far_scores(binding, N, H, G, lens, d, dtype, sign, size, scale):
+    """Scores of any size that fp32 holds: the row is that of its largest one, not NaN."""
+    t = far(Attn(binding, 200 + N + H, lens, N, H, G, d, 16, dtype, 0.8 if N > 1 else 1.0), sign, size)
+    t.scale = scale
+    want, sure = hard_attention(t)
+    drafted = torch.from_numpy(t.tok) >= 0
+    assert int(sure.sum()) * 4 > int(drafted.sum()) * H
+    got = t.h.tree_attention(**t.on_gpu()).cpu()
+    assert bool(torch.isfinite(got).all())
+    assert torch.equal(got[sure], want[sure])
+    assert bool((got[~drafted] == 0).all())
+
+
+def test_attention_of_far_scores_beside_ordinary_ones(binding):
+    """Rows of one wave with scores of 1e9 and rows with scores of 1: the ordinary rows keep their errors."""
+    for N, H, G, d, dtype in ((16, 4, 2, 128, BF), (33, 7, 1, 64, HF), (16, 2, 1, 64, HF)):
+        t = Attn(binding, 230 + N, [900, 77, 0], N, H, G, d, 16, dtype, 1.0)
+        t.q[:, ::3] *= 2.0 ** 13                          # (eight times 2^13 and more is infinite in fp16: such queries have no value)
+        loud = t.q[:, ::3].clone()
+        known = torch.isfinite(t.q).all(dim=3)
+        got = t.h.tree_attention(**t.on_gpu()).cpu()
+        want, sure = hard_attention(t)
+        sure &= known
+        assert bool(torch.isfinite(got[known]).all()) and bool(sure[:, ::3].any()) and torch.equal(got[sure], want[sure])
+        t.q[:, ::3] = 0
+        want, tol = t.want()
+        keep = torch.arange(N) % 3 != 0
+        assert bool(((got.double() - want).abs() <= tol)[:, keep].all())
+        t.q[:, ::3] = loud
+
+
+@pytest.mark.parametrize("N,H,G", [(1, 4, 1), (16, 4, 1), (16, 14, 1)])
+def test_attention_scores_that_are_minus_infinity_count_for_nothing(binding, N, H, G):
+    """Keys of minus infinity leave a row to the others; a row that has no other is NaN, as is one with an infinite score."""
+    t = Attn(binding, 240 + N + H, [200, 40, 0], N, H, G, 64, 16, BF, 1.0)
+    t.q.copy_(t.q.abs() + 0.25)
+    want, tol = t.want()
+    used = [(t.table[0, p // 16], p % 16) for p in range(0, 200)]
+    for a, p in used[:150]:                               # whole stages and parts of one
+        t.kp[0][a, p] = float("-inf")
+    want, tol = (x.clone() for x in (want, tol))
+    s = t.lens
+    t.lens = [50, 40, 0]
+    table, t.table = t.table, t.table.copy()
+    keep = used[150:]
+    K = torch.stack([t.kp[0][a, p] for a, p in keep])
+    V = torch.stack([t.vp[0][a, p] for a, p in keep])
+    kp, vp = t.kp, t.vp
+    t.kp, t.vp = t.kp.clone(), t.vp.clone()
+    for i in range(50):
+        t.kp[0][t.table[0, i // 16], i % 16], t.vp[0][t.table[0, i // 16], i % 16] = K[i], V[i]
+    want, tol = t.want()
+    t.kp, t.vp, t.table, t.lens = kp, vp, table, s
+    got = t.h.tree_attention(**t.on_gpu()).cpu().double()
+    assert bool(((got - want).abs() <= tol).all())
+    t.k[1, 0] = float("inf")                              # the root's key: every row of that trajectory sees it
+    t.k[2] = float("-inf")                                # nothing but the tree, and nothing of it counts
+    got = t.h.tree_attention(**t.on_gpu()).cpu().double()
+    assert bool(((got - want).abs() <= tol)[0].all()) and bool(torch.isnan(got[1:]).all())

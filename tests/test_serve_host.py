@@ -1,9 +1,9 @@
-"""The host side of the operators around a verification, without a GPU: how a commit's positions are shared out."""
+"""The host side of the operators around a verification, without a GPU: how a commit's positions are shared out, what is refused."""
 import ctypes as C
 
 import pytest
 
-from tests import servehost
+from tests import servehost, serveplan, test_serve_plan
 
 I, U, L, P = C.c_int, C.c_uint, C.c_int64, C.c_void_p
 
@@ -44,3 +44,17 @@ def test_a_commit_copies_what_was_counted_and_nothing_else(commit, row_words):
                 assert commit.words(n, j0, per, row_words) == min(max(n - j0, 0), per) * row_words, (width, count, j0)
             # a workgroup's next position: behind the last one it is past the end of every row, in 32 bits without a sign too
             assert n + step < 2 ** 32 and (step >= width or commit.groups(width, per) == (2 ** 32 - 1) // 256)
+
+
+def test_scales_of_the_attention():
+    """A scale's product with log2(e) is a number, however large the scale is."""
+    L, c = serveplan.lib(), test_serve_plan.cache()
+
+    def call(scale):
+        rows = serveplan.TreeRows(d_q=4096, d_k=4096, d_v=4096, d_out=8192, q_heads=4, scale=scale)
+        return L.attention(3, C.byref(c), 1, 64, 64, 9, 64, C.byref(rows), 256)
+
+    for scale in (1e-45, 1e-38, 0.125, 1.0, 2.0 ** 127):
+        assert call(scale) == 0, scale
+    for scale in (0.0, -0.0, -1.0, 1.7015e38, 3.4e38, float("inf"), float("nan")):
+        assert call(scale) == test_serve_plan.EINVAL, scale
