@@ -114,8 +114,9 @@ hipError_t attn_launch(TreeAttnArgs &a, hipStream_t s)
 
 extern "C" uint64_t stand_tree_attention_work(const stand_handle *h, const stand_cache *cache, int32_t q_heads)
 {
-    if (!h || !cache_ok(cache) || !heads_ok(cache, q_heads)) return 0;
+    if (!h) return 0;
     const ServeView v = serve_view(const_cast<stand_handle *>(h));
+    if (check_attention_size(v.B, cache, q_heads) != STAND_OK) return 0;
     const AttnForm f = attn_form((int64_t)v.N * (q_heads / cache->kv_heads));
     return with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, f,
                            [&](auto s) { return attn_work_bytes<decltype(s)>(attn_groups_of<decltype(s)>(v)); });

@@ -40,6 +40,16 @@ inline bool spans_chunks(int64_t x, int64_t x_stride, int64_t y, int64_t y_strid
 
 inline bool heads_ok(const stand_cache *c, int32_t q_heads) { return q_heads >= 1 && q_heads % c->kv_heads == 0; }
 
+// Whether there is an attention of that size at all: what its workspace depends on, and how far it can count.
+inline int check_attention_size(int64_t B, const stand_cache *cache, int32_t q_heads)
+{
+    if (!cache_ok(cache) || !heads_ok(cache, q_heads)) return STAND_EINVAL;
+    if (B > kAttnMaxBatch || q_heads > 65535) return STAND_ELIMIT;
+    // the kernel counts places of a layer in 16-byte chunks, in 32 bits
+    if (!spans_chunks(cache->pages - 1, cache->page_stride, cache->page_size - 1, cache->slot_stride)) return STAND_ELIMIT;
+    return STAND_OK;
+}
+
 inline int check_tree_attention(int64_t B, const stand_cache *cache, int32_t layer, const int32_t *d_len, const int32_t *d_table,
                                 int32_t table_width, const int32_t *d_draft_tok, const stand_tree_rows *rows, const void *d_work)
 {
@@ -49,13 +59,9 @@ inline int check_tree_attention(int64_t B, const stand_cache *cache, int32_t lay
     if (!aligned16(rows->d_q) || !aligned16(rows->d_k) || !aligned16(rows->d_v) || !aligned16(rows->d_out)) return STAND_EINVAL;
     if (!strides_ok(rows->q_stride) || !strides_ok(rows->k_stride) || !strides_ok(rows->v_stride) || !strides_ok(rows->out_stride))
         return STAND_EINVAL;
-    if (!heads_ok(cache, rows->q_heads)) return STAND_EINVAL;
     if (!(rows->scale > 0.0f && rows->scale <= 0x1p127f)) return STAND_EINVAL;   // (its product with log2(e) is a number)
     if ((int64_t)table_width * cache->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
-    if (B > kAttnMaxBatch || rows->q_heads > 65535) return STAND_ELIMIT;
-    // the kernel counts places of a layer in 16-byte chunks, in 32 bits
-    if (!spans_chunks(cache->pages - 1, cache->page_stride, cache->page_size - 1, cache->slot_stride)) return STAND_ELIMIT;
-    return STAND_OK;
+    return check_attention_size(B, cache, rows->q_heads);
 }
 
 inline int check_cache_commit(int64_t B, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots, int32_t width)

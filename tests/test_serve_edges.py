@@ -146,3 +146,16 @@ def test_attention_scores_that_are_minus_infinity_count_for_nothing(binding, N, 
     t.k[2] = float("-inf")                                # nothing but the tree, and nothing of it counts
     got = t.h.tree_attention(**t.on_gpu()).cpu().double()
     assert bool(((got - want).abs() <= tol)[0].all()) and bool(torch.isnan(got[1:]).all())
+
+
+def test_attention_workspaces_of_refused_calls_have_no_size(binding):
+    """0 bytes say that the call would be refused: a caller can ask before it has any queries."""
+    h, many = handle(binding, 2, tree(9)), handle(binding, 4097, tree(1))
+    x = torch.zeros((1, 4, 16, 2, 64), dtype=BF, device="cuda")
+    cache = binding.PagedCache(x, x)
+    size = h._lib.stand_tree_attention_work
+    assert size(h.h, cache.ref, 4) > 0 and size(h.h, cache.ref, 65534) > 0
+    assert size(h.h, cache.ref, 65536) == 0 and size(h.h, cache.ref, 3) == 0 and size(h.h, cache.ref, 0) == 0 and size(None, cache.ref, 4) == 0
+    assert size(many.h, cache.ref, 4) == 0 and size(h.h, None, 4) == 0
+    cache.desc.page_stride, cache.desc.pages = 2 ** 40, 2 ** 20
+    assert size(h.h, cache.ref, 4) == 0

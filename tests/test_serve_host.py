@@ -58,3 +58,29 @@ def test_scales_of_the_attention():
         assert call(scale) == 0, scale
     for scale in (0.0, -0.0, -1.0, 1.7015e38, 3.4e38, float("inf"), float("nan")):
         assert call(scale) == test_serve_plan.EINVAL, scale
+
+
+@pytest.fixture(scope="module")
+def checks():
+    return servehost.build("""
+#include "serve_checks.hpp"
+using namespace stand;
+extern "C" {
+int sized(int64_t B, const stand_cache *c, int q_heads) { return check_attention_size(B, c, q_heads); }
+int call(int64_t B, const stand_cache *c, const stand_tree_rows *r)
+{
+    const int32_t *x = (const int32_t *)64;
+    return check_tree_attention(B, c, 0, x, x, 9, x, r, (const void *)256);
+}
+}""", dict(sized=([L, P, I], I), call=([L, P, P], I)))
+
+
+def test_no_workspace_is_named_for_an_attention_that_is_refused(checks):
+    """What the size of the workspace depends on is refused by both, by the same code."""
+    far = dict(pages=2 ** 15 + 1, page_size=16)
+    for B, q, kw in ((3, 4, {}), (4096, 4, {}), (4097, 4, {}), (65535, 4, {}), (3, 65534, {}), (3, 65535, {}), (3, 65536, {}), (3, 3, {}), (3, 0, {}), (3, -2, {}),
+                     (3, 4, dict(far, page_stride=2 ** 20)), (3, 4, dict(far, page_stride=2 ** 20 - 128)), (3, 4, dict(page_size=4096, slot_stride=(1 << 48) - 8)),
+                     (4097, 3, {}), *((3, 4, kw) for kw in test_serve_plan.BAD_CACHE)):
+        c = test_serve_plan.cache(**kw)
+        rows = serveplan.TreeRows(d_q=4096, d_k=4096, d_v=4096, d_out=8192, q_heads=q, scale=0.125)
+        assert checks.sized(B, C.byref(c), q) == checks.call(B, C.byref(c), C.byref(rows)), (B, q, kw)
