@@ -9,6 +9,7 @@
 //     x <- -inf                    where the row's mask has no bit for v, unless it has no bit at all
 // in binary32, rounded once to the type of the logits.
 #pragma once
+#include "row_words.hpp"
 #include "wave_ops.hpp"
 
 namespace stand {
@@ -30,23 +31,22 @@ struct ShapeArgs {
     long long rows;
 };
 
-struct alignas(2) Half8 { uint16_t h[8]; };   // eight logits at any alignment: rows of an odd vocabulary start anywhere
-struct alignas(4) Float4 { float f[4]; };
-struct alignas(4) Int4 { uint32_t i[4]; };
-typedef uint32_t Words4 __attribute__((ext_vector_type(4)));
+struct Half8 { uint16_t h[8]; };
+struct Float4 { float f[4]; };
+struct Int4 { uint32_t i[4]; };        // counts and mask words: aligned like one of them
 
 // (Streamed past the caches: 296 us instead of 308 us for 32 trees of 64 rows of 152064.)
 template <int DT>
 __device__ __forceinline__ void load_tokens(const void *row, int t, float (&x)[8])
 {
     if constexpr (DT == kDtBf16) {
-        const Half8 w = __builtin_bit_cast(Half8, __builtin_nontemporal_load((const Words4 *)((const uint16_t *)row + t)));
+        const Half8 w = __builtin_bit_cast(Half8, __builtin_nontemporal_load((const RowWords<2>::type *)((const uint16_t *)row + t)));
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = u2f((uint32_t)w.h[i] << 16);
     } else {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
-            const Float4 w = __builtin_bit_cast(Float4, __builtin_nontemporal_load((const Words4 *)((const float *)row + t + 4 * q)));
+            const Float4 w = __builtin_bit_cast(Float4, __builtin_nontemporal_load((const RowWords<4>::type *)((const float *)row + t + 4 * q)));
 #pragma unroll
             for (int i = 0; i < 4; ++i) x[4 * q + i] = w.f[i];
         }
@@ -63,12 +63,12 @@ __device__ __forceinline__ void store_tokens(void *row, int t, const float (&x)[
         Half8 w;
 #pragma unroll
         for (int i = 0; i < 8; ++i) w.h[i] = bf16_bits(x[i]);
-        __builtin_nontemporal_store(__builtin_bit_cast(Words4, w), (Words4 *)((uint16_t *)row + t));
+        __builtin_nontemporal_store(__builtin_bit_cast(RowWords<2>::type, w), (RowWords<2>::type *)((uint16_t *)row + t));
     } else {
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
             const Float4 w = {{x[4 * q], x[4 * q + 1], x[4 * q + 2], x[4 * q + 3]}};
-            __builtin_nontemporal_store(__builtin_bit_cast(Words4, w), (Words4 *)((float *)row + t + 4 * q));
+            __builtin_nontemporal_store(__builtin_bit_cast(RowWords<4>::type, w), (RowWords<4>::type *)((float *)row + t + 4 * q));
         }
     }
 }

@@ -84,3 +84,31 @@ def test_no_workspace_is_named_for_an_attention_that_is_refused(checks):
         c = test_serve_plan.cache(**kw)
         rows = serveplan.TreeRows(d_q=4096, d_k=4096, d_v=4096, d_out=8192, q_heads=q, scale=0.125)
         assert checks.sized(B, C.byref(c), q) == checks.call(B, C.byref(c), C.byref(rows)), (B, q, kw)
+
+
+def test_words_of_a_row_are_aligned_like_its_elements():
+    """What the shaped logits are read and written through promises no more than the accepted pointers keep (2 and 4 bytes)."""
+    lib = servehost.build("""
+#include "row_words.hpp"
+using namespace stand;
+template <int ES> static int sum(const char *row, int first)
+{
+    typedef typename RowWords<ES>::type Words;
+    const Words w = *(const Words *)(row + first * ES);
+    return (int)(w[0] + w[1] + w[2] + w[3]);
+}
+extern "C" {
+int alignment(int es) { return es == 2 ? (int)alignof(RowWords<2>::type) : (int)alignof(RowWords<4>::type); }
+int bytes(int es) { return es == 2 ? (int)sizeof(RowWords<2>::type) : (int)sizeof(RowWords<4>::type); }
+int sum_at(int es, const void *row, int first) { return es == 2 ? sum<2>((const char *)row, first) : sum<4>((const char *)row, first); }
+}""", dict(alignment=([I], I), bytes=([I], I), sum_at=([I, P, I], I)))
+    row = (C.c_uint8 * 64)(*range(64))
+    for es in (2, 4):
+        assert lib.alignment(es) == es and lib.bytes(es) == 16
+        for first in range(8):
+            data = bytes(row)[first * es: first * es + 16]
+            want = sum(int.from_bytes(data[4 * i: 4 * i + 4], "little") for i in range(4)) & 0xFFFFFFFF
+            assert lib.sum_at(es, row, first) & 0xFFFFFFFF == want
+    text = open(servehost.CSRC + "/shape_logits.hpp").read()
+    rows = [line for line in text.splitlines() if "__builtin_nontemporal_" in line]
+    assert rows and all("RowWords<" in line for line in rows)
