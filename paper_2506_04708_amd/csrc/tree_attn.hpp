@@ -144,15 +144,15 @@ __device__ __forceinline__ float raise_row(const Exponent &e, float top, float &
 }
 
 // Asynchronous copies from global memory to LDS: lane l's 16 (4) bytes go to `to` + 16 l (4 l).  They have no result register;
-// whoever reads what they bring waits for them (wait_loads) first.  (As builtins they make the compiler wait for all of them
-// before any read of LDS, also of another buffer.)
+// whoever reads what they bring waits for them (wait_loads) first.  `to` is in m0, which has to be set an instruction ahead of the
+// copy.  (As builtins they make the compiler wait for all of them before any read of LDS, also of another buffer.)
 __device__ __forceinline__ void copy16_async(const void *from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"{m0}"(to), "v"(from) : "memory");
 }
 __device__ __forceinline__ void copy4_async(const void *from, uint32_t to)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(to), "v"(from) : "memory");
 }
 template <int NEWER>
 __device__ __forceinline__ void wait_loads()

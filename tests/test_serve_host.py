@@ -1,5 +1,8 @@
 """The host side of the operators around a verification, without a GPU: how a commit's positions are shared out, what is refused."""
 import ctypes as C
+import glob
+import os
+import re
 
 import pytest
 
@@ -112,3 +115,14 @@ int sum_at(int es, const void *row, int first) { return es == 2 ? sum<2>((const 
     text = open(servehost.CSRC + "/shape_logits.hpp").read()
     rows = [line for line in text.splitlines() if "__builtin_nontemporal_" in line]
     assert rows and all("RowWords<" in line for line in rows)
+
+
+def test_inline_assembly_writes_no_register_behind_the_compilers_back():
+    """m0 and other registers by name are operands of the statements that need them, never written inside."""
+    found = 0
+    for path in glob.glob(os.path.join(servehost.CSRC, "*.h*")):
+        for text in re.findall(r'asm volatile\(\s*"([^"]*)"', open(path).read()):
+            found += 1
+            for line in text.replace("\\t", "").split("\\n"):
+                assert not re.match(r"\w+\s+(m0|vcc|exec|[sv]\d+|[sv]\[)", line.strip()), (path, line)
+    assert found > 4
