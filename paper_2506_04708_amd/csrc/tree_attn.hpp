@@ -13,7 +13,9 @@
 // key/value head share its keys, so a tile has up to 256 rows of (node, head) that read a key once.  A wave has 32 of them.  It
 // computes S^T = K Q^T with 32x32x16 products, so that a lane has one row and 16 of 32 keys: maximum and sum need one exchange
 // between two lanes, and the weights stand where the second product O^T = V^T P^T wants its right operand, with the keys in
-// another order; the values are read in that order (transposed by the LDS reads).  Nothing but keys and values passes through LDS.
+// another order; the values are read in that order (transposed by the LDS reads).  Queries, scores and weights stay in registers;
+// what passes through LDS beside keys and values is page numbers, the nodes' ancestors and list, and parts of waves that have
+// different keys of the same rows.
 //
 // Keys come in stages of 64 or 128 by asynchronous copies, page numbers two stages ahead of them, into a swizzled layout that
 // both products read without bank conflicts.  Four stages of memory: two on their way, one in work, one whose values are
@@ -197,7 +199,9 @@ struct AttnShape {
     static constexpr int BYTES = MISC + WAVES * 128;
     static_assert(KW % KPI == 0 && KW >= KPI && KW <= 64, "a copy instruction brings whole keys of one wave");
     static_assert(SUB == 1 || SUB == 2, "a step reads the keys of the other one of two subtiles ahead");
-    static_assert((WK - 1) * TM * (D + 2) * 4 <= NBUF * STAGE, "parts of the key waves are joined in the stages' memory");
+    // a wave's part as its registers stand: 16 (D / 32) outputs, maximum and sum of every lane
+    static constexpr int LANE_PART = 16 * (D / 32) + 2, KEY_PARTS = (WK - 1) * WR * LANE_PART * 64 * 4;
+    static_assert(KEY_PARTS <= NBUF * STAGE, "parts of the key waves are joined in the stages' memory");
     // 16-byte chunk c of key k stands at chunk c ^ swizzle(k): reads of one chunk of 16 keys (K) and of four chunks of four
     // keys (V) touch every bank once
     static __device__ __forceinline__ int swizzle_k(int k) { return D == 128 ? k & 15 : (k >> 1) & 7; }
@@ -740,9 +744,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         m = fmaxf(m, kLowest);                         // (nothing seen: differences of maxima are numbers)
         if constexpr (S::WK > 1) {
             __syncthreads();
-            float *join = (float *)attn_lds;           // [WK - 1][WR][16 DT + 2][64]
+            float *join = (float *)attn_lds;           // [WK - 1][WR][LANE_PART][64]
             if (wk > 0) {
-                float *to = join + ((wk - 1) * S::WR + wr) * (16 * DT + 2) * 64 + lane;
+                float *to = join + ((wk - 1) * S::WR + wr) * S::LANE_PART * 64 + lane;
                 to[0] = m; to[64] = l;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
@@ -753,7 +757,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             if (wk == 0) {
                 float next = m;
 #pragma unroll
-                for (int k = 0; k < S::WK - 1; ++k) next = fmaxf(next, join[(k * S::WR + wr) * (16 * DT + 2) * 64 + lane]);
+                for (int k = 0; k < S::WK - 1; ++k) next = fmaxf(next, join[(k * S::WR + wr) * S::LANE_PART * 64 + lane]);
                 const float f = __builtin_amdgcn_exp2f((m - next) * c);
                 l *= f;
 #pragma unroll
@@ -762,7 +766,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                     for (int i = 0; i < 16; ++i) o[d][i] *= f;
 #pragma unroll
                 for (int k = 0; k < S::WK - 1; ++k) {
-                    const float *from = join + (k * S::WR + wr) * (16 * DT + 2) * 64 + lane;
+                    const float *from = join + (k * S::WR + wr) * S::LANE_PART * 64 + lane;
                     const float g = __builtin_amdgcn_exp2f((from[0] - next) * c);
                     l = fmaf(g, from[64], l);
 #pragma unroll
