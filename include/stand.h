@@ -420,8 +420,9 @@ typedef struct {
  * query . key (summed in fp32, before the scale) that is neither finite nor -infinity makes the row NaN, and so does a row of nothing
  * but -infinity; finite ones of any size do not.  A drafted node's ancestors are drafted.
  *   Keys (and values) of one layer span less than 64 GiB (STAND_ELIMIT).
- *   Products are summed in fp32, the weights p are rounded to the cache's type for the product with the values (relative error
- * 2^-9 in bf16, 2^-12 in fp16 each, at most half a step) and summed as rounded; the result is rounded once.
+ *   Products are summed in fp32, the weights p are rounded to the cache's type for the product with the values and summed as
+ * rounded; the result is rounded once.  A weight's error is half a step of its type: up to 2^-8 of it in bf16, 2^-11 in fp16, and in
+ * fp16 not less than 2^-31 of the row's largest weight, so that n far smaller ones together may be off by n * 2^-31 of that one.
  *   d_work: 16-byte aligned device memory of stand_tree_attention_work bytes, used from the call's start to its end on the
  * stream; no content is expected or kept.  Calls that may overlap (other streams, other graphs) need one each. */
 int stand_tree_attention(stand_handle *h, const stand_cache *cache, int32_t layer, const int32_t *d_len, const int32_t *d_table,

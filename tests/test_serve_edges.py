@@ -7,7 +7,12 @@ pytestmark = pytest.mark.gpu
 
 torch = pytest.importorskip("torch")
 
+from paper_2506_04708_amd import synth  # noqa: E402
+from tests import test_serve_ops  # noqa: E402
 from tests.test_serve_ops import BF, HF, Attn, binding, drafts, handle, tree  # noqa: E402,F401
+
+for _n, _deep, _fan in ((20, 5, [4, 2, 2, 1]), (70, 8, [8, 4, 2, 1]), (300, 12, [8, 4, 2, 1]), (1024, 31, [8, 4, 2, 1])):
+    test_serve_ops.TREES.setdefault(_n, synth.make_tree(_n, _deep, _fan).tolist())
 
 
 @pytest.mark.parametrize("G,d,width", [(64, 128, 2 ** 21 + 5), (8, 128, 2 ** 21 + 5), (64, 128, 2 ** 24 + 5)])
@@ -159,3 +164,74 @@ def test_attention_workspaces_of_refused_calls_have_no_size(binding):
     assert size(many.h, cache.ref, 4) == 0 and size(h.h, None, 4) == 0
     cache.desc.page_stride, cache.desc.pages = 2 ** 40, 2 ** 20
     assert size(h.h, cache.ref, 4) == 0
+
+
+@pytest.mark.parametrize("B,N,H,G,d,dtype", [
+    (20, 70, 1, 1, 64, BF), (20, 70, 2, 1, 128, HF),     # drafted nodes counted eight trajectories at a time
+    (40, 70, 1, 1, 64, HF), (100, 70, 1, 1, 128, BF),    # ... and sixteen, more of them than a wave has lanes
+    (90, 20, 1, 1, 64, BF), (260, 9, 3, 1, 128, HF),     # several trajectories in a wave, in many turns
+    (70, 33, 1, 1, 128, BF), (70, 33, 1, 1, 64, HF),     # the form of up to 64 rows
+])
+def test_attention_of_many_trees(binding, B, N, H, G, d, dtype):
+    lens = [int(x) for x in np.random.default_rng(B + N).integers(0, 50, B)]
+    Attn(binding, 250 + B + N, lens, N, H, G, d, 16, dtype, 0.5).check()
+
+
+@pytest.mark.parametrize("N,H,G,d,dtype,share", [
+    (300, 2, 1, 64, BF, 0.7), (300, 3, 3, 128, HF, 1.0), (1024, 1, 1, 128, BF, 1.0), (1024, 2, 1, 64, HF, 0.9), (1024, 2, 2, 64, BF, 0.6),
+])
+def test_attention_of_large_trees(binding, N, H, G, d, dtype, share):
+    """The longest lists of nodes, with NaN in the nodes that were not drafted and values that are not finite in leaves."""
+    t = Attn(binding, 260 + N + H, [70, 0], N, H, G, d, 16, dtype, share)
+    if share < 1:
+        t.tok[1] = t.tok[0]                                # (the last one has nothing drafted)
+    gone = torch.from_numpy(t.tok) < 0
+    for x in (t.q, t.k, t.v):
+        x[gone] = float("nan")
+    t.check()
+    want, tol = t.want()
+    drafted = np.nonzero(t.tok[0] >= 0)[0]
+    inner = set(t.parent[drafted].tolist())
+    leaves = [int(u) for u in drafted if int(u) not in inner]
+    per = H // G
+    some = [leaves[0], leaves[len(leaves) // 2], leaves[-1]]
+    for i, u in enumerate(some):
+        t.v[0, u, G - 1, 5 + i] = float("-inf") if i % 2 else float("nan")
+    got = t.h.tree_attention(**t.on_gpu()).cpu().double()
+    for i, u in enumerate(some):
+        assert not bool(torch.isfinite(got[0, u, (G - 1) * per:, 5 + i]).any())
+        got[0, u, (G - 1) * per:, 5 + i] = want[0, u, (G - 1) * per:, 5 + i]
+    assert bool(((got - want).abs() <= tol).all())
+
+
+@pytest.mark.parametrize("d,dtype,N", [(64, BF, 1), (128, HF, 16), (128, BF, 64)])
+def test_places_far_into_a_cache(binding, d, dtype, N):
+    """Pages 9 GiB apart: places past 2^32 bytes and past 2^31 chunks of 16 bytes, for rows that come and rows that are read."""
+    apart, page, G = (9 << 30) // 2, 16, 2
+    t = Attn(binding, 270 + N, [64, 33], N, 4, G, d, page, dtype, 1.0)
+    t.pages = 5
+    t.kp, t.vp = t.kp[:, :5].contiguous(), t.vp[:, :5].contiguous()
+    t.table[0, :4], t.table[1, :3] = [4, 1, 0, 3], [4, 2, 3]  # (shared pages: both read the same)
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 36 GiB of device memory")
+    flat = torch.empty(4 * apart + 2 * page * G * d, dtype=dtype, device="cuda")
+    shape, strides = (1, 5, page, G, d), (8, apart, G * d, d, 1)
+    k, v = (flat.as_strided(shape, strides, i * page * G * d) for i in range(2))
+    cache = binding.PagedCache(k, v)
+    slots = torch.arange(5 * page, dtype=torch.int64, device="cuda").flip(0).contiguous()[None]
+    rows = [x.cuda().reshape(1, 1, 5 * page, G, d) for x in (t.kp, t.vp)]
+    one = handle(binding, 1, tree(1))
+    one.cache_commit(cache, rows[0], rows[1], slots, slots.int())
+    assert torch.equal(k.cpu(), t.kp) and torch.equal(v.cpu(), t.vp)
+    t.check(t.h.tree_attention(**dict(t.on_gpu(), cache=cache)))
+
+
+def test_attention_of_many_small_weights(binding):
+    """fp16 weights far below the largest are as coarse as the documentation says, and not coarser."""
+    t = Attn(binding, 280, [30000, 5], 1, 4, 1, 64, 16, HF, 1.0)
+    for x in (t.q, t.k, t.kp):
+        x.zero_()
+    t.q[..., 0] = 8.0
+    t.kp[..., 0] = -1.85 - torch.rand(t.kp.shape[:-1], generator=torch.Generator().manual_seed(1)) * 0.1
+    t.scale = 1.0
+    t.check()

@@ -126,3 +126,9 @@ def test_inline_assembly_writes_no_register_behind_the_compilers_back():
             for line in text.replace("\\t", "").split("\\n"):
                 assert not re.match(r"\w+\s+(m0|vcc|exec|[sv]\d+|[sv]\[)", line.strip()), (path, line)
     assert found > 4
+
+
+@pytest.mark.parametrize("kind", ["short", "any"])
+def test_shares_of_heads_of_64_with_64_rows(kind):
+    """The partition of the one form that tests/test_serve_plan.py leaves out: tiles of 64 rows, beginnings of eight units."""
+    test_serve_plan.test_shares_cover_every_unit_once(kind, 64, 64, 8, 1, 1)
