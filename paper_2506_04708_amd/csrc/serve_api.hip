@@ -47,7 +47,7 @@ int bad_device(const ServeView &v, hipError_t e)
 //   up to 32: four waves on different keys, each loading its own without a barrier (32 trees of 17 .. 32 rows, d 64: 44 us, with
 //     tiles of 256 rows 51; up to 64 rows it would be behind: 90 us instead of 74, d 128);
 //   up to 64: two waves of rows on each half of a stage's keys (32 trees, d 128: 72 us, with tiles of 256 rows 75; d 64: 42 and
-//     49 us);
+//     49 us).  With d 128 it has 16 vector registers too few: they are stored and loaded again once per item, outside the loop;
 //   above: eight waves of rows with d 128, 256 of them (four waves of rows on halves of the keys took the same times, 85 .. 89 us,
 //     with 128 rows); with d 64 four, whose two workgroups share a compute unit (128 trees of 128 nodes: 190 us, eight: 207).
 enum AttnForm { kAttn32, kAttn64, kAttnMore };
