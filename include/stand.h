@@ -481,7 +481,7 @@ int stand_cache_pages(stand_handle *h, const stand_pages *p, const int32_t *d_ad
  *   the grammar does not reach: its parent's mask keeps it from being accepted), so that its maximum stays finite.
  * Rows of nodes that were not drafted are copied.
  *   d_count    [B][V] kept by stand_count_tokens, or NULL (nothing generated, no prompt; the path's tokens count all the same)
- *   d_penalty  [B][3]: repetition (> 0; 1: none), presence, frequency (0: none); or NULL
+ *   d_penalty  [B][3]: repetition (> 0, no subnormal number; 1: none), presence, frequency (finite; 0: none); or NULL
  *   d_bias_id  [B][bias_width], d_bias [B][bias_width]: ids outside [0, V) are left out, of entries with the same id the last
  *              counts; biases are finite or -inf; bias_width 0: none
  *   d_allow    [B][N][(V + 31) / 32]: bit v % 32 of word v / 32; bits past V do not matter; or NULL

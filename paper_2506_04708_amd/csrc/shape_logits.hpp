@@ -165,6 +165,7 @@ __global__ __launch_bounds__(kShapeThreads) void shape_logits_kernel(ShapeArgs a
     int32_t c0[8];
     float shift[8];
     const float rho = a.penalty ? a.penalty[3 * b] : 1.0f, inverse = 1.0f / rho;
+    const float divisor = rho < __builtin_huge_valf() ? rho : 0.0f;   // (an infinite one's quotients are zero without a remainder)
     const float present = a.penalty ? a.penalty[3 * b + 1] : 0.0f;
     const float often = a.penalty ? a.penalty[3 * b + 2] : 0.0f;
     bool touched = false;                         // this thread's tokens are not all as they were
@@ -226,7 +227,7 @@ __global__ __launch_bounds__(kShapeThreads) void shape_logits_kernel(ShapeArgs a
                     for (int e = 0; e < 8; ++e) {
                         const float times = (float)(c[e] & (kPromptFlag - 1)), z = x[k][e];
                         // the quotient to half a step: one correction with the exact remainder (there is none of an infinity)
-                        const float q = z * inverse, p = q < __builtin_huge_valf() ? fmaf(fmaf(-q, rho, z), inverse, q) : q;
+                        const float q = z * inverse, p = q < __builtin_huge_valf() ? fmaf(fmaf(-q, divisor, z), inverse, q) : q;
                         float y = z > 0.0f ? p : z * rho;
                         y = y - often * times;
                         y = times > 0.0f ? y - present : y;

@@ -235,3 +235,22 @@ def test_attention_of_many_small_weights(binding):
     t.kp[..., 0] = -1.85 - torch.rand(t.kp.shape[:-1], generator=torch.Generator().manual_seed(1)) * 0.1
     t.scale = 1.0
     t.check()
+
+
+@pytest.mark.parametrize("rho", [2.0 ** -126, 1e-30, 1e30, 3.4e38, float("inf")])
+def test_repetition_penalties_of_any_size(binding, rho):
+    """Quotients and products by what a penalty may be: 1 / rho is then subnormal, zero or nearly infinite."""
+    t = test_serve_ops.Shape(binding, 290, 1, 2, 64, torch.float32, 0, None, True, False, share=1.0)
+    t.count = torch.full((1, 64), 1, dtype=torch.int32)
+    t.penalty = torch.tensor([[rho, 0.0, 0.0]])
+    t.x[0, 0] = torch.cat([torch.linspace(-3, -0.1, 31), torch.linspace(0.1, 3, 33)])
+    t.x[0, 1] = torch.cat([10.0 ** torch.linspace(-37, 38, 40), -10.0 ** torch.linspace(-37, 38, 24)])
+    got = t.h.shape_logits(out=None, **t.args()).cpu()
+    r = t.penalty[0, 0].double()
+    x = t.x.double()
+    exact = torch.where(x > 0, x / r, x * r)
+    want = exact.float()
+    # half a step, of a subnormal number 2^-150; past the largest number infinity
+    off = (got.double() - want.double()).abs()
+    same = (got == want) | (off <= want.double().abs() * 2.0 ** -23) | (off <= 2.0 ** -149)
+    assert bool(same.all()), (got[~same], want[~same])
