@@ -6,7 +6,7 @@ namespace stand {
 
 constexpr int kCommitThreads = 256;
 
-// Positions that a workgroup copies at a time: at least four 16-byte words a thread, where a row (row_words of them) is no longer.
+// Positions that a workgroup copies at a time: as many rows of row_words 16-byte words as make four words a thread.
 STAND_BOTH int commit_per_group(int row_words) { return (1024 + row_words - 1) / row_words; }
 // Workgroups of a trajectory in a layer: one for each such piece of the width, as far as a launch's dimension has threads for them
 // (2^32 - 1); past that they go on by `groups` pieces at a time.  (Positions past 2^31 fit 32 bits without a sign.)

@@ -124,6 +124,52 @@ def test_attention_of_far_scores_beside_ordinary_ones(binding):
 
 
 @pytest.mark.parametrize("N,H,G", [(1, 4, 1), (16, 4, 1), (16, 14, 1)])
+def test_attention_of_extreme_scales(binding, N, H, G):
+    """From the smallest number, which leaves the mean of the values, to the largest that is accepted, which leaves one of them."""
+    for d, dtype in ((64, HF), (128, BF)):
+        t = Attn(binding, 245 + N + H, [300, 0, 2000], N, H, G, d, 16, dtype, 0.8 if N > 1 else 1.0)
+        for t.scale in (2.0 ** -149, 1e-40, 2.0 ** -126, 1e-20):
+            t.check()
+        t.scale = 2.0 ** 127
+        want, sure = hard_attention(t)
+        got = t.h.tree_attention(**t.on_gpu()).cpu()
+        assert bool(sure.any()) and bool(torch.isfinite(got).all()) and torch.equal(got[sure], want[sure])
+
+
+@pytest.mark.parametrize("N,H,G,lens", [(1, 4, 1, [5000, 0]), (16, 3, 1, [1500, 40, 3]), (16, 14, 1, [3000, 1])])
+@pytest.mark.parametrize("d,dtype,e", [(128, BF, 20), (128, BF, 22), (64, BF, 23), (64, BF, 60), (64, HF, 21), (128, HF, 22), (64, HF, 23), (128, HF, 30)])
+def test_attention_of_equal_scores_of_any_size(binding, N, H, G, lens, d, dtype, e):
+    """Keys that are all the same leave the mean of the values, below the size from which maxima are taken off and above it, also
+    where a row is joined from several parts; rows of both kinds and of both signs in one wave."""
+    t = Attn(binding, 248 + N + H, lens, N, H, G, d, 16, dtype, 0.8 if N > 1 else 1.0)
+    t.scale = 1.0
+    for x in (t.k, t.kp):
+        x.fill_(2.0 ** (e // 2 - 3))
+    t.q.fill_(2.0 ** (e - e // 2 + 3) / d)                 # scores of 2^e exactly, some of -2^e, 3 * 2^e and 1
+    t.q[:, ::3] *= -1
+    t.q[:, 1::4] *= 3
+    t.q[:, 2::5] *= 2.0 ** -e if dtype is BF else 2.0 ** -10
+    got = t.h.tree_attention(**t.on_gpu()).cpu().double()
+    half = 2.0 ** -8 if dtype is BF else 2.0 ** -11
+    for b, n in enumerate(lens):
+        pos = torch.arange(n)
+        V = t.vp[0][torch.from_numpy(t.table[b]).long()[pos // 16], pos % 16].double()
+        for u in range(N):
+            if t.tok[b, u] < 0:
+                continue
+            own, v = [], u
+            while v >= 0:
+                own.append(v)
+                v = int(t.parent[v])
+            for i in range(H):
+                all_v = torch.cat([V[:, i // (H // G)], t.v[b, own, i // (H // G)].double()])
+                mean = all_v.mean(0)
+                # equal weights: sums of so many terms in fp32, parts joined, one quotient and the rounding of the result
+                tol = all_v.abs().mean(0) * (len(all_v) + 64) * 2.0 ** -24 * 2 + mean.abs() * half + (2.0 ** -25 if dtype is HF else 0)
+                assert bool(((got[b, u, i] - mean).abs() <= tol).all()), (b, u, i)
+
+
+@pytest.mark.parametrize("N,H,G", [(1, 4, 1), (16, 4, 1), (16, 14, 1)])
 def test_attention_scores_that_are_minus_infinity_count_for_nothing(binding, N, H, G):
     """Keys of minus infinity leave a row to the others; a row that has no other is NaN, as is one with an infinite score."""
     t = Attn(binding, 240 + N + H, [200, 40, 0], N, H, G, 64, 16, BF, 1.0)
