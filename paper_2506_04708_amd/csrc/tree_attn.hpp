@@ -117,6 +117,22 @@ template <bool F16> constexpr float kUp = F16 ? 6.0f : 0.0f;
 constexpr float kFarRow = 4194304.0f;   // 2^22: c * m is rounded by at most a quarter
 constexpr float kLowest = -3.402823466e+38f;
 
+// What c * m is rounded by in a row's shift: nothing where the row is far.
+template <bool F16>
+__device__ __forceinline__ float shift_error(const Exponent &e, float m)
+{
+    const float shift = fmaf(-m, e.c, kUp<F16>), off = fmaf(m, e.c, shift) - kUp<F16>;
+    return fabsf(shift) > kFarRow ? 0.0f : off;
+}
+// What sums made with a maximum `from` are multiplied by where they join those made with `to`, as an exponent.  (c * (from - to)
+// alone would be off by what the shifts were rounded by, an eighth of a weight at 2^21.)  `to` is no less than `from`, and one of
+// them is finite.
+template <bool F16>
+__device__ __forceinline__ float lowered(const Exponent &e, float from, float to)
+{
+    return (from - to) * e.c + (shift_error<F16>(e, to) - shift_error<F16>(e, from));
+}
+
 // The running maximum m of a lane's row before the products with the values of the scores s[0 .. NS), whose largest one is `top`:
 // -> the shift of their exponents, c * s + shift.  m is raised, and the sum l and outputs o are scaled, where `top` passes it by more
 // than `rise`; m begins at -infinity.  Rows with |c * m| > 2^22 (nothing but -infinity seen among them) come here with every stage
@@ -126,7 +142,7 @@ __device__ __forceinline__ float raise_row(const Exponent &e, float top, float &
 {
     float shift = fmaf(-m, e.c, kUp<F16>);
     if (__ballot(top > m + e.rise || fabsf(shift) > kFarRow)) {
-        const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(next > m ? (m - next) * e.c : 0.0f);
+        const float next = fmaxf(m, top), f = __builtin_amdgcn_exp2f(next > m ? lowered<F16>(e, m, next) : 0.0f);
         m = next;
         l *= f;
 #pragma unroll
@@ -758,7 +774,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 float next = m;
 #pragma unroll
                 for (int k = 0; k < S::WK - 1; ++k) next = fmaxf(next, join[(k * S::WR + wr) * S::LANE_PART * 64 + lane]);
-                const float f = __builtin_amdgcn_exp2f((m - next) * c);
+                const float f = __builtin_amdgcn_exp2f(lowered<S::F16>(ex, m, next));
                 l *= f;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
@@ -767,7 +783,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                 for (int k = 0; k < S::WK - 1; ++k) {
                     const float *from = join + (k * S::WR + wr) * S::LANE_PART * 64 + lane;
-                    const float g = __builtin_amdgcn_exp2f((from[0] - next) * c);
+                    const float g = __builtin_amdgcn_exp2f(lowered<S::F16>(ex, from[0], next));
                     l = fmaf(g, from[64], l);
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
@@ -823,7 +839,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int w = blockIdx.x, wr = blockIdx.y, at = wr * 32 + (lane & 31);
     const JoinRecord r = a.join[w];
-    const float c = exponent_of(a.scale).c;
+    const Exponent ex = exponent_of(a.scale);
     if (wr * 32 >= r.rows) return;
     const int turn = w - r.first - 1;                  // 0: the item's second share
     const bool share = r.last - r.first + 1 > kJoinShared;
@@ -852,7 +868,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
             float best = top;
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) best = fmaxf(best, m[k]);
-            const float f = __builtin_amdgcn_exp2f((top - best) * c);
+            const float f = __builtin_amdgcn_exp2f(lowered<F16>(ex, top, best));
             top = best;
             l *= f;
 #pragma unroll
@@ -860,7 +876,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
 #pragma unroll
             for (int k = 0; k < AT_ONCE; ++k) {
                 if (g0 + k * step > r.last) continue;
-                const float y = __builtin_amdgcn_exp2f((m[k] - best) * c);
+                const float y = __builtin_amdgcn_exp2f(lowered<F16>(ex, m[k], best));
                 l = fmaf(y, x[k], l);
 #pragma unroll
                 for (int i = 0; i < COUNT; ++i)
@@ -891,7 +907,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
     l = 0.0f;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
-        const float f = __builtin_amdgcn_exp2f((shared[k][4 * E][lane] - best) * c);
+        const float f = __builtin_amdgcn_exp2f(lowered<F16>(ex, shared[k][4 * E][lane], best));
         l = fmaf(f, shared[k][4 * E + 1][lane], l);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] = fmaf(f, shared[k][4 * wave + e][lane], x[e]);

@@ -9,6 +9,7 @@ torch = pytest.importorskip("torch")
 
 from paper_2506_04708_amd import synth  # noqa: E402
 from tests import test_serve_ops  # noqa: E402
+from tests.serveref import depths as serveref_depths  # noqa: E402
 from tests.test_serve_ops import BF, HF, Attn, binding, drafts, handle, tree  # noqa: E402,F401
 
 for _n, _deep, _fan in ((20, 5, [4, 2, 2, 1]), (70, 8, [8, 4, 2, 1]), (300, 12, [8, 4, 2, 1]), (1024, 31, [8, 4, 2, 1])):
@@ -167,6 +168,39 @@ def test_attention_of_equal_scores_of_any_size(binding, N, H, G, lens, d, dtype,
                 # equal weights: sums of so many terms in fp32, parts joined, one quotient and the rounding of the result
                 tol = all_v.abs().mean(0) * (len(all_v) + 64) * 2.0 ** -24 * 2 + mean.abs() * half + (2.0 ** -25 if dtype is HF else 0)
                 assert bool(((got[b, u, i] - mean).abs() <= tol).all()), (b, u, i)
+
+
+@pytest.mark.parametrize("size", [2 ** 15, 2 ** 20, 2 ** 21 + 2 ** 20, -(2 ** 21) - 2 ** 20, 2907264, 2907272, -2907264, -2907272, 2 ** 22 + 2 ** 21])
+@pytest.mark.parametrize("N,H,G,n", [(1, 1, 1, 700), (16, 1, 1, 700), (1, 4, 1, 9000), (16, 3, 1, 700), (16, 14, 1, 700), (16, 14, 1, 9000)])
+def test_attention_raises_its_maximum_exactly(binding, N, H, G, n, size):
+    """Many keys of one score and then one of six more, exact numbers both: what the sums so far are scaled by is as exact as a
+    weight, whatever the size of the scores (2^22 / log2(e) lies between two of them)."""
+    for d, dtype in ((64, BF), (128, HF)):
+        t = Attn(binding, 285 + N + H, [n], N, H, G, d, 16, dtype, 1.0)
+        t.scale = 1.0
+        sign, whole, rest = (1 if size > 0 else -1), abs(size) >> 9, abs(size) & 511
+        parts = [whole >> 9, whole & 511]                  # |size| = 512 * (512 * parts[0] + parts[1]) + rest
+        for x in (t.q, t.k, t.kp, t.v, t.vp):
+            x.zero_()
+        t.q[..., 0], t.q[..., 1], t.q[..., 2], t.q[..., 3], t.q[..., 4] = 512.0, 512.0, 1.0, 2.0, 1.0
+        for x in (t.k, t.kp):
+            for e, (y, by) in enumerate(((parts[0], 512), (parts[1], 1))):
+                x[..., e] = sign * float(y) * by           # (whole numbers of at most eight bits, times powers of two: exact in both types)
+            x[..., 2], x[..., 3] = sign * float(rest & 255), sign * float(rest >> 8) * 128.0
+        assert float(t.kp[0, 0, 0, 0, :5].double() @ t.q[0, 0, 0, :5].double()) == size
+        t.vp[..., :] = 1.0
+        t.v[..., :] = 1.0
+        last = (t.table[0, (n - 1) // 16], (n - 1) % 16)
+        t.kp[0][last][:, 4] = 6.0
+        t.vp[0][last] = 0.0
+        deep = serveref_depths(t.parent)
+        got = t.h.tree_attention(**t.on_gpu()).cpu().double()
+        many = torch.tensor(n - 1 + deep + 1.0)[None, :, None, None]      # keys of the one score: the cache's and the path's
+        want = many / (many + np.exp(6.0))
+        # a weight of either kind is off by half a step, the exponent by a rounding of the difference and c's own (six of 2^-24)
+        half = 2.0 ** -8 if dtype is BF else 2.0 ** -11
+        tol = want * (1 - want) * 2 * half + want * (half + (n + 64) * 2.0 ** -23)
+        assert bool(((got - want).abs() <= tol).all()), (float(got.min()), float(got.max()), float(want.min()), float(want.max()))
 
 
 @pytest.mark.parametrize("N,H,G", [(1, 4, 1), (16, 4, 1), (16, 14, 1)])
