@@ -14,7 +14,7 @@ namespace stand {
 // is page * page_size + place in the page.  All strides are in 16-byte words.  A thread copies 16 bytes of a key, then of a value,
 // then the next pair: four to eight of them where there are as many positions, more where a row has more than 1024 words.  Bound by HBM
 // with prompts (751 MB in and out, 16 layers x 4 x 2100 rows of 2 KB: 148 us, 5.1 TB/s).  After a step it is bound by its trips to
-// memory, one behind the other: count, then slot, key and value for each pair, two or three times (5.7 us for 28 layers of 32 short
+// memory, one behind the other: count, then slot, key and value for each pair, two or three times (5.5 us for 28 layers of 32 short
 // paths); the pairs do not depend on each other, but the compiler may not load past a store.
 struct CommitArgs {
     const uint4 *k_rows, *v_rows;

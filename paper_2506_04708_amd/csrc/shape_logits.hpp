@@ -103,9 +103,9 @@ __global__ __launch_bounds__(256) void shape_rows_kernel(ShapeArgs a)
 // once and stay in registers, and so do the mask bits of all its nodes, so that the nodes' rows pass without a barrier between
 // them, kShapeAhead at a time.  In fp32 these are in flight together; in bf16 each is unpacked where it is loaded, so a thread has
 // one row in flight and the other waves of the compute unit have theirs.  What a mask leaves nothing of is not read.  Bound by
-// HBM where there is much to do (2048 rows of 152064: 288 us, 4.5 TB/s): logits in and out, mask bits, counts once for every
-// kShapeNodes nodes; else by the chain nodes -> mask, counts and biases -> rows (16 rows of 32000 in fp32: 5.9 us, 64 rows of 50257:
-// 12 us).  In place, rows that were not drafted are read all the same.
+// HBM where there is much to do (2048 rows of 152064: 289 us, 4.5 TB/s): logits in and out, mask bits, counts once for every
+// kShapeNodes nodes; else by the chain nodes -> mask, counts and biases -> rows (16 rows of 32000 in fp32: 5.8 us, 64 rows of 50257:
+// 11 us).  In place, rows that were not drafted are read all the same.
 constexpr int kShapeNodes = 16, kShapeAhead = 4;
 
 template <int DT>

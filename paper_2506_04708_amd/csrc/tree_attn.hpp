@@ -25,11 +25,11 @@
 // every workgroup the chip holds (attn_plan.hpp); items that were cut are joined by a second kernel.  No sum is made by atomics:
 // the same call gives the same bits.
 //
-// Bound: decoding by HBM (2.04 GB of cache in 353 us, 5.8 TB/s; a torch copy reaches 4.9 counting both ways); larger trees by
+// Bound: decoding by HBM (2.04 GB of cache in 354 us, 5.8 TB/s; a torch copy reaches 4.9 counting both ways); larger trees by
 // what a wave issues between its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128:
-// 130 .. 136 us for 70 GFLOP, 520 .. 540 TFLOP/s on rows as they are, where a large matrix product reaches 1211); alone on a SIMD a
+// 124 .. 134 us for 70 GFLOP, 525 .. 565 TFLOP/s on rows as they are, where a large matrix product reaches 1211); alone on a SIMD a
 // step of 32 keys takes a wave 404 ns, of which its 16 matrix instructions are 262.  Short calls are bound by the chain lengths ->
-// shares -> nodes -> page numbers -> keys, each a trip to memory: 10.3 us, and 2.3 us for the join.
+// shares -> nodes -> page numbers -> keys, each a trip to memory: 10.8 us, and 2.2 us for the join.
 #pragma once
 #include "attn_plan.hpp"
 #include "wave_ops.hpp"
