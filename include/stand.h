@@ -366,7 +366,10 @@ int stand_read_rows(const void *d_src, uint64_t row_bytes, uint64_t rows, uint32
  * which were accepted), so that the host never waits for a length:
  *
  *   stand_cache_pages      lengths move on by what was accepted; pages are taken and given back; slots of the next tokens
+ *   stand_tree_rotate      in every layer: the nodes' queries and keys are normed and rotated by their positions
  *   stand_tree_attention   in every layer: the tree's nodes attend to the cache and to their ancestors in the tree
+ *   stand_cache_append     in every layer, for prompts and single tokens: the same for a row's keys, on their way into the cache
+ *   stand_cache_read       tokens out of the cache, as rows: what a prompt's next part attends to
  *   stand_count_tokens,
  *   stand_shape_logits     penalties, biases and a grammar's masks on the tree's logits, before stand_verify / stand_step
  *   stand_cache_commit     keys and values of the accepted path go to their slots, all layers at once
@@ -381,20 +384,32 @@ int stand_read_rows(const void *d_src, uint64_t row_bytes, uint64_t rows, uint32
  * a tree stay in the caller's buffers until stand_cache_commit; rejected nodes never reach the cache. */
 
 #define STAND_F16 2         /* binary16: caches only, not logits */
+#define STAND_MXFP4 4       /* a cache of 4 bits: this + STAND_BF16 or + STAND_F16, the type of the rows given with it */
 #define STAND_MAX_PAGE 4096 /* tokens of a page, a power of two */
 #define STAND_MAX_CACHED (1 << 30) /* tokens that a row of a block table covers */
 
 /* A paged cache: element e of head g at place s of page p in layer l is d_k[l * layer_stride + p * page_stride + s * slot_stride
  * + g * head_stride + e], d_v likewise.  Strides are in elements, not negative and multiples of 8; pointers are 16-byte aligned.
- * A slot is p * page_size + s. */
+ * A slot is p * page_size + s.
+ *   4 bits (STAND_MXFP4 + the rows' type): strides are multiples of 32 elements, and element e of a head is in the low (e even) or high
+ * half of byte e / 2 from the head's first one: bit 3 the sign, bits 0 .. 2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Each 32 neighbouring elements of a
+ * head share a byte s for the power of two 2^(s - 127) that they are multiplied by (255: they are NaN): block i of that head is d_k_scale[l *
+ * scale_layer_stride + p * scale_page_stride + s * scale_slot_stride + g * scale_head_stride + i].  Those strides are in bytes, not
+ * negative and, like the scales' pointers, multiples of head_dim / 32.  The calls below write s = floor(log2(m)) - 2 + 127 for
+ * the block's largest magnitude m rounded to two significant bits (halfway: up), at least 2 and at most 252 with bf16 rows, 104 and 140 with fp16 ones, and
+ * each element as the nearest one (halfway: the one with bit 0 clear; above 6: 6); a block with an infinity or a NaN gets s = 255.  Scales
+ * of other origin keep to those limits: past them products may not be numbers of the rows' type.
+ *   The members from d_k_scale on are read for caches of 4 bits alone. */
 typedef struct {
     void *d_k, *d_v;
-    int32_t dtype;      /* STAND_BF16 or STAND_F16, also that of the rows given with it */
+    int32_t dtype;      /* STAND_BF16 or STAND_F16, also that of the rows given with it; or STAND_MXFP4 + that */
     int32_t layers, pages;
     int32_t page_size;  /* a power of two <= STAND_MAX_PAGE */
     int32_t kv_heads;   /* <= 4096 */
     int32_t head_dim;   /* 64 or 128 */
     int64_t layer_stride, page_stride, slot_stride, head_stride;
+    void *d_k_scale, *d_v_scale;
+    int64_t scale_layer_stride, scale_page_stride, scale_slot_stride, scale_head_stride;
 } stand_cache;
 
 /* Queries, keys, values and outputs of the tree's nodes in one layer: strides of batch, node and head in elements, not
@@ -419,8 +434,8 @@ typedef struct {
  * that a row sees is infinite or NaN, that element of its output is one of the two (which is not specified); a product
  * query . key (summed in fp32, before the scale) that is neither finite nor -infinity makes the row NaN, and so does a row of nothing
  * but -infinity; finite ones of any size do not.  A drafted node's ancestors are drafted.
- *   Keys (and values) of one layer span less than 64 GiB (STAND_ELIMIT).
- *   Products are summed in fp32, the weights p are rounded to the cache's type for the product with the values and summed as
+ *   Keys (and values) of one layer span less than 64 GiB, their scales less than 2^32 times head_dim / 32 bytes (STAND_ELIMIT).
+ *   Products are summed in fp32, the weights p are rounded to the rows' type (a cache's 4 bits are, without loss) for the product with the values and summed as
  * rounded; the result is rounded once.  A weight's error is half a step of its type: up to 2^-8 of it in bf16, 2^-11 in fp16, and in
  * fp16 not less than 2^-31 of the row's largest weight, so that n far smaller ones together may be off by n * 2^-31 of that one.
  *   d_work: 16-byte aligned device memory of stand_tree_attention_work bytes, used from the call's start to its end on the
@@ -441,11 +456,68 @@ typedef struct {
 
 /* Rows into the cache: for all layers, trajectories b and j < d_count[b], row d_row[b][j] of trajectory b goes to slot
  * d_slots[b][j] (stand_cache_pages).  After a verification d_row is d_out_node and d_count is d_out_len (width = depth + 1); a
- * prompt's rows go in as they stand with d_row NULL (row j).  d_count NULL: `width` each.  A negative slot or row (or one past
+ * prompt's rows go in as they stand with d_row NULL (row j).  Into a cache of 4 bits they go as described at stand_cache.  d_count NULL: `width` each.  A negative slot or row (or one past
  * the end) is left out.  d_slots, d_row: [B][width].  The slots of a call differ from each other (where they do not, what
  * ends up there is not specified); the rows do not overlap the cache. */
 int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots, int32_t width,
                        const int32_t *d_row, const int32_t *d_count, void *stream);
+
+/* Rows for the tokens of a cache, written: as stand_cache_rows. */
+typedef struct {
+    void *d_k, *d_v;
+    int32_t rows;
+    int64_t layer_stride, batch_stride, row_stride, head_stride;
+} stand_cache_rows_out;
+
+/* Tokens out of the cache: for the layers first_layer .. first_layer + layers - 1, trajectories b and j < d_count[b] (NULL, or where
+ * it is more: rows->rows), keys and values of token d_start[b] + j (NULL: token j) go to row j, of 4 bits as the numbers of the rows' type that they
+ * stand for, exactly.  Token t is in page d_table[b][t / page_size]; one outside the table, or in a page outside the cache, is
+ * zeros.  Rows from d_count[b] on are left as they were.  The rows do not overlap the cache. */
+int stand_cache_read(stand_handle *h, const stand_cache *cache, int32_t first_layer, int32_t layers, const int32_t *d_table, int32_t table_width,
+                     const int32_t *d_start, const int32_t *d_count, const stand_cache_rows_out *rows, void *stream);
+
+/* ---- norms of heads and rotation by positions ----
+ *
+ * A head x of a row at position p becomes
+ *     y = w x / sqrt(mean(x^2) + eps)                                                   (without weights w: y = x)
+ *     y[i], y[j] <- y[i] cos - y[j] sin, y[i] sin + y[j] cos      for the pairs i < dims / 2
+ * with cos = d_turns[p][i], sin = d_turns[p][dims / 2 + i] and (i, j) = (i, i + dims / 2), or (2 i, 2 i + 1) with `neighbours`; elements from dims
+ * on are not rotated.  Computed in fp64, rounded to fp32 and from there to the rows' type or to 4 bits.  A position outside the
+ * table makes the head's rotated elements NaN. */
+typedef struct {
+    const float *d_turns;            /* [positions][dims], 16-byte aligned; may be NULL with dims 0 */
+    int32_t positions, dims;         /* dims: a multiple of 16, at most the head's elements; 0: no rotation */
+    int32_t neighbours;              /* how pairs stand: 0: half of dims apart, else side by side */
+    float eps;                       /* of the norms, not negative, finite */
+    const void *d_q_norm, *d_k_norm; /* weights [head_dim], type of the rows, 16-byte aligned; NULL: no norm */
+} stand_rotation;
+
+/* Queries, keys and (where a call takes them) values of `rows` rows of each trajectory, strides as in stand_tree_rows.  An output
+ * may be its input with the same strides (in place); otherwise outputs overlap no input.  d_q NULL: no queries.  d_k_out NULL: the keys go
+ * to the cache alone. */
+typedef struct {
+    const void *d_q, *d_k, *d_v;
+    void *d_q_out, *d_k_out;
+    int32_t dtype;                   /* STAND_BF16 or STAND_F16 */
+    int32_t rows, q_heads, kv_heads; /* q_heads: any number where there are queries */
+    int32_t head_dim;                /* 64 or 128 */
+    int64_t q_stride[3], k_stride[3], v_stride[3], q_out_stride[3], k_out_stride[3];
+} stand_turned_rows;
+
+/* Queries and keys of the drafted nodes, before stand_tree_attention: node u of trajectory b stands at position d_len[b] +
+ * depth(u).  rows->rows is the tree's number of nodes, rows->d_v is not used, d_k and d_k_out are needed.  Rows of nodes that were not drafted
+ * are left as they were. */
+int stand_tree_rotate(stand_handle *h, const stand_rotation *rotation, const int32_t *d_len, const int32_t *d_draft_tok,
+                      const stand_turned_rows *rows, void *stream);
+
+/* Rows of prompts, or single tokens, into one layer of a cache.  For trajectory b and j < d_count[b] (NULL, or where it is more:
+ * rows->rows), row j stands at position d_start[b] + j (NULL: j); its keys, normed and rotated, and its values, as they are, go to
+ * slot d_slots[b][j] (stand_cache_pages), its queries, normed and rotated, to d_q_out, its keys also to d_k_out where there is one.  With a negative slot
+ * (or one past the end) keys and values do not go to the cache.  rotation NULL: rows as they are.  d_slots: [B][width], width >= rows->rows.  rows->dtype,
+ * kv_heads and head_dim are the cache's.  Rows from d_count[b] on are not read and, as outputs, left as they were.  The slots of a
+ * call differ from each other. */
+int stand_cache_append(stand_handle *h, const stand_cache *cache, int32_t layer, const stand_rotation *rotation, const stand_turned_rows *rows,
+                       const int32_t *d_start, const int64_t *d_slots, int32_t width, const int32_t *d_count, void *stream);
 
 /* The pages of a cache.  Free pages stand in a ring: entries mark[0] .. mark[1] - 1, modulo `pages`; a new cache has every page
  * in the ring, mark = {0, pages}, and all lengths and held counts 0.  d_table rows are valid up to d_held[b] entries. */

@@ -14,7 +14,7 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libstand.so")
 
-STAND_BF16, STAND_F32, STAND_F16 = 0, 1, 2
+STAND_BF16, STAND_F32, STAND_F16, STAND_MXFP4 = 0, 1, 2, 4
 DRAFT_GUMBEL_TOPK, DRAFT_MULTINOMIAL, DRAFT_DETERMINISTIC = 0, 1, 2
 MERGE_MEAN, MERGE_REPLACE = 0, 1
 STEP_AUTO, STEP_SERIAL, STEP_FUSED = 0, 1, 2
@@ -31,6 +31,7 @@ EXPORTED = [
     "stand_get_record_slots",
     "stand_tree_attention", "stand_tree_attention_work", "stand_cache_commit", "stand_cache_pages", "stand_shape_logits",
     "stand_shape_logits_work",    "stand_count_tokens",
+    "stand_tree_rotate", "stand_cache_append", "stand_cache_read",
 ]
 
 
@@ -58,12 +59,23 @@ class CacheDesc(C.Structure):
         ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("dtype", C.c_int32), ("layers", C.c_int32), ("pages", C.c_int32),
         ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("layer_stride", C.c_int64),
         ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
+        ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p), ("scale_layer_stride", C.c_int64), ("scale_page_stride", C.c_int64),
+        ("scale_slot_stride", C.c_int64), ("scale_head_stride", C.c_int64),
     ]
 
 
-# stand_tree_rows and stand_cache_rows, filled in anew by every call (a ctypes structure takes three times as long)
+class RotationDesc(C.Structure):
+    _fields_ = [
+        ("d_turns", C.c_void_p), ("positions", C.c_int32), ("dims", C.c_int32), ("neighbours", C.c_int32), ("eps", C.c_float),
+        ("d_q_norm", C.c_void_p), ("d_k_norm", C.c_void_p),
+    ]
+
+
+# stand_tree_rows, stand_cache_rows (and stand_cache_rows_out) and stand_turned_rows, filled in anew by every call (a ctypes structure
+# takes three times as long)
 _TREE_ROWS = struct.Struct("@4Pif12q")
 _CACHE_ROWS = struct.Struct("@2Pi4x4q")
+_TURNED_ROWS = struct.Struct("@5P5i4x15q")
 
 
 class PagesDesc(C.Structure):
@@ -120,6 +132,9 @@ def load_library():
     lib.stand_shape_logits_work.argtypes = [vp]
     lib.stand_shape_logits_work.restype = C.c_uint64
     lib.stand_count_tokens.argtypes = [vp, vp, vp, vp, C.c_int32, C.c_int32, vp]
+    lib.stand_tree_rotate.argtypes = [vp, vp, vp, vp, vp, vp]
+    lib.stand_cache_append.argtypes = [vp, vp, C.c_int32, vp, vp, vp, vp, C.c_int32, vp, vp]
+    lib.stand_cache_read.argtypes = [vp, vp, C.c_int32, C.c_int32, vp, C.c_int32, vp, vp, vp, vp]
     lib.stand_strerror.restype = C.c_char_p
     lib.stand_strerror.argtypes = [C.c_int]
     lib.stand_last_hip_error.argtypes = [vp]
@@ -227,15 +242,55 @@ _HALF = {torch.bfloat16: STAND_BF16, torch.float16: STAND_F16}
 
 
 class PagedCache:
-    """Keys and values of a paged cache: tensors indexed [layer, page, place, head, element], any strides but for the last."""
+    """Keys and values of a paged cache: tensors indexed [layer, page, place, head, element], any strides but for the last.  In 4 bits: bytes
+    of two elements [.., d / 2] with their blocks' scales [.., d / 32], also bytes, and the type of the rows given with the cache."""
 
-    def __init__(self, k, v):
+    def __init__(self, k, v, k_scale=None, v_scale=None, dtype=None):
         assert k.dim() == 5 and k.shape == v.shape and k.stride() == v.stride() and k.dtype == v.dtype and k.device == v.device
-        assert k.is_cuda and k.dtype in _HALF and k.stride(4) == 1
-        self.k, self.v = k, v
-        self.dtype, self.index, (self.layers, self.pages, self.page_size, self.heads, self.dim) = k.dtype, k.get_device(), k.shape
-        self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), _HALF[k.dtype], *k.shape, *k.stride()[:4])
+        assert k.is_cuda and k.stride(4) == 1 and (k_scale is None) == (v_scale is None) == (dtype is None)
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+        self.index, (self.layers, self.pages, self.page_size, self.heads, self.dim) = k.get_device(), k.shape
+        if k_scale is None:
+            assert k.dtype in _HALF
+            self.dtype = k.dtype
+            self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), _HALF[k.dtype], *k.shape, *k.stride()[:4])
+        else:
+            assert k.dtype is k_scale.dtype is v_scale.dtype is torch.uint8 and dtype in _HALF
+            self.dtype, self.dim = dtype, 2 * self.dim
+            assert k_scale.shape == v_scale.shape == (*k.shape[:4], self.dim // 32) and k_scale.stride() == v_scale.stride() and k_scale.stride(4) == 1
+            assert k_scale.device == v_scale.device == k.device
+            self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), STAND_MXFP4 + _HALF[dtype], *k.shape[:4], self.dim, *(2 * s for s in k.stride()[:4]),
+                                  k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride()[:4])
         self.ref = C.addressof(self.desc)
+
+    @classmethod
+    def new4(cls, layers, pages, page_size, heads, dim, dtype=torch.bfloat16, device="cuda"):
+        """An empty cache of 4 bits, to be given rows of `dtype`."""
+        k, v = (torch.zeros((layers, pages, page_size, heads, dim // 2), dtype=torch.uint8, device=device) for _ in range(2))
+        ks, vs = (torch.full((layers, pages, page_size, heads, dim // 32), 127, dtype=torch.uint8, device=device) for _ in range(2))
+        return cls(k, v, ks, vs, dtype)
+
+
+class Rotation:
+    """Rotation of heads by positions, and norms of heads before it (stand_rotation): turns [positions, dims] fp32, cosines of the dims / 2
+    pairs, then their sines (None: no rotation); pairs "halves" (dims / 2 apart) or "neighbours"; weights [d] of the rows' type or None."""
+
+    def __init__(self, turns=None, pairs="halves", q_norm=None, k_norm=None, eps=1e-6):
+        assert pairs in ("halves", "neighbours") and (turns is None or (turns.dim() == 2 and turns.dtype is torch.float32 and turns.is_contiguous()))
+        some = [t for t in (turns, q_norm, k_norm) if t is not None]
+        norms = [t for t in (q_norm, k_norm) if t is not None]
+        assert all(t.is_cuda and t.device == some[0].device for t in some)
+        assert all(t.dim() == 1 and t.is_contiguous() and t.dtype is norms[0].dtype and t.shape == norms[0].shape for t in norms)
+        self.turns, self.q_norm, self.k_norm = turns, q_norm, k_norm
+        self.index = some[0].get_device() if some else None
+        self.dtype, self.dim = (norms[0].dtype, norms[0].shape[0]) if norms else (None, None)
+        positions, dims = (0, 0) if turns is None else turns.shape
+        self.desc = RotationDesc(None if turns is None else turns.data_ptr(), positions, dims, int(pairs == "neighbours"), eps,
+                                 *(None if t is None else t.data_ptr() for t in (q_norm, k_norm)))
+        self.ref = C.addressof(self.desc)
+
+    def fits(self, dtype, dim, index):
+        return self.index in (None, index) and (self.dtype is None or (self.dtype is dtype and self.dim == dim))
 
 
 class Pages:
@@ -457,6 +512,62 @@ class Stand:
         desc = _CACHE_ROWS.pack(k.data_ptr(), v.data_ptr(), rows, *stride[:4])
         _check(self._lib.stand_cache_commit(self.h, cache.ref, desc, self._arg(slots, torch.int64), slots.shape[1],
                                             self._arg(row, torch.int32), self._arg(count, torch.int32), self._stream()), self.h)
+
+    def _turned(self, dtype, q, k, v, q_out, k_out):
+        """stand_turned_rows of k [B, rows, kv heads, d] and what goes with it."""
+        B, rows, heads, d = k.shape
+        assert dtype in _HALF and B == self.B and k.get_device() == self._index
+        assert k.dtype is dtype and (v is None or v.shape == k.shape)
+        assert (q is None) == (q_out is None) and (q is None or (q.shape == q_out.shape and q.shape[:2] == (B, rows) and q.shape[3] == d))
+        assert k_out is None or k_out.shape == k.shape
+        ptr, strides = [], []
+        for t in (q, k, v, q_out, k_out):
+            if t is None:
+                ptr.append(0)
+                strides += (0, 0, 0)
+                continue
+            s0, s1, s2, s3 = t.stride()
+            assert s3 == 1 and t.dtype is dtype and t.get_device() == self._index
+            ptr.append(t.data_ptr())
+            strides += (s0, s1, s2)
+        return _TURNED_ROWS.pack(*ptr, _HALF[dtype], rows, 0 if q is None else q.shape[2], heads, d, *strides)
+
+    def tree_rotate(self, rotation, length, draft_tok, q, k, q_out=None, k_out=None):
+        """Queries q [B, N, heads, d] and keys k [B, N, kv heads, d] of the drafted nodes normed and rotated by their positions; an
+        output that is None is the input."""
+        q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
+        assert k.shape[1] == self.N and length.shape == (self.B,) and draft_tok.shape == (self.B, self.N)
+        assert rotation.fits(k.dtype, k.shape[3], self._index)
+        desc = self._turned(k.dtype, q, k, None, q_out, k_out)
+        _check(self._lib.stand_tree_rotate(self.h, rotation.ref, self._arg(length, torch.int32), self._arg(draft_tok, torch.int32), desc,
+                                           self._stream()), self.h)
+        return q_out, k_out
+
+    def cache_append(self, cache, layer, k, v, slots, start=None, count=None, rotation=None, q=None, q_out=None, k_out=None):
+        """Rows k, v [B, rows, kv heads, d] into one layer of the cache: row j < count[b] (None: all) at position start[b] + j, to slot
+        slots[b][j], its key normed and rotated; queries q [B, rows, heads, d] along with them into q_out (None: in place)."""
+        q_out = q if q_out is None else q_out
+        assert slots.dim() == 2 and slots.shape[0] == self.B and slots.shape[1] >= k.shape[1] and k.shape[2] == cache.heads and k.shape[3] == cache.dim
+        assert (start is None or start.shape == (self.B,)) and (count is None or count.shape == (self.B,)) and self._index == cache.index
+        assert rotation is None or rotation.fits(k.dtype, k.shape[3], self._index)
+        desc = self._turned(cache.dtype, q, k, v, q_out, k_out)
+        _check(self._lib.stand_cache_append(self.h, cache.ref, layer, None if rotation is None else rotation.ref, desc, self._arg(start, torch.int32),
+                                            self._arg(slots, torch.int64), slots.shape[1], self._arg(count, torch.int32), self._stream()), self.h)
+        return q_out
+
+    def cache_read(self, cache, table, k, v, count=None, start=None, layer=0):
+        """Tokens start[b] + j (None: j), j < count[b] (None: all rows), of the layers from `layer` on into rows k, v
+        [layers, B, rows, kv heads, d]."""
+        layers, B, rows, heads, d = k.shape
+        stride = k.stride()
+        assert k.shape == v.shape and stride == v.stride() and stride[4] == 1 and cache.dtype is k.dtype and cache.dtype is v.dtype
+        assert B == self.B and heads == cache.heads and d == cache.dim and table.dim() == 2 and table.shape[0] == B
+        assert (count is None or count.shape == (B,)) and (start is None or start.shape == (B,))
+        assert self._index == cache.index == k.get_device() == v.get_device()
+        desc = _CACHE_ROWS.pack(k.data_ptr(), v.data_ptr(), rows, *stride[:4])
+        _check(self._lib.stand_cache_read(self.h, cache.ref, layer, layers, self._arg(table, torch.int32), table.shape[1], self._arg(start, torch.int32),
+                                          self._arg(count, torch.int32), desc, self._stream()), self.h)
+        return k, v
 
     def cache_pages(self, pages, add=None, room=None, slots=None, missing=None, out=None):
         """Moves lengths on by add, takes and gives back pages for room more tokens (None: a whole path); slots [B, any] and

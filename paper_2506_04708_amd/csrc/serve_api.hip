@@ -1,6 +1,8 @@
 // serve_api.hip -- host side of the operators around a verification (include/stand.h): argument checks and launches.
 // Nothing here allocates, waits or keeps state between calls; everything a call needs comes with it.
+#include "cache_four.hpp"
 #include "cache_ops.hpp"
+#include "row_turns.hpp"
 #include "serve_checks.hpp"
 #include "serve_view.hpp"
 #include "shape_logits.hpp"
@@ -53,20 +55,80 @@ int bad_device(const ServeView &v, hipError_t e)
 enum AttnForm { kAttn32, kAttn64, kAttnMore };
 AttnForm attn_form(int64_t rows) { return rows <= 32 ? kAttn32 : rows <= 64 ? kAttn64 : kAttnMore; }
 
-template <int D, bool F16, typename Call>
+template <int D, bool F16, bool FOUR, typename Call>
 auto with_attn_shape(AttnForm f, Call call)
 {
     switch (f) {
-    case kAttn32: return call(AttnShape<D, F16, 1, 4, 1>{});
-    case kAttn64: return call(AttnShape<D, F16, 2, 2, 1>{});
-    default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2>{});
+    case kAttn32: return call(AttnShape<D, F16, 1, 4, 1, FOUR>{});
+    case kAttn64: return call(AttnShape<D, F16, 2, 2, 1, FOUR>{});
+    default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2, FOUR>{});
     }
 }
 template <typename Call>
-auto with_attn_shape(int head_dim, bool f16, AttnForm f, Call call)
+auto with_attn_shape(const stand_cache *c, AttnForm f, Call call)
 {
-    if (head_dim == 64) return f16 ? with_attn_shape<64, true>(f, call) : with_attn_shape<64, false>(f, call);
-    return f16 ? with_attn_shape<128, true>(f, call) : with_attn_shape<128, false>(f, call);
+    auto of_type = [&](auto f16, auto four) {
+        constexpr bool F16 = decltype(f16)::value, FOUR = decltype(four)::value;
+        return c->head_dim == 64 ? with_attn_shape<64, F16, FOUR>(f, call) : with_attn_shape<128, F16, FOUR>(f, call);
+    };
+    using Yes = std::true_type;
+    using No = std::false_type;
+    if (of_four(c)) return rows_dtype(c) == STAND_F16 ? of_type(Yes{}, Yes{}) : of_type(No{}, Yes{});
+    return rows_dtype(c) == STAND_F16 ? of_type(Yes{}, No{}) : of_type(No{}, No{});
+}
+
+// The cache as kernels that count in 16-byte chunks see it.
+CachePlaces places_of(const stand_cache *c)
+{
+    CachePlaces p;
+    const int64_t chunk = of_four(c) ? 32 : 8;
+    p.k = (char *)c->d_k; p.v = (char *)c->d_v;
+    p.layer = c->layer_stride / chunk; p.page = c->page_stride / chunk; p.slot = c->slot_stride / chunk; p.head = c->head_stride / chunk;
+    p.k_scale = p.v_scale = nullptr;
+    p.scale_layer = p.scale_page = p.scale_slot = p.scale_head = 0;
+    if (of_four(c)) {
+        p.k_scale = (uint8_t *)c->d_k_scale; p.v_scale = (uint8_t *)c->d_v_scale;
+        p.scale_layer = c->scale_layer_stride; p.scale_page = c->scale_page_stride; p.scale_slot = c->scale_slot_stride;
+        p.scale_head = c->scale_head_stride;
+    }
+    p.page_shift = log2_of(c->page_size); p.pages = c->pages;
+    return p;
+}
+
+// The kernel's view of the rows of stand_tree_rotate and stand_cache_append; -> workgroups of a trajectory.
+unsigned turn_args(TurnArgs &a, const stand_rotation *rotation, const stand_turned_rows *rows, bool values)
+{
+    a.q = (const uint16_t *)rows->d_q; a.k = (const uint16_t *)rows->d_k; a.v = (const uint16_t *)rows->d_v;
+    a.q_out = (uint16_t *)rows->d_q_out; a.k_out = (uint16_t *)rows->d_k_out;
+    for (int i = 0; i < 3; ++i) {
+        a.qs[i] = rows->q_stride[i]; a.ks[i] = rows->k_stride[i]; a.vs[i] = rows->v_stride[i];
+        a.qos[i] = rows->q_out_stride[i]; a.kos[i] = rows->k_out_stride[i];
+    }
+    a.turns = nullptr; a.q_norm = a.k_norm = nullptr; a.eps = 0.0; a.positions = a.half = a.neighbours = 0;
+    if (rotation) {
+        a.turns = rotation->d_turns; a.positions = rotation->positions; a.half = rotation->dims / 2; a.neighbours = rotation->neighbours != 0;
+        a.q_norm = (const uint16_t *)rotation->d_q_norm; a.k_norm = (const uint16_t *)rotation->d_k_norm; a.eps = rotation->eps;
+    }
+    a.rows = rows->rows; a.q_heads = rows->q_heads; a.kv_heads = rows->kv_heads;
+    a.q_groups = a.q ? (int)turn_groups(rows->rows, rows->q_heads, rows->head_dim) : 0;
+    a.k_groups = (int)turn_groups(rows->rows, rows->kv_heads, rows->head_dim);
+    a.tok = nullptr; a.anc = nullptr; a.anc_words = 0; a.start = a.count = nullptr;
+    a.slots = nullptr; a.width = 0; a.slot_count = 0;
+    return (unsigned)(a.q_groups + (values ? 2 : 1) * a.k_groups);
+}
+template <TurnTarget TO>
+void turn_launch(const TurnArgs &a, const stand_turned_rows *rows, unsigned groups, int B, hipStream_t s)
+{
+    const dim3 grid(groups, (unsigned)B), threads(kTurnThreads);
+    const bool f16 = rows->dtype == STAND_F16;
+    static_assert(turn_heads_of_group(64) == 64 && turn_heads_of_group(128) == 32, "turn_groups() counts with these");
+    if (rows->head_dim == 64) {
+        if (f16) row_turns_kernel<64, true, TO><<<grid, threads, 0, s>>>(a);
+        else row_turns_kernel<64, false, TO><<<grid, threads, 0, s>>>(a);
+    } else {
+        if (f16) row_turns_kernel<128, true, TO><<<grid, threads, 0, s>>>(a);
+        else row_turns_kernel<128, false, TO><<<grid, threads, 0, s>>>(a);
+    }
 }
 
 // Workgroups of a launch: as many as the device holds at once, a multiple of its eight XCDs; 0: the device refused.  (Above
@@ -118,7 +180,7 @@ extern "C" uint64_t stand_tree_attention_work(const stand_handle *h, const stand
     const ServeView v = serve_view(const_cast<stand_handle *>(h));
     if (check_attention_size(v.B, cache, q_heads) != STAND_OK) return 0;
     const AttnForm f = attn_form((int64_t)v.N * (q_heads / cache->kv_heads));
-    return with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, f,
+    return with_attn_shape(cache, f,
                            [&](auto s) { return attn_work_bytes<decltype(s)>(attn_groups_of<decltype(s)>(v)); });
 }
 
@@ -133,8 +195,16 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     TreeAttnArgs a;
     a.q = (const uint16_t *)rows->d_q; a.k_new = (const uint16_t *)rows->d_k; a.v_new = (const uint16_t *)rows->d_v;
     a.out = (uint16_t *)rows->d_out;
-    a.k_pool = (const uint16_t *)cache->d_k + layer * cache->layer_stride;
-    a.v_pool = (const uint16_t *)cache->d_v + layer * cache->layer_stride;
+    const bool four = of_four(cache);
+    a.k_pool = (const uint16_t *)cache->d_k + layer * cache->layer_stride / (four ? 4 : 1);
+    a.v_pool = (const uint16_t *)cache->d_v + layer * cache->layer_stride / (four ? 4 : 1);
+    a.k_scale = a.v_scale = nullptr;
+    a.scale_page = a.scale_slot = a.scale_head = 0;
+    if (four) {
+        a.k_scale = (const uint8_t *)cache->d_k_scale + layer * cache->scale_layer_stride;
+        a.v_scale = (const uint8_t *)cache->d_v_scale + layer * cache->scale_layer_stride;
+        a.scale_page = cache->scale_page_stride; a.scale_slot = cache->scale_slot_stride; a.scale_head = cache->scale_head_stride;
+    }
     a.len = d_len; a.table = d_table; a.draft_tok = d_draft_tok;
     a.anc = (const uint32_t *)v.anc; a.anc_words = 2 * v.anc_words;      // (little endian: words of 32 nodes)
     a.join = (JoinRecord *)d_work;
@@ -144,7 +214,7 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     a.pool_page = cache->page_stride; a.pool_slot = cache->slot_stride; a.pool_head = cache->head_stride;
     a.scale = rows->scale; a.B = v.B; a.N = v.N; a.kv_heads = cache->kv_heads; a.per_kv = rows->q_heads / cache->kv_heads;
     a.width = table_width; a.pages = cache->pages; a.page_shift = log2_of(cache->page_size);
-    return with_attn_shape(cache->head_dim, cache->dtype == STAND_F16, attn_form((int64_t)v.N * a.per_kv), [&](auto s) {
+    return with_attn_shape(cache, attn_form((int64_t)v.N * a.per_kv), [&](auto s) {
         using S = decltype(s);
         a.groups = attn_groups_of<S>(v);
         if (a.groups == 0) return STAND_EHIP;
@@ -163,6 +233,25 @@ extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, con
     const ServeView v = serve_view(h);
     const int refused = check_cache_commit(v.B, cache, rows, d_slots, width);
     if (refused) return refused;
+    if (of_four(cache)) {
+        CommitFourArgs a;
+        a.units = cache->head_dim / 16;
+        a.heads = cache->kv_heads;
+        a.per_group = commit_per_group(a.heads * a.units);
+        const int64_t groups = commit_groups(width, a.per_group);
+        const DeviceScope scope(v.device);
+        if (scope.e != hipSuccess) return bad_device(v, scope.e);
+        a.k_rows = (const uint4 *)rows->d_k; a.v_rows = (const uint4 *)rows->d_v;
+        a.to = places_of(cache);
+        a.slots = d_slots; a.row = d_row; a.count = d_count;
+        a.src_layer = rows->layer_stride / 8; a.src_batch = rows->batch_stride / 8; a.src_row = rows->row_stride / 8; a.src_head = rows->head_stride / 8;
+        a.slot_count = (long long)cache->pages << a.to.page_shift;
+        a.rows = rows->rows; a.width = width;
+        const dim3 grid((unsigned)groups, (unsigned)v.B, (unsigned)cache->layers), threads(kCommitThreads);
+        if (rows_dtype(cache) == STAND_F16) cache_commit4_kernel<true><<<grid, threads, 0, (hipStream_t)stream>>>(a);
+        else cache_commit4_kernel<false><<<grid, threads, 0, (hipStream_t)stream>>>(a);
+        return launched(v);
+    }
     CommitArgs a;
     a.words = cache->head_dim / 8;
     a.heads = cache->kv_heads;
@@ -180,6 +269,71 @@ extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, con
     a.slot_count = (long long)cache->pages << a.page_shift;
     a.B = v.B; a.rows = rows->rows; a.width = width;
     cache_commit_kernel<<<dim3((unsigned)groups, (unsigned)v.B, (unsigned)cache->layers), dim3(kCommitThreads), 0, (hipStream_t)stream>>>(a);
+    return launched(v);
+}
+
+extern "C" int stand_cache_read(stand_handle *h, const stand_cache *cache, int32_t first_layer, int32_t layers, const int32_t *d_table,
+                                int32_t table_width, const int32_t *d_start, const int32_t *d_count, const stand_cache_rows_out *rows, void *stream)
+{
+    if (!h) return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    const int refused = check_cache_read(v.B, cache, first_layer, layers, d_table, table_width, rows);
+    if (refused) return refused;
+    ReadArgs a;
+    a.units = cache->head_dim / 16;
+    a.heads = cache->kv_heads;
+    a.per_group = commit_per_group(a.heads * a.units);
+    const int64_t groups = commit_groups(rows->rows, a.per_group);
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    a.k_rows = (uint4 *)rows->d_k; a.v_rows = (uint4 *)rows->d_v;
+    a.from = places_of(cache);
+    a.table = d_table; a.start = d_start; a.count = d_count;
+    a.dst_layer = rows->layer_stride / 8; a.dst_batch = rows->batch_stride / 8; a.dst_row = rows->row_stride / 8; a.dst_head = rows->head_stride / 8;
+    a.first_layer = first_layer; a.rows = rows->rows; a.width = table_width;
+    const dim3 grid((unsigned)groups, (unsigned)v.B, (unsigned)layers), threads(kCommitThreads);
+    if (!of_four(cache)) cache_read_kernel<kRead16><<<grid, threads, 0, (hipStream_t)stream>>>(a);
+    else if (rows_dtype(cache) == STAND_F16) cache_read_kernel<kReadF16><<<grid, threads, 0, (hipStream_t)stream>>>(a);
+    else cache_read_kernel<kReadBf16><<<grid, threads, 0, (hipStream_t)stream>>>(a);
+    return launched(v);
+}
+
+extern "C" int stand_tree_rotate(stand_handle *h, const stand_rotation *rotation, const int32_t *d_len, const int32_t *d_draft_tok,
+                                 const stand_turned_rows *rows, void *stream)
+{
+    if (!h) return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    const int refused = check_tree_rotate(v.B, v.N, rotation, d_len, d_draft_tok, rows);
+    if (refused) return refused;
+    TurnArgs a;
+    const unsigned groups = turn_args(a, rotation, rows, false);
+    a.start = d_len; a.tok = d_draft_tok; a.anc = v.anc; a.anc_words = v.anc_words;
+    a.to = CachePlaces{};
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    turn_launch<kTurnRows>(a, rows, groups, v.B, (hipStream_t)stream);
+    return launched(v);
+}
+
+extern "C" int stand_cache_append(stand_handle *h, const stand_cache *cache, int32_t layer, const stand_rotation *rotation,
+                                  const stand_turned_rows *rows, const int32_t *d_start, const int64_t *d_slots, int32_t width,
+                                  const int32_t *d_count, void *stream)
+{
+    if (!h) return STAND_EINVAL;
+    const ServeView v = serve_view(h);
+    const int refused = check_cache_append(v.B, cache, layer, rotation, rows, d_slots, width);
+    if (refused) return refused;
+    TurnArgs a;
+    const unsigned groups = turn_args(a, rotation, rows, true);
+    a.start = d_start; a.count = d_count; a.slots = d_slots; a.width = width;
+    a.to = places_of(cache);
+    a.to.k += layer * a.to.layer * 16; a.to.v += layer * a.to.layer * 16;
+    if (a.to.k_scale) { a.to.k_scale += layer * a.to.scale_layer; a.to.v_scale += layer * a.to.scale_layer; }
+    a.slot_count = (long long)cache->pages << a.to.page_shift;
+    const DeviceScope scope(v.device);
+    if (scope.e != hipSuccess) return bad_device(v, scope.e);
+    if (of_four(cache)) turn_launch<kTurnCache4>(a, rows, groups, v.B, (hipStream_t)stream);
+    else turn_launch<kTurnCache16>(a, rows, groups, v.B, (hipStream_t)stream);
     return launched(v);
 }
 

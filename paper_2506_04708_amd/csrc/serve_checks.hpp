@@ -5,6 +5,7 @@
 #include "attn_plan.hpp"
 
 #include <cmath>
+#include <cstring>
 
 namespace stand {
 
@@ -22,18 +23,30 @@ inline int log2_of(int64_t x)
     return s;
 }
 
-inline bool cache_ok(const stand_cache *c)
+inline bool of_four(const stand_cache *c) { return c->dtype == STAND_MXFP4 + STAND_BF16 || c->dtype == STAND_MXFP4 + STAND_F16; }
+inline int rows_dtype(const stand_cache *c) { return of_four(c) ? c->dtype - STAND_MXFP4 : c->dtype; }
+// Scales of a cache of 4 bits: a head's stand together.
+inline bool scales_ok(const stand_cache *c)
 {
-    return c && c->d_k && c->d_v && aligned16(c->d_k) && aligned16(c->d_v) && (c->dtype == STAND_BF16 || c->dtype == STAND_F16) &&
-           c->layers >= 1 && c->pages >= 1 && page_size_ok(c->page_size) && c->kv_heads >= 1 && c->kv_heads <= 4096 &&
-           (c->head_dim == 64 || c->head_dim == 128) && stride_ok(c->layer_stride) && stride_ok(c->page_stride) &&
-           stride_ok(c->slot_stride) && stride_ok(c->head_stride);
+    const int64_t unit = c->head_dim / 32;
+    auto ok = [&](int64_t s) { return s >= 0 && s % unit == 0 && s < ((int64_t)1 << 48); };
+    return c->d_k_scale && c->d_v_scale && (uintptr_t)c->d_k_scale % unit == 0 && (uintptr_t)c->d_v_scale % unit == 0 && ok(c->scale_layer_stride) &&
+           ok(c->scale_page_stride) && ok(c->scale_slot_stride) && ok(c->scale_head_stride) && c->layer_stride % 32 == 0 &&
+           c->page_stride % 32 == 0 && c->slot_stride % 32 == 0 && c->head_stride % 32 == 0;
 }
 
-// Whether places (x, y) up to these lie less than 2^32 chunks of eight elements from the first one (x, y < 2^31).
-inline bool spans_chunks(int64_t x, int64_t x_stride, int64_t y, int64_t y_stride)
+inline bool cache_ok(const stand_cache *c)
 {
-    const int64_t most = (int64_t)1 << 32, xs = x_stride / 8, ys = y_stride / 8;
+    return c && c->d_k && c->d_v && aligned16(c->d_k) && aligned16(c->d_v) && (c->dtype == STAND_BF16 || c->dtype == STAND_F16 || of_four(c)) &&
+           c->layers >= 1 && c->pages >= 1 && page_size_ok(c->page_size) && c->kv_heads >= 1 && c->kv_heads <= 4096 &&
+           (c->head_dim == 64 || c->head_dim == 128) && stride_ok(c->layer_stride) && stride_ok(c->page_stride) &&
+           stride_ok(c->slot_stride) && stride_ok(c->head_stride) && (!of_four(c) || scales_ok(c));
+}
+
+// Whether places (x, y) up to these lie less than 2^32 chunks of that many elements from the first one (x, y < 2^31).
+inline bool spans_chunks(int64_t x, int64_t x_stride, int64_t y, int64_t y_stride, int64_t chunk = 8)
+{
+    const int64_t most = (int64_t)1 << 32, xs = x_stride / chunk, ys = y_stride / chunk;
     if ((x && xs >= most / x) || (y && ys >= most / y)) return false;
     return x * xs + y * ys < most - 64;
 }
@@ -45,8 +58,10 @@ inline int check_attention_size(int64_t B, const stand_cache *cache, int32_t q_h
 {
     if (!cache_ok(cache) || !heads_ok(cache, q_heads)) return STAND_EINVAL;
     if (B > kAttnMaxBatch || q_heads > 65535) return STAND_ELIMIT;
-    // the kernel counts places of a layer in 16-byte chunks, in 32 bits
-    if (!spans_chunks(cache->pages - 1, cache->page_stride, cache->page_size - 1, cache->slot_stride)) return STAND_ELIMIT;
+    // the kernel counts places of a layer in 16-byte chunks, in 32 bits, and those of scales in heads' scales
+    if (!spans_chunks(cache->pages - 1, cache->page_stride, cache->page_size - 1, cache->slot_stride, of_four(cache) ? 32 : 8)) return STAND_ELIMIT;
+    if (of_four(cache) && !spans_chunks(cache->pages - 1, cache->scale_page_stride, cache->page_size - 1, cache->scale_slot_stride, cache->head_dim / 32))
+        return STAND_ELIMIT;
     return STAND_OK;
 }
 
@@ -72,6 +87,70 @@ inline int check_cache_commit(int64_t B, const stand_cache *cache, const stand_c
     if (!stride_ok(rows->layer_stride) || !stride_ok(rows->batch_stride) || !stride_ok(rows->row_stride) || !stride_ok(rows->head_stride))
         return STAND_EINVAL;
     return B > kServeMaxBatch || cache->layers > 65535 ? STAND_ELIMIT : STAND_OK;
+}
+
+// Rows that a layer's or a trajectory's lie side by side in: one element of the next row behind a head's would be another's.
+inline int check_cache_read(int64_t B, const stand_cache *cache, int32_t first_layer, int32_t layers, const int32_t *d_table, int32_t table_width,
+                            const stand_cache_rows_out *rows)
+{
+    if (!cache_ok(cache) || !rows || !rows->d_k || !rows->d_v || !d_table || table_width < 1) return STAND_EINVAL;
+    if (first_layer < 0 || layers < 1 || layers > cache->layers || first_layer > cache->layers - layers) return STAND_EINVAL;
+    if (rows->rows < 1 || rows->rows > kServeMaxWidth || (int64_t)table_width * cache->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
+    if (!aligned16(rows->d_k) || !aligned16(rows->d_v)) return STAND_EINVAL;
+    if (!stride_ok(rows->layer_stride) || !stride_ok(rows->batch_stride) || !stride_ok(rows->row_stride) || !stride_ok(rows->head_stride))
+        return STAND_EINVAL;
+    return B > kServeMaxBatch || layers > 65535 ? STAND_ELIMIT : STAND_OK;
+}
+
+inline bool rotation_ok(const stand_rotation *r, int32_t head_dim)
+{
+    if (!r || r->dims < 0 || r->dims % 16 || r->dims > head_dim || (r->dims && (!r->d_turns || !aligned16(r->d_turns) || r->positions < 1))) return false;
+    if (!aligned16(r->d_q_norm) || !aligned16(r->d_k_norm)) return false;
+    return !(r->d_q_norm || r->d_k_norm) || (r->eps >= 0.0f && r->eps <= 3.402823466e+38f);
+}
+
+// An output is its input in the same places, or somewhere else.
+inline bool output_ok(const void *out, const int64_t *out_stride, const void *in, const int64_t *in_stride)
+{
+    return out && aligned16(out) && strides_ok(out_stride) && (out != in || !memcmp(out_stride, in_stride, 3 * sizeof(int64_t)));
+}
+
+constexpr int64_t kTurnMaxGroups = (1 << 24) - 1;      // workgroups of a trajectory: a launch's dimension has threads for so many
+inline int64_t turn_groups(int64_t rows, int64_t heads, int32_t head_dim)
+{
+    const int64_t at_once = 256 / (head_dim / 16);
+    return (rows * heads + at_once - 1) / at_once;
+}
+
+inline int check_turned_rows(int64_t B, const stand_turned_rows *r, bool values, bool k_out)
+{
+    if (!r || !r->d_k || !aligned16(r->d_k) || !strides_ok(r->k_stride)) return STAND_EINVAL;
+    if ((r->dtype != STAND_BF16 && r->dtype != STAND_F16) || (r->head_dim != 64 && r->head_dim != 128)) return STAND_EINVAL;
+    if (r->rows < 1 || r->rows > kServeMaxWidth || r->kv_heads < 1 || r->kv_heads > 4096) return STAND_EINVAL;
+    if (r->d_q && (r->q_heads < 1 || !aligned16(r->d_q) || !strides_ok(r->q_stride) || !output_ok(r->d_q_out, r->q_out_stride, r->d_q, r->q_stride)))
+        return STAND_EINVAL;
+    if ((k_out || r->d_k_out) && !output_ok(r->d_k_out, r->k_out_stride, r->d_k, r->k_stride)) return STAND_EINVAL;
+    if (values && (!r->d_v || !aligned16(r->d_v) || !strides_ok(r->v_stride))) return STAND_EINVAL;
+    if (B > kServeMaxBatch || (r->d_q && r->q_heads > 65535)) return STAND_ELIMIT;
+    const int64_t q = r->d_q ? turn_groups(r->rows, r->q_heads, r->head_dim) : 0, k = turn_groups(r->rows, r->kv_heads, r->head_dim);
+    return q + k + (values ? k : 0) > kTurnMaxGroups ? STAND_ELIMIT : STAND_OK;
+}
+
+inline int check_tree_rotate(int64_t B, int32_t N, const stand_rotation *rotation, const int32_t *d_len, const int32_t *d_draft_tok,
+                             const stand_turned_rows *rows)
+{
+    if (!rows || (rows->head_dim != 64 && rows->head_dim != 128) || !rotation_ok(rotation, rows->head_dim) || !d_len || !d_draft_tok) return STAND_EINVAL;
+    if (rows->rows != N) return STAND_EINVAL;
+    return check_turned_rows(B, rows, false, true);
+}
+
+inline int check_cache_append(int64_t B, const stand_cache *cache, int32_t layer, const stand_rotation *rotation, const stand_turned_rows *rows,
+                              const int64_t *d_slots, int32_t width)
+{
+    if (!cache_ok(cache) || !rows || layer < 0 || layer >= cache->layers || !d_slots) return STAND_EINVAL;
+    if (rows->dtype != rows_dtype(cache) || rows->kv_heads != cache->kv_heads || rows->head_dim != cache->head_dim) return STAND_EINVAL;
+    if ((rotation && !rotation_ok(rotation, rows->head_dim)) || width < rows->rows || width > kServeMaxWidth) return STAND_EINVAL;
+    return check_turned_rows(B, rows, true, false);
 }
 
 inline int check_cache_pages(int64_t B, const stand_pages *p, const int64_t *d_slots, int32_t slot_width, const int32_t *d_missing,
