@@ -390,27 +390,31 @@ int stand_read_rows(const void *d_src, uint64_t row_bytes, uint64_t rows, uint32
 
 /* A paged cache: element e of head g at place s of page p in layer l is d_k[l * layer_stride + p * page_stride + s * slot_stride
  * + g * head_stride + e], d_v likewise.  Strides are in elements, not negative and multiples of 8; pointers are 16-byte aligned.
- * A slot is p * page_size + s.
- *   4 bits (STAND_MXFP4 + the rows' type): strides are multiples of 32 elements, and element e of a head is in the low (e even) or high
- * half of byte e / 2 from the head's first one: bit 3 the sign, bits 0 .. 2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Each 32 neighbouring elements of a
- * head share a byte s for the power of two 2^(s - 127) that they are multiplied by (255: they are NaN): block i of that head is d_k_scale[l *
- * scale_layer_stride + p * scale_page_stride + s * scale_slot_stride + g * scale_head_stride + i].  Those strides are in bytes, not
- * negative and, like the scales' pointers, multiples of head_dim / 32.  The calls below write s = floor(log2(m)) - 2 + 127 for
- * the block's largest magnitude m rounded to two significant bits (halfway: up), at least 2 and at most 252 with bf16 rows, 104 and 140 with fp16 ones, and
- * each element as the nearest one (halfway: the one with bit 0 clear; above 6: 6); a block with an infinity or a NaN gets s = 255.  Scales
- * of other origin keep to those limits: past them products may not be numbers of the rows' type.
- *   The members from d_k_scale on are read for caches of 4 bits alone. */
+ * A slot is p * page_size + s. */
 typedef struct {
     void *d_k, *d_v;
-    int32_t dtype;      /* STAND_BF16 or STAND_F16, also that of the rows given with it; or STAND_MXFP4 + that */
+    int32_t dtype;      /* STAND_BF16 or STAND_F16, also that of the rows given with it; or STAND_MXFP4 + that (stand_cache4) */
     int32_t layers, pages;
     int32_t page_size;  /* a power of two <= STAND_MAX_PAGE */
     int32_t kv_heads;   /* <= 4096 */
     int32_t head_dim;   /* 64 or 128 */
     int64_t layer_stride, page_stride, slot_stride, head_stride;
+} stand_cache;
+
+/* A cache of 4 bits: wherever a call takes a stand_cache whose dtype is STAND_MXFP4 + the rows' type, it is the first member of
+ * this.  Its strides are multiples of 32 elements, and element e of a head is in the low (e even) or high half of byte e / 2 from the head's
+ * first one: bit 3 the sign, bits 0 .. 2 one of 0, 0.5, 1, 1.5, 2, 3, 4, 6.  Each 32 neighbouring elements of a head share a byte s for the power of
+ * two 2^(s - 127) that they are multiplied by (255: they are NaN): block i of that head has d_k_scale[l * scale_layer_stride + p *
+ * scale_page_stride + s * scale_slot_stride + g * scale_head_stride + i].  Those strides are in bytes, not negative and, like the scales'
+ * pointers, multiples of head_dim / 32.  The calls below write s = floor(log2(m)) - 2 + 127 for the block's largest magnitude m
+ * rounded to two significant bits (halfway: up), at least 2 and at most 252 with bf16 rows, 104 and 140 with fp16 ones, and each element as the
+ * nearest one (halfway: the one with bit 0 clear; above 6: 6); a block with an infinity or a NaN gets s = 255.  Scales of other
+ * origin keep to those limits: past them products may not be numbers of the rows' type. */
+typedef struct {
+    stand_cache cache;
     void *d_k_scale, *d_v_scale;
     int64_t scale_layer_stride, scale_page_stride, scale_slot_stride, scale_head_stride;
-} stand_cache;
+} stand_cache4;
 
 /* Queries, keys, values and outputs of the tree's nodes in one layer: strides of batch, node and head in elements, not
  * negative and multiples of 8 (slices of a fused projection are fine); a head's elements are contiguous; pointers are
@@ -456,7 +460,7 @@ typedef struct {
 
 /* Rows into the cache: for all layers, trajectories b and j < d_count[b], row d_row[b][j] of trajectory b goes to slot
  * d_slots[b][j] (stand_cache_pages).  After a verification d_row is d_out_node and d_count is d_out_len (width = depth + 1); a
- * prompt's rows go in as they stand with d_row NULL (row j).  Into a cache of 4 bits they go as described at stand_cache.  d_count NULL: `width` each.  A negative slot or row (or one past
+ * prompt's rows go in as they stand with d_row NULL (row j).  Into a cache of 4 bits they go as described at stand_cache4.  d_count NULL: `width` each.  A negative slot or row (or one past
  * the end) is left out.  d_slots, d_row: [B][width].  The slots of a call differ from each other (where they do not, what
  * ends up there is not specified); the rows do not overlap the cache. */
 int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots, int32_t width,

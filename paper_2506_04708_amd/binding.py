@@ -59,8 +59,13 @@ class CacheDesc(C.Structure):
         ("d_k", C.c_void_p), ("d_v", C.c_void_p), ("dtype", C.c_int32), ("layers", C.c_int32), ("pages", C.c_int32),
         ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("layer_stride", C.c_int64),
         ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
-        ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p), ("scale_layer_stride", C.c_int64), ("scale_page_stride", C.c_int64),
-        ("scale_slot_stride", C.c_int64), ("scale_head_stride", C.c_int64),
+    ]
+
+
+class Cache4Desc(C.Structure):
+    _fields_ = [
+        ("cache", CacheDesc), ("d_k_scale", C.c_void_p), ("d_v_scale", C.c_void_p), ("scale_layer_stride", C.c_int64),
+        ("scale_page_stride", C.c_int64), ("scale_slot_stride", C.c_int64), ("scale_head_stride", C.c_int64),
     ]
 
 
@@ -259,8 +264,9 @@ class PagedCache:
             self.dtype, self.dim = dtype, 2 * self.dim
             assert k_scale.shape == v_scale.shape == (*k.shape[:4], self.dim // 32) and k_scale.stride() == v_scale.stride() and k_scale.stride(4) == 1
             assert k_scale.device == v_scale.device == k.device
-            self.desc = CacheDesc(k.data_ptr(), v.data_ptr(), STAND_MXFP4 + _HALF[dtype], *k.shape[:4], self.dim, *(2 * s for s in k.stride()[:4]),
-                                  k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride()[:4])
+            desc = CacheDesc(k.data_ptr(), v.data_ptr(), STAND_MXFP4 + _HALF[dtype], *k.shape[:4], self.dim, *(2 * s for s in k.stride()[:4]))
+            self.whole = Cache4Desc(desc, k_scale.data_ptr(), v_scale.data_ptr(), *k_scale.stride()[:4])
+            self.desc = self.whole.cache    # (its first member, in place)
         self.ref = C.addressof(self.desc)
 
     @classmethod

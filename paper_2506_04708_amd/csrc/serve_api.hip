@@ -87,9 +87,10 @@ CachePlaces places_of(const stand_cache *c)
     p.k_scale = p.v_scale = nullptr;
     p.scale_layer = p.scale_page = p.scale_slot = p.scale_head = 0;
     if (of_four(c)) {
-        p.k_scale = (uint8_t *)c->d_k_scale; p.v_scale = (uint8_t *)c->d_v_scale;
-        p.scale_layer = c->scale_layer_stride; p.scale_page = c->scale_page_stride; p.scale_slot = c->scale_slot_stride;
-        p.scale_head = c->scale_head_stride;
+        const stand_cache4 *f = four_of(c);
+        p.k_scale = (uint8_t *)f->d_k_scale; p.v_scale = (uint8_t *)f->d_v_scale;
+        p.scale_layer = f->scale_layer_stride; p.scale_page = f->scale_page_stride; p.scale_slot = f->scale_slot_stride;
+        p.scale_head = f->scale_head_stride;
     }
     p.page_shift = log2_of(c->page_size); p.pages = c->pages;
     return p;
@@ -201,9 +202,10 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     a.k_scale = a.v_scale = nullptr;
     a.scale_page = a.scale_slot = a.scale_head = 0;
     if (four) {
-        a.k_scale = (const uint8_t *)cache->d_k_scale + layer * cache->scale_layer_stride;
-        a.v_scale = (const uint8_t *)cache->d_v_scale + layer * cache->scale_layer_stride;
-        a.scale_page = cache->scale_page_stride; a.scale_slot = cache->scale_slot_stride; a.scale_head = cache->scale_head_stride;
+        const stand_cache4 *f = four_of(cache);
+        a.k_scale = (const uint8_t *)f->d_k_scale + layer * f->scale_layer_stride;
+        a.v_scale = (const uint8_t *)f->d_v_scale + layer * f->scale_layer_stride;
+        a.scale_page = f->scale_page_stride; a.scale_slot = f->scale_slot_stride; a.scale_head = f->scale_head_stride;
     }
     a.len = d_len; a.table = d_table; a.draft_tok = d_draft_tok;
     a.anc = (const uint32_t *)v.anc; a.anc_words = 2 * v.anc_words;      // (little endian: words of 32 nodes)

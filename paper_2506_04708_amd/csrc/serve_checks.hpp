@@ -25,13 +25,15 @@ inline int log2_of(int64_t x)
 
 inline bool of_four(const stand_cache *c) { return c->dtype == STAND_MXFP4 + STAND_BF16 || c->dtype == STAND_MXFP4 + STAND_F16; }
 inline int rows_dtype(const stand_cache *c) { return of_four(c) ? c->dtype - STAND_MXFP4 : c->dtype; }
+inline const stand_cache4 *four_of(const stand_cache *c) { return reinterpret_cast<const stand_cache4 *>(c); }   // (its first member)
 // Scales of a cache of 4 bits: a head's stand together.
 inline bool scales_ok(const stand_cache *c)
 {
+    const stand_cache4 *f = four_of(c);
     const int64_t unit = c->head_dim / 32;
     auto ok = [&](int64_t s) { return s >= 0 && s % unit == 0 && s < ((int64_t)1 << 48); };
-    return c->d_k_scale && c->d_v_scale && (uintptr_t)c->d_k_scale % unit == 0 && (uintptr_t)c->d_v_scale % unit == 0 && ok(c->scale_layer_stride) &&
-           ok(c->scale_page_stride) && ok(c->scale_slot_stride) && ok(c->scale_head_stride) && c->layer_stride % 32 == 0 &&
+    return f->d_k_scale && f->d_v_scale && (uintptr_t)f->d_k_scale % unit == 0 && (uintptr_t)f->d_v_scale % unit == 0 && ok(f->scale_layer_stride) &&
+           ok(f->scale_page_stride) && ok(f->scale_slot_stride) && ok(f->scale_head_stride) && c->layer_stride % 32 == 0 &&
            c->page_stride % 32 == 0 && c->slot_stride % 32 == 0 && c->head_stride % 32 == 0;
 }
 
@@ -60,7 +62,8 @@ inline int check_attention_size(int64_t B, const stand_cache *cache, int32_t q_h
     if (B > kAttnMaxBatch || q_heads > 65535) return STAND_ELIMIT;
     // the kernel counts places of a layer in 16-byte chunks, in 32 bits, and those of scales in heads' scales
     if (!spans_chunks(cache->pages - 1, cache->page_stride, cache->page_size - 1, cache->slot_stride, of_four(cache) ? 32 : 8)) return STAND_ELIMIT;
-    if (of_four(cache) && !spans_chunks(cache->pages - 1, cache->scale_page_stride, cache->page_size - 1, cache->scale_slot_stride, cache->head_dim / 32))
+    if (of_four(cache) && !spans_chunks(cache->pages - 1, four_of(cache)->scale_page_stride, cache->page_size - 1, four_of(cache)->scale_slot_stride,
+                                         cache->head_dim / 32))
         return STAND_ELIMIT;
     return STAND_OK;
 }

@@ -14,6 +14,7 @@ BF, HF, MX, EINVAL, ELIMIT = 0, 2, 4, -1, -5
 
 
 class Cache(C.Structure):
+    """stand_cache4, the stand_cache that it begins with spelled out."""
     _fields_ = [("d_k", P), ("d_v", P), ("dtype", C.c_int32), ("layers", C.c_int32), ("pages", C.c_int32), ("page_size", C.c_int32),
                 ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("layer_stride", L), ("page_stride", L), ("slot_stride", L), ("head_stride", L),
                 ("d_k_scale", P), ("d_v_scale", P), ("scale_layer_stride", L), ("scale_page_stride", L), ("scale_slot_stride", L),
@@ -55,7 +56,7 @@ int append(int64_t B, const stand_cache *c, int layer, const stand_rotation *r, 
 { return check_cache_append(B, c, layer, r, rows, (const int64_t *)slots, width); }
 int rd(int64_t B, const stand_cache *c, int first, int layers, const void *table, int width, const stand_cache_rows_out *rows)
 { return check_cache_read(B, c, first, layers, (const int32_t *)table, width, rows); }
-int sizes(int i) { const int s[] = {sizeof(stand_cache), sizeof(stand_rotation), sizeof(stand_turned_rows), sizeof(stand_cache_rows_out)}; return s[i]; }
+int sizes(int i) { const int s[] = {sizeof(stand_cache4), sizeof(stand_rotation), sizeof(stand_turned_rows), sizeof(stand_cache_rows_out)}; return s[i]; }
 int64_t groups(int64_t rows, int64_t heads, int d) { return turn_groups(rows, heads, d); }
 }""", dict(scale=([U, I], I), sized=([L, P, I], I), commit=([P], I), rotate=([L, I, P, P, P, P], I), append=([L, P, I, P, P, P, I], I),
            rd=([L, P, I, I, P, I, P], I), sizes=([I], I), groups=([L, L, I], L)))
@@ -64,7 +65,7 @@ int64_t groups(int64_t rows, int64_t heads, int d) { return turn_groups(rows, he
 def test_structures_are_as_the_binding_packs_them(lib):
     from paper_2506_04708_amd import binding
     assert [lib.sizes(i) for i in range(4)] == [C.sizeof(Cache), C.sizeof(Rotation), C.sizeof(Rows), C.sizeof(Out)]
-    assert C.sizeof(binding.CacheDesc) == lib.sizes(0) and C.sizeof(binding.RotationDesc) == lib.sizes(1)
+    assert C.sizeof(binding.Cache4Desc) == lib.sizes(0) and C.sizeof(binding.RotationDesc) == lib.sizes(1)
     assert binding._TURNED_ROWS.size == lib.sizes(2) and binding._CACHE_ROWS.size == lib.sizes(3)
     assert binding.STAND_MXFP4 == MX
 
