@@ -7,6 +7,7 @@
 #include "serve_view.hpp"
 #include "shape_logits.hpp"
 #include "tree_attn.hpp"
+#include "tree_attn4.hpp"
 
 #include <algorithm>
 #include <atomic>
@@ -55,27 +56,36 @@ int bad_device(const ServeView &v, hipError_t e)
 enum AttnForm { kAttn32, kAttn64, kAttnMore };
 AttnForm attn_form(int64_t rows) { return rows <= 32 ? kAttn32 : rows <= 64 ? kAttn64 : kAttnMore; }
 
-template <int D, bool F16, bool FOUR, typename Call>
+template <int D, bool F16, typename Call>
 auto with_attn_shape(AttnForm f, Call call)
 {
     switch (f) {
-    case kAttn32: return call(AttnShape<D, F16, 1, 4, 1, FOUR>{});
-    case kAttn64: return call(AttnShape<D, F16, 2, 2, 1, FOUR>{});
-    default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2, FOUR>{});
+    case kAttn32: return call(AttnShape<D, F16, 1, 4, 1>{});
+    case kAttn64: return call(AttnShape<D, F16, 2, 2, 1>{});
+    default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2>{});
     }
 }
+// Over a cache of 4 bits there is one form: a wave for every 32 rows.
 template <typename Call>
 auto with_attn_shape(const stand_cache *c, AttnForm f, Call call)
 {
-    auto of_type = [&](auto f16, auto four) {
-        constexpr bool F16 = decltype(f16)::value, FOUR = decltype(four)::value;
-        return c->head_dim == 64 ? with_attn_shape<64, F16, FOUR>(f, call) : with_attn_shape<128, F16, FOUR>(f, call);
-    };
-    using Yes = std::true_type;
-    using No = std::false_type;
-    if (of_four(c)) return rows_dtype(c) == STAND_F16 ? of_type(Yes{}, Yes{}) : of_type(No{}, Yes{});
-    return rows_dtype(c) == STAND_F16 ? of_type(Yes{}, No{}) : of_type(No{}, No{});
+    const bool f16 = rows_dtype(c) == STAND_F16;
+    if (of_four(c)) {
+        if (c->head_dim == 64) return f16 ? call(Attn4Shape<64, true>{}) : call(Attn4Shape<64, false>{});
+        return f16 ? call(Attn4Shape<128, true>{}) : call(Attn4Shape<128, false>{});
+    }
+    if (c->head_dim == 64) return f16 ? with_attn_shape<64, true>(f, call) : with_attn_shape<64, false>(f, call);
+    return f16 ? with_attn_shape<128, true>(f, call) : with_attn_shape<128, false>(f, call);
 }
+template <int D, bool F16, int WR, int WK, int SUB>
+const void *kernel_of(AttnShape<D, F16, WR, WK, SUB>) { return (const void *)tree_attn_kernel<AttnShape<D, F16, WR, WK, SUB>>; }
+template <int D, bool F16>
+const void *kernel_of(Attn4Shape<D, F16>) { return (const void *)tree_attn4_kernel<Attn4Shape<D, F16>>; }
+// Shares of a launch of that many workgroups.
+template <int D, bool F16, int WR, int WK, int SUB>
+int shares_of(AttnShape<D, F16, WR, WK, SUB>, int workgroups) { return workgroups; }
+template <int D, bool F16>
+int shares_of(Attn4Shape<D, F16>, int workgroups) { return workgroups * Attn4Shape<D, F16>::WAVES; }
 
 // The cache as kernels that count in 16-byte chunks see it.
 CachePlaces places_of(const stand_cache *c)
@@ -144,7 +154,7 @@ int attn_groups_of(const ServeView &v)
     int per_cu = at < 0 ? 0 : known[at].load(std::memory_order_relaxed);
     if (per_cu == 0) {
         const DeviceScope scope(v.device);
-        const void *kernel = (const void *)tree_attn_kernel<S>;
+        const void *kernel = kernel_of(S{});
         hipError_t e = scope.e;
         if (e == hipSuccess) e = hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, S::BYTES);
         if (e == hipSuccess) e = hipOccupancyMaxActiveBlocksPerMultiprocessor(&per_cu, kernel, S::THREADS, S::BYTES);
@@ -164,11 +174,14 @@ uint64_t attn_work_bytes(int groups)
 }
 
 template <typename S>
-hipError_t attn_launch(TreeAttnArgs &a, hipStream_t s)
+hipError_t attn_launch(TreeAttn4Args &a, hipStream_t s)
 {
+    a.groups = shares_of(S{}, a.workgroups);
     a.place = (long long *)(a.join + a.groups);
     a.part = (float *)(a.place + (size_t)a.groups * S::TM);
-    tree_attn_kernel<S><<<dim3((unsigned)a.groups), dim3(S::THREADS), S::BYTES, s>>>(a);
+    const dim3 grid((unsigned)a.workgroups), threads(S::THREADS);
+    if constexpr (S::WR == 1 && S::KT == 32) tree_attn4_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
+    else tree_attn_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
     tree_attn_join_kernel<S::D, S::TM, S::F16><<<dim3((unsigned)a.groups, S::WR), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }
@@ -182,7 +195,7 @@ extern "C" uint64_t stand_tree_attention_work(const stand_handle *h, const stand
     if (check_attention_size(v.B, cache, q_heads) != STAND_OK) return 0;
     const AttnForm f = attn_form((int64_t)v.N * (q_heads / cache->kv_heads));
     return with_attn_shape(cache, f,
-                           [&](auto s) { return attn_work_bytes<decltype(s)>(attn_groups_of<decltype(s)>(v)); });
+                           [&](auto s) { return attn_work_bytes<decltype(s)>(shares_of(s, attn_groups_of<decltype(s)>(v))); });
 }
 
 extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, int32_t layer, const int32_t *d_len,
@@ -193,7 +206,7 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     const ServeView v = serve_view(h);
     const int refused = check_tree_attention(v.B, cache, layer, d_len, d_table, table_width, d_draft_tok, rows, d_work);
     if (refused) return refused;
-    TreeAttnArgs a;
+    TreeAttn4Args a;
     a.q = (const uint16_t *)rows->d_q; a.k_new = (const uint16_t *)rows->d_k; a.v_new = (const uint16_t *)rows->d_v;
     a.out = (uint16_t *)rows->d_out;
     const bool four = of_four(cache);
@@ -218,9 +231,9 @@ extern "C" int stand_tree_attention(stand_handle *h, const stand_cache *cache, i
     a.width = table_width; a.pages = cache->pages; a.page_shift = log2_of(cache->page_size);
     return with_attn_shape(cache, attn_form((int64_t)v.N * a.per_kv), [&](auto s) {
         using S = decltype(s);
-        a.groups = attn_groups_of<S>(v);
-        if (a.groups == 0) return STAND_EHIP;
-        if (work_bytes < attn_work_bytes<S>(a.groups)) return STAND_EINVAL;
+        a.workgroups = attn_groups_of<S>(v);
+        if (a.workgroups == 0) return STAND_EHIP;
+        if (work_bytes < attn_work_bytes<S>(shares_of(s, a.workgroups))) return STAND_EINVAL;
         const DeviceScope scope(v.device);
         if (scope.e != hipSuccess) return bad_device(v, scope.e);
         const hipError_t e = attn_launch<S>(a, (hipStream_t)stream);

@@ -32,7 +32,6 @@
 // shares -> nodes -> page numbers -> keys, each a trip to memory: 10.8 us, and 2.2 us for the join.
 #pragma once
 #include "attn_plan.hpp"
-#include "mx4.hpp"
 #include "wave_ops.hpp"
 
 #include <type_traits>
@@ -54,9 +53,6 @@ struct TreeAttnArgs {
     long long pool_page, pool_slot, pool_head;
     float scale;
     int anc_words, B, N, per_kv, kv_heads, width, pages, page_shift, groups;
-    // a cache of 4 bits: pools of its blocks of 16 bytes, and of their scales with their strides in bytes
-    const uint8_t *k_scale, *v_scale;
-    long long scale_page, scale_slot, scale_head;
 };
 
 typedef short short4v __attribute__((ext_vector_type(4)));
@@ -189,10 +185,10 @@ __device__ __forceinline__ void group_barrier()
 }
 
 // A form of the kernel: WR waves with 32 rows each times WK waves with SUB * 32 keys of a stage each.
-template <int D_, bool F16_, int WR_, int WK_, int SUB_, bool FOUR_ = false>
+template <int D_, bool F16_, int WR_, int WK_, int SUB_>
 struct AttnShape {
     static constexpr int D = D_, WR = WR_, WK = WK_, SUB = SUB_;
-    static constexpr bool F16 = F16_, FOUR = FOUR_;    // FOUR: the cache has 4 bits
+    static constexpr bool F16 = F16_;
     static constexpr int WAVES = WR * WK, THREADS = 64 * WAVES;
     static constexpr int MIN_WAVES = 2;                // of a SIMD: 256 registers for each
     static constexpr int TM = 32 * WR;                 // query rows of a tile
@@ -210,10 +206,6 @@ struct AttnShape {
     static constexpr int KPI = 64 / CPR;               // keys of one copy instruction
     static constexpr int KW = KT / WAVES;              // keys that a wave loads per stage
     static constexpr int COPIES = 2 * KW / KPI;
-    // a cache of 4 bits: blocks of a key, and those of a wave's keys and values that a lane has; lanes have whole instructions
-    // of keys and of values where there are more than one
-    static constexpr int BLOCKS = D / kMx4Block, MINE = 2 * KW * BLOCKS / 64, IDS_MINE = MINE > 1 ? MINE / 2 : 1;
-    static_assert(2 * KW * BLOCKS == 64 * MINE, "a wave's blocks of a stage are shared out evenly");
     static constexpr int STAGE = 2 * KT * ROW;
     static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
     // LDS: stages (unit sums before them) | page numbers or ancestors, [8 stages][WAVES][64] | node list | values that are not finite
@@ -228,12 +220,15 @@ struct AttnShape {
     static_assert(KEY_PARTS <= NBUF * STAGE, "parts of the key waves are joined in the stages' memory");
     // 16-byte chunk c of key k stands at chunk c ^ swizzle(k): reads of one chunk of 16 keys (K) and of four chunks of four
     // keys (V) touch every bank once
+    static __device__ __forceinline__ int tree_keys(int nodes) { return nodes; }
+    static __device__ __forceinline__ int workgroups(const TreeAttnArgs &a) { return a.groups; }
     static __device__ __forceinline__ int swizzle_k(int k) { return D == 128 ? k & 15 : (k >> 1) & 7; }
     static __device__ __forceinline__ int swizzle_v(int k) { return D == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2; }
 };
 
 // Units of work before each trajectory, prefix[0 .. B], in LDS: a unit is a stage of KT keys for one tile of rows and one
-// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) + ceil(N / KT) units.
+// key/value head.  Trajectory b has kv_heads * ceil(drafted * per_kv / TM) items of START + ceil(len / KT) + ceil(N / KT) units
+// (N or what the form counts in its place).
 // Every workgroup counts all drafted nodes for itself, up to 16 reads of a wave in flight (128 trees of 128 nodes: 7 us).
 template <typename S>
 __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *prefix)
@@ -285,7 +280,7 @@ __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *pref
         for (int b0 = 0; b0 < a.B; b0 += 64) {
             const int b = b0 + lane;
             long long x = 0;
-            if (b < a.B) x = (S::START + item_units(b0 ? a.len[b] : first_len, (long long)a.width << a.page_shift, a.N, S::KT)) * head_weight((int)prefix[b + 1] * a.per_kv, S::TM, S::HEAVY, S::LIGHT) * a.kv_heads;
+            if (b < a.B) x = (S::START + item_units(b0 ? a.len[b] : first_len, (long long)a.width << a.page_shift, S::tree_keys(a.N), S::KT)) * head_weight((int)prefix[b + 1] * a.per_kv, S::TM, S::HEAVY, S::LIGHT) * a.kv_heads;
             for (int off = 1; off < 64; off <<= 1) {
                 const long long y = __shfl_up(x, off);
                 if (lane >= off) x += y;
@@ -299,11 +294,11 @@ __device__ __forceinline__ void unit_sums(const TreeAttnArgs &a, long long *pref
 }
 
 // Rows of nodes that were not drafted: zeros, an equal number of rows for every workgroup.
-template <typename S>
-__device__ __forceinline__ void zero_rows(const TreeAttnArgs &a)
+template <typename S, typename Args>
+__device__ __forceinline__ void zero_rows(const Args &a)
 {
     const int lane = threadIdx.x & 63;
-    const unsigned all = a.B * a.N, each = (all + a.groups - 1) / a.groups, r0 = min(all, blockIdx.x * each), r1 = min(all, r0 + each);
+    const unsigned all = a.B * a.N, each = (all + S::workgroups(a) - 1) / S::workgroups(a), r0 = min(all, blockIdx.x * each), r1 = min(all, r0 + each);
     for (unsigned x = r0; x < r1; x += 64) {
         unsigned long long gone = __ballot(x + lane < r1 && a.draft_tok[x + lane < r1 ? x + lane : r0] < 0);
         for (; gone; gone &= gone - 1) {
@@ -425,16 +420,14 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         const int n = u1 - u0, cached = cache_units - u0;       // units, those (if any) of the cache
         const int32_t *table = a.table + (long long)b * a.width;
         // (places in the cache are counted in 16-byte chunks: 32 bits reach over 64 GiB of keys or values of a layer)
-        constexpr int CHUNK = S::FOUR ? kMx4Block : 8;          // elements of one
-        const uint16_t *k_pool = a.k_pool + hk * a.pool_head / (S::FOUR ? 4 : 1), *v_pool = a.v_pool + hk * a.pool_head / (S::FOUR ? 4 : 1);
-        const uint32_t pool_page = (uint32_t)(a.pool_page / CHUNK), pool_slot = (uint32_t)(a.pool_slot / CHUNK);
+        const uint16_t *k_pool = a.k_pool + hk * a.pool_head, *v_pool = a.v_pool + hk * a.pool_head;
+        const uint32_t pool_page = (uint32_t)(a.pool_page / 8), pool_slot = (uint32_t)(a.pool_slot / 8);
         const int pages = a.pages, page_shift = a.page_shift;
         const int share = wave * S::KW;                         // this wave's keys of a stage (ALONE: those it uses)
         // page numbers of a stage's keys; of the tree's stages the words of this wave's rows' ancestors
         auto load_ids = [&](int i) {
             const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + S::IDS + wave * 256 + (i & 7) * (S::WAVES * 256));
             if (i < cached) {
-                if constexpr (S::FOUR) return;
                 int key = (u0 + i) * KT + share + lane % S::KW;
                 key = key < len ? key : len - 1;
                 copy4_async(table + (key >> page_shift), to);
@@ -442,55 +435,6 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                 const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
                 const int v = (i - cached) * KT + (wk * SUB + half % SUB) * 32;
                 copy4_async(a.anc + (long long)node * a.anc_words + (v < a.N ? v / 32 : 0), to);
-            }
-        };
-        // A cache of 4 bits: a lane's blocks of a stage come into registers, a stage ahead of their conversion into the stage's
-        // memory (which is a stage ahead of the products), and the page numbers of the next one behind them.
-        uint4v block[S::FOUR ? S::MINE : 1];
-        uint32_t scale[S::FOUR ? S::MINE : 1];
-        int page4[S::FOUR ? S::IDS_MINE : 1];
-        auto of_block = [&](int r, int &key, int &piece) {      // -> whether it is one of the values'
-            const int x = r * 64 + lane, y = x % (S::KW * S::BLOCKS);
-            key = share + y / S::BLOCKS;
-            piece = y % S::BLOCKS;
-            return x >= S::KW * S::BLOCKS;
-        };
-        auto ids4 = [&](int i) {
-#pragma unroll
-            for (int r = 0; r < S::IDS_MINE; ++r) {
-                int in_stage, piece;
-                of_block(r, in_stage, piece);
-                const int key = (u0 + i) * KT + in_stage;
-                page4[r] = table[(key < len ? key : len - 1) >> page_shift];
-            }
-        };
-        auto load4 = [&](int i, uint4v *to, uint32_t *to_scale) {
-            const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
-            const uint8_t *k_scale = a.k_scale + hk * a.scale_head, *v_scale = a.v_scale + hk * a.scale_head;
-            const uint32_t scale_page = (uint32_t)(a.scale_page / S::BLOCKS), scale_slot = (uint32_t)(a.scale_slot / S::BLOCKS);
-#pragma unroll
-            for (int r = 0; r < S::MINE; ++r) {
-                int in_stage, piece;
-                const bool is_v = of_block(r, in_stage, piece);
-                int key = (u0 + i) * KT + in_stage;
-                key = key < len ? key : len - 1;                // behind the end: the last key again, weighted with zero
-                const uint32_t page = (uint32_t)clamp_page(page4[r % S::IDS_MINE], pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
-                const uint32_t from = page * pool_page + place * pool_slot, sfrom = page * scale_page + place * scale_slot;
-                to[r] = *((const uint4v *)(is_v ? v_pool : k_pool) + from + piece);
-                to_scale[r] = (is_v ? v_scale : k_scale)[(unsigned long long)sfrom * S::BLOCKS + piece];
-            }
-        };
-        auto store4 = [&](int i, const uint4v *from, const uint32_t *from_scale) {
-            const uint32_t buf = lds0 + (i % S::NBUF) * S::STAGE;
-#pragma unroll
-            for (int r = 0; r < S::MINE; ++r) {
-                int in_stage, piece;
-                const bool is_v = of_block(r, in_stage, piece);
-                const uint32_t at = buf + (is_v ? KT * S::ROW : 0) + in_stage * S::ROW, flip = is_v ? S::swizzle_v(in_stage) : S::swizzle_k(in_stage);
-                const float factor = mx4_factor(from_scale[r]);
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    *(lds_uint4v *)(uintptr_t)(at + (((uint32_t)(4 * piece + x) ^ flip) << 4)) = __builtin_bit_cast(uint4v, mx4_eight<S::F16>(from[r][x], factor));
             }
         };
         constexpr int LOADS = S::KW / S::KPI;
@@ -513,7 +457,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         };
         auto load_stage = [&](int i) {
             if (i < cached) {
-                if constexpr (!S::FOUR) load_cached(i);
+                load_cached(i);
                 return;
             }
             const TreeAttnArgs &a = fresh_args<TreeAttnArgs>();
@@ -667,8 +611,6 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
         using Yes = std::true_type;
         using No = std::false_type;
         load_ids(0); load_ids(1); load_ids(2);
-        if constexpr (S::FOUR)
-            if (cached > 0) ids4(0);
         {
             const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2] + 8 * half;
 #pragma unroll
@@ -677,36 +619,15 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
             for (int i = 0; i < DC; ++i) asm volatile("" : "+v"(q[i]));
         }
-        if constexpr (S::FOUR)
-            if (cached > 0) {                                   // the first two stages' blocks at once
-                uint4v block0[S::MINE];
-                uint32_t scale0[S::MINE];
-                load4(0, block0, scale0);
-                if (cached > 1) {
-                    ids4(1);
-                    load4(1, block, scale);
-                    if (cached > 2) ids4(2);
-                }
-                store4(0, block0, scale0);
-            }
         wait_loads<0>();
         load_stage(0);
         if (n > 1) { load_ids(3); load_stage(1); }
-        // the next stage's conversion, the loads of the one behind it
-        auto advance4 = [&](int i) {
-            if (i + 1 < min(cached, n)) store4(i + 1, block, scale);
-            if (i + 2 < min(cached, n)) {
-                load4(i + 2, block, scale);
-                ids4(i + 3);
-            }
-        };
         uint32_t *wild = (uint32_t *)(attn_lds + S::MISC);      // [WAVES][32]: nodes with a value that is no finite number, found by a wave
         if (lane < 32) wild[wave * 32 + lane] = 0;
         // A unit that has come: everyone's copies are there, two units ahead are on their way, the tree's values are finite.
         // -> the keys of this wave's subtile t that count for this lane's query: bits, `all` of them.
         auto arrive = [&](int i) {
-            if (S::FOUR && i < cached) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            else if (i + 1 < n) wait_loads<S::COPIES + 1>();    // (the unit's own copies are all older than the newest that many)
+            if (i + 1 < n) wait_loads<S::COPIES + 1>();         // (the unit's own copies are all older than the newest that many)
             else wait_loads<0>();
             if (i >= cached) {
                 // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
@@ -734,7 +655,6 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
             }
             if constexpr (!S::ALONE) {
                 group_barrier();                                // ... and everyone is done with the unit two before
-                if constexpr (S::FOUR) advance4(i);
                 if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
         };
@@ -762,7 +682,6 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
                     values(off);
                 }
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                if constexpr (S::FOUR) advance4(i);
                 if (i + 2 < n) { load_ids(i + 4); load_stage(i + 2); }
             }
         } else {
@@ -780,17 +699,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn_kernel(Tre
 #pragma unroll
                 for (int x = 0; x < AT_ONCE; ++x) {
                     const int i = first + x;
-                    if constexpr (S::FOUR) {
-                        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                        group_barrier();
-                        advance4(i);
-                        load_ids(i + 4);                        // (where it is one of the tree's)
-                    } else {
-                        wait_loads<S::COPIES + 1>();
-                        group_barrier();
-                        load_ids(i + 4);
-                        load_cached(i + 2);
-                    }
+                    wait_loads<S::COPIES + 1>();
+                    group_barrier();
+                    load_ids(i + 4);
+                    load_cached(i + 2);
                     const uint32_t off = (i % S::NBUF) * S::STAGE;
                     if (busy) {
 #pragma unroll

@@ -1,0 +1,343 @@
+// tree_attn4.hpp -- attention of the nodes of a drafted tree over a paged cache of 4 bits and over their own ancestors.
+//
+// The mathematics is tree_attn.hpp's: one pass over the keys with a running maximum, S^T = K Q^T and O^T = V^T P^T with 32x32x16
+// products, weights rounded to the rows' type.  What differs is where the time goes: a token's key and value are a quarter of the
+// bytes, so that reading them once for every 32 rows costs less than sharing them out, and making 16-bit numbers of them takes a
+// wave 64 conversions for 32 keys beside 16 matrix instructions.  So every wave works by itself: it has 32 rows of one
+// key/value head and a run of its keys, no barrier and no other wave's pace, and rows are cut into groups of 32 that leave few lanes empty.
+//
+// Keys: a lane has half of a key, D / 64 blocks, straight from memory.  A block's four words, converted with its scale (one
+// instruction for two numbers, exact), are the left operand of four products; the queries' elements are held in the same
+// order.  Values: a lane has half of a token's too; converted they go through 32 rows of LDS of the wave's own, from which the
+// transposing reads take them as V^T.  Rows of LDS are swizzled by 16 bytes so that both touch every bank once.
+//
+// The tree: the nodes that the wave's rows see, ancestors of a few nodes, are collected first, so that most trees take one step
+// of 32 keys.  Their rows have 16 bits and take the same way without the conversions.
+//
+// Work is cut as attn_plan.hpp says, a share for every wave that the chip holds; a unit is 32 keys, the whole tree is one.
+#pragma once
+#include "mx4.hpp"
+#include "tree_attn.hpp"
+
+namespace stand {
+
+struct TreeAttn4Args : TreeAttnArgs {                // k_pool, v_pool: blocks of 16 bytes; groups: shares
+    const uint8_t *k_scale, *v_scale;                // pools of the blocks' scales, strides in bytes
+    long long scale_page, scale_slot, scale_head;
+    int workgroups;
+};
+
+template <int D_, bool F16_>
+struct Attn4Shape {
+    static constexpr int D = D_;
+    static constexpr bool F16 = F16_;
+    static constexpr int WAVES = 4, THREADS = 64 * WAVES, MIN_WAVES = 2;
+    static constexpr int TM = 32, KT = 32, WR = 1;   // rows of a wave, keys of a unit
+    static constexpr int START = 6, HEAVY = 1, LIGHT = 1;
+    static constexpr int ROW = 2 * D, CPR = D / 8;   // bytes and 16-byte chunks of a value
+    static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
+    // LDS: values of each wave (unit sums before them) | its trajectory's drafted nodes | nodes that its rows see
+    static constexpr int VALUES = 32 * ROW, LIST = WAVES * VALUES > SUMS ? WAVES * VALUES : SUMS;
+    static constexpr int SEEN = LIST + WAVES * 2048, BYTES = SEEN + WAVES * 2048;
+    // chunk c of token k stands at chunk c ^ swizzle(k): a quarter of the chunks for four tokens of a transposing read, all of them
+    // for sixteen tokens of a write
+    static __device__ __forceinline__ int tree_keys(int) { return 1; }
+    static __device__ __forceinline__ int workgroups(const TreeAttn4Args &a) { return a.workgroups; }
+    static __device__ __forceinline__ int swizzle(int k) { return (D == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2) | ((k >> 2) & 3); }
+};
+
+// What a wave's lanes have written to LDS is read by others of them behind this (accesses of one wave are in order).
+__device__ __forceinline__ void lanes_agree()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+template <typename S>
+__global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(TreeAttn4Args args)
+{
+    const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
+    constexpr int D = S::D, DT = D / 32, DC = D / 16, HB = D / 64;   // tiles of the output, products of a score, blocks of half a key
+    constexpr bool F16 = S::F16;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int col = lane & 31, half = lane >> 5;
+
+    long long *sums = (long long *)attn_lds;
+    unit_sums<S>(a, sums);
+    const long long total = sums[a.B];
+    const long long W = attn_groups(total, a.groups, S::START, S::HEAVY);
+    const int share_number = (int)blockIdx.x * S::WAVES + wave;
+    if (lane == 0 && share_number >= W) a.join[share_number] = JoinRecord{0, 0, 0, 0};   // (no share has this number)
+    // neighbours in the order of the work share an XCD and so its L2
+    const int per_xcd = (int)((W + 7) / 8), in_xcd = (int)(blockIdx.x / 8) * S::WAVES + wave;
+    const long long w = (long long)(blockIdx.x % 8) * per_xcd + in_xcd;
+    const bool has_share = in_xcd < per_xcd && w < W;
+    long long unit = 0, unit_end = 0, b_start = 0;
+    int b = 0;
+    if (has_share) {
+        unit = group_start(w, total, W);
+        unit_end = group_start(w + 1, total, W);
+        int lo = 0, hi = a.B - 1;                      // last b with sums[b] <= unit (and units of its own)
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) / 2;
+            if (sums[mid] <= unit) lo = mid; else hi = mid - 1;
+        }
+        b = __builtin_amdgcn_readfirstlane(lo);
+        b_start = sums[b];
+    }
+    __syncthreads();                                   // (the sums make room)
+    int listed = -1, nodes = 0;
+    bool first_item = true;
+    const Exponent ex = exponent_of(a.scale);
+    const float c = ex.c;
+    uint16_t *const list = (uint16_t *)(attn_lds + S::LIST + wave * 2048), *const seen = (uint16_t *)(attn_lds + S::SEEN + wave * 2048);
+    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char *)attn_lds) + wave * S::VALUES;
+    // where this lane's half of token `col` goes, its chunk 0 (chunk x: ^ x << 4), and where its reads of tokens 4 half + j4 and of
+    // those eight further on begin
+    const uint32_t put = lds0 + col * S::ROW + (((4 * HB * half) ^ S::swizzle(col)) << 4);
+    const int piece = lane & 3, j4 = (lane >> 2) & 3, dsub = (lane >> 4) & 1;
+    const uint32_t get = lds0 + (4 * half + j4) * S::ROW + (((2 * dsub + (piece >> 1)) ^ S::swizzle(4 * half + j4)) << 4) + (piece & 1) * 8;
+
+    const int B = a.B;
+    while (unit < unit_end && b < B) {
+        // ---- the item: trajectory, key/value head, 32 rows ----
+        const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
+        if (listed != b) {
+            int base = 0;
+            for (int u0 = 0; u0 < a.N; u0 += 256) {
+                int tok[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) tok[k] = a.draft_tok[b * a.N + min(u0 + 64 * k + lane, a.N - 1)];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int u = u0 + 64 * k + lane;
+                    const bool there = u < a.N && tok[k] >= 0;
+                    const unsigned long long bits = __ballot(there);
+                    if (there) list[base + __popcll(bits & ((1ull << lane) - 1))] = (uint16_t)u;
+                    base += __popcll(bits);
+                }
+            }
+            nodes = __builtin_amdgcn_readfirstlane(base);
+            listed = b;
+            lanes_agree();
+        }
+        if (nodes == 0) { ++b; continue; }             // nothing drafted: no units
+        const long long most = (long long)a.width << a.page_shift;
+        const int len = __builtin_amdgcn_readfirstlane((int)clamp_length(a.len[b], most));
+        const int cache_units = (len + S::KT - 1) / S::KT, units = cache_units + 1, per_item = units + S::START;
+        const int all_rows = nodes * a.per_kv;
+        const long long per_head = per_item * head_weight(all_rows, S::TM, S::HEAVY, S::LIGHT);
+        const int heads_before = (int)quotient(unit - b_start, per_head);
+        const long long head_start = b_start + heads_before * per_head;
+        const int tile = (int)quotient(unit - head_start, per_item);
+        const int row0 = tile * S::TM, rows = min(all_rows, row0 + S::TM);
+        const int hk = (heads_before + b) % a.kv_heads;   // (not the same head of all trajectories at one time)
+        const long long item_start = head_start + (long long)tile * per_item, item_end = item_start + per_item;
+        const int u0 = (int)units_before(unit - item_start, 1, S::START, units), u1 = (int)units_before(unit_end - item_start, 1, S::START, units);
+        if (u1 == 0) break;                            // the next one's
+        bool leads = false;                            // this share is the second one of its first item
+        if (first_item) {
+            first_item = false;
+            const long long from = first_group(item_start, total, W, S::START, 1);
+            leads = u0 > 0 && from == w - 1;
+            if (lane == 0)                             // (every share comes here: none ends before its first item begins)
+                a.join[w] = JoinRecord{(int)from, (int)group_of(item_end - 1, total, W), u0 > 0 ? rows - row0 : 0, 0};
+        }
+        const int row = row0 + col, my_row = row < rows ? row : rows - 1;
+        const int node = list[my_row / a.per_kv], head = hk * a.per_kv + my_row % a.per_kv;
+
+        float16v o[DT];
+#pragma unroll
+        for (int i = 0; i < DT; ++i) o[i] = float16v{0};
+        float m = -__builtin_huge_valf(), l = 0.0f;    // running maximum of the products with the keys, sum of the weights
+        uint4v q[DC];                                  // in the order of the lanes' halves of keys
+        {
+            const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2] + D / 2 * half;
+#pragma unroll
+            for (int i = 0; i < DC; ++i) q[i] = *(const uint4v *)(qp + 8 * i);
+        }
+        // Weights of the scores t of 32 keys, their products with the values in LDS.
+        auto values = [&](float16v &t) {
+            uint4v vf[2][DT];
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)((get ^ (d << 6)) + 16 * k * S::ROW));
+                    const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)((get ^ (d << 6) ^ 32) + (16 * k + 8) * S::ROW));
+                    vf[k][d] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+            float top = t[0];
+#pragma unroll
+            for (int x = 1; x < 16; ++x) top = fmaxf(top, t[x]);
+            float16v *const of[1] = {&t};
+            const float shift = raise_row<F16>(ex, other_half_max(top), m, l, o, of);
+            uint32_t p[8];
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                p[x] = pack2<F16>(__builtin_amdgcn_exp2f(fmaf(t[2 * x], c, shift)), __builtin_amdgcn_exp2f(fmaf(t[2 * x + 1], c, shift)));
+                l = add2<F16>(p[x], l);
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int d = 0; d < DT; ++d) o[d] = mfma32<F16>(vf[k][d], uint4v{p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]}, o[d]);
+        };
+
+        // ---- the cached keys of this share: blocks a unit ahead, page numbers two ----
+        const int n = min(u1, cache_units) - u0;
+        if (n > 0) {
+            const int32_t *table = a.table + (long long)b * a.width;
+            const int page_shift = a.page_shift, pages = a.pages;
+            const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
+            const uint32_t scale_page = (uint32_t)(a.scale_page / (2 * HB)), scale_slot = (uint32_t)(a.scale_slot / (2 * HB));
+            const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4) + HB * half, *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4) + HB * half;
+            const uint8_t *k_scale = a.k_scale + hk * a.scale_head + HB * half, *v_scale = a.v_scale + hk * a.scale_head + HB * half;
+            uint4v kb[HB], vb[HB];
+            uint32_t ks, vs;                           // a byte for each block
+            auto key_of = [&](int i) { return min((u0 + i) * S::KT + col, len - 1); };   // behind the end: the last key again, weighted with zero
+            auto load = [&](int i, int page) {
+                const int key = key_of(i);
+                const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
+                const uint32_t from = at * pool_page + place * pool_slot;
+                const unsigned long long sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * (2 * HB);
+#pragma unroll
+                for (int r = 0; r < HB; ++r) {
+                    kb[r] = k_pool[(unsigned long long)from + r];
+                    vb[r] = v_pool[(unsigned long long)from + r];
+                }
+                if constexpr (HB == 2) {
+                    ks = *(const uint16_t *)(k_scale + sfrom);
+                    vs = *(const uint16_t *)(v_scale + sfrom);
+                } else {
+                    ks = k_scale[sfrom];
+                    vs = v_scale[sfrom];
+                }
+            };
+            load(0, table[key_of(0) >> page_shift]);
+            int page = table[key_of(1) >> page_shift];
+            for (int i = 0; i < n; ++i) {
+                float16v t = float16v{0};
+#pragma unroll
+                for (int r = 0; r < HB; ++r) {
+                    const float kf = mx4_factor(ks >> (8 * r) & 255u), vf = mx4_factor(vs >> (8 * r) & 255u);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        t = mfma32<F16>(__builtin_bit_cast(uint4v, mx4_eight<F16>(kb[r][x], kf)), q[4 * r + x], t);
+                        *(lds_uint4v *)(uintptr_t)(put ^ ((4 * r + x) << 4)) = __builtin_bit_cast(uint4v, mx4_eight<F16>(vb[r][x], vf));
+                    }
+                }
+                if (i + 1 < n) {
+                    load(i + 1, page);
+                    page = table[key_of(i + 2) >> page_shift];
+                }
+                const int left = len - (u0 + i) * S::KT;
+                if (left < 32) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) t[x] = 8 * (x / 4) + x % 4 + 4 * half < left ? t[x] : -__builtin_huge_valf();
+                }
+                values(t);
+            }
+        }
+
+        // ---- the tree: the nodes that these rows see ----
+        if (u1 == units) {
+            const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
+            const uint32_t *anc = a.anc + (long long)node * a.anc_words;
+            int count = 0;
+            for (int x = 0; 32 * x < a.N; ++x) {
+                uint32_t bits = anc[x];
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1) bits |= (uint32_t)__shfl_xor((int)bits, off);
+                bits = __builtin_amdgcn_readfirstlane(bits);
+                if (half == 0 && (bits >> col & 1u)) seen[count + __popc(bits & ((1u << col) - 1u))] = (uint16_t)(32 * x + col);
+                count += __popc(bits);
+            }
+            lanes_agree();
+            for (int j0 = 0; j0 < count; j0 += 32) {
+                const int v = seen[min(j0 + col, count - 1)];
+                const uint16_t *kp = a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2] + D / 2 * half;
+                const uint16_t *vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2] + D / 2 * half;
+                uint4v kw[DC], vw[DC];
+#pragma unroll
+                for (int x = 0; x < DC; ++x) { kw[x] = *(const uint4v *)(kp + 8 * x); vw[x] = *(const uint4v *)(vp + 8 * x); }
+                // which of them this lane's row sees: bits of its 16 of the 32
+                uint32_t mine = 0;
+#pragma unroll
+                for (int x = 0; x < 16; ++x) {
+                    const int j = 8 * (x / 4) + x % 4 + 4 * half, u = seen[min(j0 + j, count - 1)];
+                    mine |= (j0 + j < count ? anc[u / 32] >> (u & 31) & 1u : 0u) << j;
+                }
+                // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
+                // zeros, and the rows that see them get them added below.
+                bool found = false;
+#pragma unroll
+                for (int x = 0; x < DC; ++x) {
+                    constexpr uint32_t kExp = F16 ? 0x7C00u : 0x7F80u;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const bool lo = (vw[x][e] & kExp) == kExp, hi = ((vw[x][e] >> 16) & kExp) == kExp;
+                        found |= lo | hi;
+                        vw[x][e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
+                    }
+                    *(lds_uint4v *)(uintptr_t)(put ^ (x << 4)) = vw[x];
+                }
+                const unsigned long long wild2 = __ballot(found && j0 + col < count);
+                float16v t = float16v{0};
+#pragma unroll
+                for (int x = 0; x < DC; ++x) t = mfma32<F16>(kw[x], q[x], t);
+#pragma unroll
+                for (int x = 0; x < 16; ++x) t[x] = mine >> (8 * (x / 4) + x % 4 + 4 * half) & 1u ? t[x] : -__builtin_huge_valf();
+                values(t);
+                uint32_t wild = __builtin_amdgcn_readfirstlane((uint32_t)wild2 | (uint32_t)(wild2 >> 32));
+                const uint32_t all = mine | (uint32_t)__shfl_xor((int)mine, 32);
+                for (; wild; wild &= wild - 1) {
+                    // an infinity or NaN reaches the rows that see its node, whatever its weight
+                    const int j = __builtin_ctz(wild), u = seen[j0 + j];
+                    const uint16_t *from = a.v_new + b * a.vs[0] + u * a.vs[1] + hk * a.vs[2] + 4 * half;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                            const uint16_t h = from[32 * d + 8 * (e / 4) + e % 4];
+                            const float y = F16 ? (float)__builtin_bit_cast(_Float16, h) : __uint_as_float((uint32_t)h << 16);
+                            if ((all >> j & 1u) && !(fabsf(y) < __builtin_huge_valf())) o[d][e] += y;
+                        }
+                }
+            }
+        }
+
+        // ---- the rows' outputs, or this wave's part of them ----
+        l = other_half_sum(l);
+        m = fmaxf(m, kLowest);                         // (nothing seen: differences of maxima are numbers)
+        if (row < rows) {
+            const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
+            if (u0 == 0 && u1 == units) {
+                const float r = 1.0f / l;
+                uint16_t *op = a.out + b * a.os[0] + node * a.os[1] + head * a.os[2] + 4 * half;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *(uint2 *)(op + 32 * d + 8 * i) = uint2{pack2<F16>(o[d][4 * i] * r, o[d][4 * i + 1] * r), pack2<F16>(o[d][4 * i + 2] * r, o[d][4 * i + 3] * r)};
+            } else {
+                // (as the registers stand, so that every store is one run of 1 KiB)
+                float *to = a.part + (2 * w + (u0 == 0)) * (long long)(S::TM * (D + 2));
+                if (half == 0) { to[col] = m; to[S::TM + col] = l; }
+                float4v *to4 = (float4v *)(to + 2 * S::TM) + lane;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) to4[(4 * d + i) * 64] = float4v{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
+                if (leads && half == 0) a.place[w * S::TM + col] = b * a.os[0] + node * a.os[1] + head * a.os[2];
+            }
+        }
+        if (u1 < units) break;
+        unit = item_end;
+        if (unit == b_start + per_head * fresh_args<TreeAttn4Args>().kv_heads) { b_start = unit; ++b; }
+    }
+    zero_rows<S>(fresh_args<TreeAttn4Args>());         // (last: the first ones to be done have the time)
+}
+
+}  // namespace stand
