@@ -65,27 +65,36 @@ auto with_attn_shape(AttnForm f, Call call)
     default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2>{});
     }
 }
-// Over a cache of 4 bits there is one form: a wave for every 32 rows.
+// Over a cache of 4 bits: one, two or four waves of rows with the same keys.
+template <int D, bool F16, typename Call>
+auto with_attn4_shape(AttnForm f, Call call)
+{
+    switch (f) {
+    case kAttn32: return call(Attn4Shape<D, F16, 1>{});
+    case kAttn64: return call(Attn4Shape<D, F16, 2>{});
+    default: return call(Attn4Shape<D, F16, 4>{});
+    }
+}
 template <typename Call>
 auto with_attn_shape(const stand_cache *c, AttnForm f, Call call)
 {
     const bool f16 = rows_dtype(c) == STAND_F16;
     if (of_four(c)) {
-        if (c->head_dim == 64) return f16 ? call(Attn4Shape<64, true>{}) : call(Attn4Shape<64, false>{});
-        return f16 ? call(Attn4Shape<128, true>{}) : call(Attn4Shape<128, false>{});
+        if (c->head_dim == 64) return f16 ? with_attn4_shape<64, true>(f, call) : with_attn4_shape<64, false>(f, call);
+        return f16 ? with_attn4_shape<128, true>(f, call) : with_attn4_shape<128, false>(f, call);
     }
     if (c->head_dim == 64) return f16 ? with_attn_shape<64, true>(f, call) : with_attn_shape<64, false>(f, call);
     return f16 ? with_attn_shape<128, true>(f, call) : with_attn_shape<128, false>(f, call);
 }
 template <int D, bool F16, int WR, int WK, int SUB>
 const void *kernel_of(AttnShape<D, F16, WR, WK, SUB>) { return (const void *)tree_attn_kernel<AttnShape<D, F16, WR, WK, SUB>>; }
-template <int D, bool F16>
-const void *kernel_of(Attn4Shape<D, F16>) { return (const void *)tree_attn4_kernel<Attn4Shape<D, F16>>; }
+template <int D, bool F16, int WR>
+const void *kernel_of(Attn4Shape<D, F16, WR>) { return (const void *)tree_attn4_kernel<Attn4Shape<D, F16, WR>>; }
 // Shares of a launch of that many workgroups.
 template <int D, bool F16, int WR, int WK, int SUB>
 int shares_of(AttnShape<D, F16, WR, WK, SUB>, int workgroups) { return workgroups; }
-template <int D, bool F16>
-int shares_of(Attn4Shape<D, F16>, int workgroups) { return workgroups * Attn4Shape<D, F16>::WAVES; }
+template <int D, bool F16, int WR>
+int shares_of(Attn4Shape<D, F16, WR>, int workgroups) { return workgroups * Attn4Shape<D, F16, WR>::TEAMS; }
 
 // The cache as kernels that count in 16-byte chunks see it.
 CachePlaces places_of(const stand_cache *c)
@@ -180,7 +189,7 @@ hipError_t attn_launch(TreeAttn4Args &a, hipStream_t s)
     a.place = (long long *)(a.join + a.groups);
     a.part = (float *)(a.place + (size_t)a.groups * S::TM);
     const dim3 grid((unsigned)a.workgroups), threads(S::THREADS);
-    if constexpr (S::WR == 1 && S::KT == 32) tree_attn4_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
+    if constexpr (S::KT == 32) tree_attn4_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
     else tree_attn_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
     tree_attn_join_kernel<S::D, S::TM, S::F16><<<dim3((unsigned)a.groups, S::WR), dim3(256), 0, s>>>(a);
     return hipGetLastError();

@@ -27,12 +27,13 @@ struct TreeAttn4Args : TreeAttnArgs {                // k_pool, v_pool: blocks o
     int workgroups;
 };
 
-template <int D_, bool F16_>
+// A form: WR waves of a workgroup have 32 rows each and the same keys (a team); the others are more teams.
+template <int D_, bool F16_, int WR_>
 struct Attn4Shape {
-    static constexpr int D = D_;
+    static constexpr int D = D_, WR = WR_;
     static constexpr bool F16 = F16_;
     static constexpr int WAVES = 4, THREADS = 64 * WAVES, MIN_WAVES = 2;
-    static constexpr int TM = 32, KT = 32, WR = 1;   // rows of a wave, keys of a unit
+    static constexpr int TEAMS = WAVES / WR, TM = 32 * WR, KT = 32;   // rows of a team, keys of a unit
     static constexpr int START = 6, HEAVY = 1, LIGHT = 1;
     static constexpr int ROW = 2 * D, CPR = D / 8;   // bytes and 16-byte chunks of a value
     static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
@@ -67,10 +68,10 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
     unit_sums<S>(a, sums);
     const long long total = sums[a.B];
     const long long W = attn_groups(total, a.groups, S::START, S::HEAVY);
-    const int share_number = (int)blockIdx.x * S::WAVES + wave;
-    if (lane == 0 && share_number >= W) a.join[share_number] = JoinRecord{0, 0, 0, 0};   // (no share has this number)
+    const int wr = wave % S::WR, team = wave / S::WR, share_number = (int)blockIdx.x * S::TEAMS + team;
+    if (wr == 0 && lane == 0 && share_number >= W) a.join[share_number] = JoinRecord{0, 0, 0, 0};   // (no share has this number)
     // neighbours in the order of the work share an XCD and so its L2
-    const int per_xcd = (int)((W + 7) / 8), in_xcd = (int)(blockIdx.x / 8) * S::WAVES + wave;
+    const int per_xcd = (int)((W + 7) / 8), in_xcd = (int)(blockIdx.x / 8) * S::TEAMS + team;
     const long long w = (long long)(blockIdx.x % 8) * per_xcd + in_xcd;
     const bool has_share = in_xcd < per_xcd && w < W;
     long long unit = 0, unit_end = 0, b_start = 0;
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
 
     const int B = a.B;
     while (unit < unit_end && b < B) {
-        // ---- the item: trajectory, key/value head, 32 rows ----
+        // ---- the item: trajectory, key/value head, a team's rows ----
         const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
         if (listed != b) {
             int base = 0;
@@ -131,7 +132,9 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
         const int heads_before = (int)quotient(unit - b_start, per_head);
         const long long head_start = b_start + heads_before * per_head;
         const int tile = (int)quotient(unit - head_start, per_item);
-        const int row0 = tile * S::TM, rows = min(all_rows, row0 + S::TM);
+        // (the groups of 32 rows in equal numbers for the head's tiles)
+        const int row_groups = (all_rows + 31) / 32, tiles = (row_groups + S::WR - 1) / S::WR;
+        const int row0 = tile * row_groups / tiles * 32, rows = min(all_rows, (tile + 1) * row_groups / tiles * 32);
         const int hk = (heads_before + b) % a.kv_heads;   // (not the same head of all trajectories at one time)
         const long long item_start = head_start + (long long)tile * per_item, item_end = item_start + per_item;
         const int u0 = (int)units_before(unit - item_start, 1, S::START, units), u1 = (int)units_before(unit_end - item_start, 1, S::START, units);
@@ -141,12 +144,13 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
             first_item = false;
             const long long from = first_group(item_start, total, W, S::START, 1);
             leads = u0 > 0 && from == w - 1;
-            if (lane == 0)                             // (every share comes here: none ends before its first item begins)
+            if (wr == 0 && lane == 0)                  // (every share comes here: none ends before its first item begins)
                 a.join[w] = JoinRecord{(int)from, (int)group_of(item_end - 1, total, W), u0 > 0 ? rows - row0 : 0, 0};
         }
-        const int row = row0 + col, my_row = row < rows ? row : rows - 1;
+        const int row = row0 + wr * 32 + col, my_row = row < rows ? row : rows - 1;
         const int node = list[my_row / a.per_kv], head = hk * a.per_kv + my_row % a.per_kv;
 
+        if (row0 + wr * 32 < rows) {                   // this wave has rows
         float16v o[DT];
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = float16v{0};
@@ -185,74 +189,25 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 for (int d = 0; d < DT; ++d) o[d] = mfma32<F16>(vf[k][d], uint4v{p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]}, o[d]);
         };
 
-        // ---- the cached keys of this share: blocks a unit ahead, page numbers two ----
-        const int n = min(u1, cache_units) - u0;
-        if (n > 0) {
-            const int32_t *table = a.table + (long long)b * a.width;
-            const int page_shift = a.page_shift, pages = a.pages;
-            const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
-            const uint32_t scale_page = (uint32_t)(a.scale_page / (2 * HB)), scale_slot = (uint32_t)(a.scale_slot / (2 * HB));
-            const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4) + HB * half, *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4) + HB * half;
-            const uint8_t *k_scale = a.k_scale + hk * a.scale_head + HB * half, *v_scale = a.v_scale + hk * a.scale_head + HB * half;
-            uint4v kb[HB], vb[HB];
-            uint32_t ks, vs;                           // a byte for each block
-            auto key_of = [&](int i) { return min((u0 + i) * S::KT + col, len - 1); };   // behind the end: the last key again, weighted with zero
-            auto load = [&](int i, int page) {
-                const int key = key_of(i);
-                const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
-                const uint32_t from = at * pool_page + place * pool_slot;
-                const unsigned long long sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * (2 * HB);
-#pragma unroll
-                for (int r = 0; r < HB; ++r) {
-                    kb[r] = k_pool[(unsigned long long)from + r];
-                    vb[r] = v_pool[(unsigned long long)from + r];
-                }
-                if constexpr (HB == 2) {
-                    ks = *(const uint16_t *)(k_scale + sfrom);
-                    vs = *(const uint16_t *)(v_scale + sfrom);
-                } else {
-                    ks = k_scale[sfrom];
-                    vs = v_scale[sfrom];
-                }
-            };
-            load(0, table[key_of(0) >> page_shift]);
-            int page = table[key_of(1) >> page_shift];
-            for (int i = 0; i < n; ++i) {
-                float16v t = float16v{0};
-#pragma unroll
-                for (int r = 0; r < HB; ++r) {
-                    const float kf = mx4_factor(ks >> (8 * r) & 255u), vf = mx4_factor(vs >> (8 * r) & 255u);
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) {
-                        t = mfma32<F16>(__builtin_bit_cast(uint4v, mx4_eight<F16>(kb[r][x], kf)), q[4 * r + x], t);
-                        *(lds_uint4v *)(uintptr_t)(put ^ ((4 * r + x) << 4)) = __builtin_bit_cast(uint4v, mx4_eight<F16>(vb[r][x], vf));
-                    }
-                }
-                if (i + 1 < n) {
-                    load(i + 1, page);
-                    page = table[key_of(i + 2) >> page_shift];
-                }
-                const int left = len - (u0 + i) * S::KT;
-                if (left < 32) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) t[x] = 8 * (x / 4) + x % 4 + 4 * half < left ? t[x] : -__builtin_huge_valf();
-                }
-                values(t);
-            }
-        }
-
         // ---- the tree: the nodes that these rows see ----
-        if (u1 == units) {
+        if (u0 == 0) {
             const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
             const uint32_t *anc = a.anc + (long long)node * a.anc_words;
             int count = 0;
-            for (int x = 0; 32 * x < a.N; ++x) {
-                uint32_t bits = anc[x];
+            for (int x0 = 0; 32 * x0 < a.N; x0 += 4) {
+                uint32_t bits[4];
 #pragma unroll
-                for (int off = 1; off < 32; off <<= 1) bits |= (uint32_t)__shfl_xor((int)bits, off);
-                bits = __builtin_amdgcn_readfirstlane(bits);
-                if (half == 0 && (bits >> col & 1u)) seen[count + __popc(bits & ((1u << col) - 1u))] = (uint16_t)(32 * x + col);
-                count += __popc(bits);
+                for (int x = 0; x < 4; ++x) bits[x] = anc[min(x0 + x, a.anc_words - 1)];
+#pragma unroll
+                for (int off = 1; off < 32; off <<= 1)
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) bits[x] |= (uint32_t)__shfl_xor((int)bits[x], off);
+#pragma unroll
+                for (int x = 0; x < 4; ++x) {
+                    const uint32_t word = x0 + x < a.anc_words ? __builtin_amdgcn_readfirstlane(bits[x]) : 0u;
+                    if (half == 0 && (word >> col & 1u)) seen[count + __popc(word & ((1u << col) - 1u))] = (uint16_t)(32 * (x0 + x) + col);
+                    count += __popc(word);
+                }
             }
             lanes_agree();
             for (int j0 = 0; j0 < count; j0 += 32) {
@@ -308,6 +263,62 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
             }
         }
 
+        // ---- the cached keys of this share: blocks a unit ahead, page numbers two ----
+        const int first = max(u0 - 1, 0), n = u1 - 1 - first;   // (the item's first unit is the tree)
+        if (n > 0) {
+            const int32_t *table = a.table + (long long)b * a.width;
+            const int page_shift = a.page_shift, pages = a.pages;
+            const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
+            const uint32_t scale_page = (uint32_t)(a.scale_page / (2 * HB)), scale_slot = (uint32_t)(a.scale_slot / (2 * HB));
+            const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4) + HB * half, *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4) + HB * half;
+            const uint8_t *k_scale = a.k_scale + hk * a.scale_head + HB * half, *v_scale = a.v_scale + hk * a.scale_head + HB * half;
+            uint4v kb[HB], vb[HB];
+            uint32_t ks, vs;                           // a byte for each block
+            auto key_of = [&](int i) { return min((first + i) * S::KT + col, len - 1); };   // behind the end: the last key again, weighted with zero
+            auto load = [&](int i, int page) {
+                const int key = key_of(i);
+                const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
+                const uint32_t from = at * pool_page + place * pool_slot;
+                const unsigned long long sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * (2 * HB);
+#pragma unroll
+                for (int r = 0; r < HB; ++r) {
+                    kb[r] = k_pool[(unsigned long long)from + r];
+                    vb[r] = v_pool[(unsigned long long)from + r];
+                }
+                if constexpr (HB == 2) {
+                    ks = *(const uint16_t *)(k_scale + sfrom);
+                    vs = *(const uint16_t *)(v_scale + sfrom);
+                } else {
+                    ks = k_scale[sfrom];
+                    vs = v_scale[sfrom];
+                }
+            };
+            load(0, table[key_of(0) >> page_shift]);
+            int page = table[key_of(1) >> page_shift];
+            for (int i = 0; i < n; ++i) {
+                float16v t = float16v{0};
+#pragma unroll
+                for (int r = 0; r < HB; ++r) {
+                    const float kf = mx4_factor(ks >> (8 * r) & 255u), vf = mx4_factor(vs >> (8 * r) & 255u);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x) {
+                        t = mfma32<F16>(__builtin_bit_cast(uint4v, mx4_eight<F16>(kb[r][x], kf)), q[4 * r + x], t);
+                        *(lds_uint4v *)(uintptr_t)(put ^ ((4 * r + x) << 4)) = __builtin_bit_cast(uint4v, mx4_eight<F16>(vb[r][x], vf));
+                    }
+                }
+                if (i + 1 < n) {
+                    load(i + 1, page);
+                    page = table[key_of(i + 2) >> page_shift];
+                }
+                const int left = len - (first + i) * S::KT;
+                if (left < 32) {
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) t[x] = 8 * (x / 4) + x % 4 + 4 * half < left ? t[x] : -__builtin_huge_valf();
+                }
+                values(t);
+            }
+        }
+
         // ---- the rows' outputs, or this wave's part of them ----
         l = other_half_sum(l);
         m = fmaxf(m, kLowest);                         // (nothing seen: differences of maxima are numbers)
@@ -324,14 +335,16 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
             } else {
                 // (as the registers stand, so that every store is one run of 1 KiB)
                 float *to = a.part + (2 * w + (u0 == 0)) * (long long)(S::TM * (D + 2));
-                if (half == 0) { to[col] = m; to[S::TM + col] = l; }
-                float4v *to4 = (float4v *)(to + 2 * S::TM) + lane;
+                const int at = wr * 32 + col;
+                if (half == 0) { to[at] = m; to[S::TM + at] = l; }
+                float4v *to4 = (float4v *)(to + 2 * S::TM) + wr * (4 * DT * 64) + lane;
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) to4[(4 * d + i) * 64] = float4v{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
-                if (leads && half == 0) a.place[w * S::TM + col] = b * a.os[0] + node * a.os[1] + head * a.os[2];
+                if (leads && half == 0) a.place[w * S::TM + at] = b * a.os[0] + node * a.os[1] + head * a.os[2];
             }
+        }
         }
         if (u1 < units) break;
         unit = item_end;
