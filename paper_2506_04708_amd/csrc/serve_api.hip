@@ -90,6 +90,18 @@ template <int D, bool F16, int WR, int WK, int SUB>
 const void *kernel_of(AttnShape<D, F16, WR, WK, SUB>) { return (const void *)tree_attn_kernel<AttnShape<D, F16, WR, WK, SUB>>; }
 template <int D, bool F16, int WR>
 const void *kernel_of(Attn4Shape<D, F16, WR>) { return (const void *)tree_attn4_kernel<Attn4Shape<D, F16, WR>>; }
+template <int D, bool F16, int WR, int WK, int SUB>
+void run_kernel(AttnShape<D, F16, WR, WK, SUB>, dim3 grid, dim3 threads, const TreeAttnArgs &a, hipStream_t s)
+{
+    using S = AttnShape<D, F16, WR, WK, SUB>;
+    tree_attn_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
+}
+template <int D, bool F16, int WR>
+void run_kernel(Attn4Shape<D, F16, WR>, dim3 grid, dim3 threads, const TreeAttn4Args &a, hipStream_t s)
+{
+    using S = Attn4Shape<D, F16, WR>;
+    tree_attn4_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
+}
 // Shares of a launch of that many workgroups.
 template <int D, bool F16, int WR, int WK, int SUB>
 int shares_of(AttnShape<D, F16, WR, WK, SUB>, int workgroups) { return workgroups; }
@@ -189,8 +201,7 @@ hipError_t attn_launch(TreeAttn4Args &a, hipStream_t s)
     a.place = (long long *)(a.join + a.groups);
     a.part = (float *)(a.place + (size_t)a.groups * S::TM);
     const dim3 grid((unsigned)a.workgroups), threads(S::THREADS);
-    if constexpr (S::KT == 32) tree_attn4_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
-    else tree_attn_kernel<S><<<grid, threads, S::BYTES, s>>>(a);
+    run_kernel(S{}, grid, threads, a, s);
     tree_attn_join_kernel<S::D, S::TM, S::F16><<<dim3((unsigned)a.groups, S::WR), dim3(256), 0, s>>>(a);
     return hipGetLastError();
 }

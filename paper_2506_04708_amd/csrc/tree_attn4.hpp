@@ -27,24 +27,39 @@ struct TreeAttn4Args : TreeAttnArgs {                // k_pool, v_pool: blocks o
     int workgroups;
 };
 
-// A form: WR waves of a workgroup have 32 rows each and the same keys (a team); the others are more teams.
+// A form.  WR = 1: every wave of a workgroup works by itself.  WR = 2, 4: the workgroup's waves have 32 rows each and the same keys.
 template <int D_, bool F16_, int WR_>
 struct Attn4Shape {
     static constexpr int D = D_, WR = WR_;
-    static constexpr bool F16 = F16_;
-    static constexpr int WAVES = 4, THREADS = 64 * WAVES, MIN_WAVES = 2;
-    static constexpr int TEAMS = WAVES / WR, TM = 32 * WR, KT = 32;   // rows of a team, keys of a unit
+    static constexpr bool F16 = F16_, ALONE = WR == 1;
+    static constexpr int WAVES = ALONE ? 4 : WR, THREADS = 64 * WAVES, MIN_WAVES = 2;
+    static constexpr int TEAMS = WAVES / WR, TM = 32 * WR;   // shares of a workgroup, rows of one
+    static constexpr int KT = ALONE || D == 128 ? 32 : 64, SUB = KT / 32;   // keys of a unit
+    static constexpr int AHEAD = WR == 4 ? 4 : 2;    // units whose blocks are on their way
     static constexpr int START = 6, HEAVY = 1, LIGHT = 1;
-    static constexpr int ROW = 2 * D, CPR = D / 8;   // bytes and 16-byte chunks of a value
+    static constexpr int ROW = 2 * D, CPR = D / 8;   // bytes and 16-byte chunks of a token's key or value
+    static constexpr int BLOCKS = D / kMx4Block, MINE = 2 * KT * BLOCKS / THREADS;   // blocks of a key, of a thread in a unit
+    static_assert(ALONE || MINE * THREADS == 2 * KT * BLOCKS, "a unit's blocks are shared out evenly");
     static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
-    // LDS: values of each wave (unit sums before them) | its trajectory's drafted nodes | nodes that its rows see
-    static constexpr int VALUES = 32 * ROW, LIST = WAVES * VALUES > SUMS ? WAVES * VALUES : SUMS;
-    static constexpr int SEEN = LIST + WAVES * 2048, BYTES = SEEN + WAVES * 2048;
-    // chunk c of token k stands at chunk c ^ swizzle(k): a quarter of the chunks for four tokens of a transposing read, all of them
-    // for sixteen tokens of a write
+    // LDS: 32 values of each wave, two units' keys and values in their place (unit sums before them) | drafted nodes of each team's
+    // trajectory | nodes that a wave's rows see
+    static constexpr int VALUES = 32 * ROW, STAGE = 2 * KT * ROW, ROWS = ALONE ? WAVES * VALUES : 2 * STAGE;
+    static_assert(ROWS >= WAVES * VALUES, "a wave's values have room");
+    static constexpr int LIST = ROWS > SUMS ? ROWS : SUMS, SEEN = LIST + TEAMS * 2048, SEEN_EACH = 2048 + 64, BYTES = SEEN + WAVES * SEEN_EACH;
     static __device__ __forceinline__ int tree_keys(int) { return 1; }
     static __device__ __forceinline__ int workgroups(const TreeAttn4Args &a) { return a.workgroups; }
-    static __device__ __forceinline__ int swizzle(int k) { return (D == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2) | ((k >> 2) & 3); }
+    // Element of a head that a lane's first one of product x is.
+    static __device__ __forceinline__ int element(int half, int x) { return ALONE ? D / 2 * half + 8 * x : 16 * x + 8 * half; }
+    // 16-byte chunk c of key k stands at chunk c ^ swizzle_k(k): reads of one chunk of 16 keys and writes of a block of each of four
+    // (two) keys touch every bank once.
+    static __device__ __forceinline__ int swizzle_k(int k) { return D == 128 ? k & 15 : (k >> 1) & 7; }
+    // Of a value: the transposing reads have four chunks of four tokens; writes have, ALONE, one chunk of 16 tokens, else as keys.
+    static __device__ __forceinline__ int swizzle_v(int k)
+    {
+        const int far = D == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
+        return far | (ALONE ? (k >> 2) & 3 : D == 128 ? k & 3 : (k >> 1) & 3);
+    }
+    static constexpr int EIGHT = ALONE ? 32 : 0;     // what it flips of an address eight tokens further on
 };
 
 // What a wave's lanes have written to LDS is read by others of them behind this (accesses of one wave are in order).
@@ -92,18 +107,22 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
     bool first_item = true;
     const Exponent ex = exponent_of(a.scale);
     const float c = ex.c;
-    uint16_t *const list = (uint16_t *)(attn_lds + S::LIST + wave * 2048), *const seen = (uint16_t *)(attn_lds + S::SEEN + wave * 2048);
-    const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char *)attn_lds) + wave * S::VALUES;
+    uint16_t *const list = (uint16_t *)(attn_lds + S::LIST + team * 2048), *const seen = (uint16_t *)(attn_lds + S::SEEN + wave * S::SEEN_EACH);
+    const uint32_t lds_begin = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_char *)attn_lds), lds0 = lds_begin + wave * S::VALUES;
     // where this lane's half of token `col` goes, its chunk 0 (chunk x: ^ x << 4), and where its reads of tokens 4 half + j4 and of
     // those eight further on begin
-    const uint32_t put = lds0 + col * S::ROW + (((4 * HB * half) ^ S::swizzle(col)) << 4);
+    const uint32_t put = lds0 + col * S::ROW + (((4 * HB * half) ^ S::swizzle_v(col)) << 4);
     const int piece = lane & 3, j4 = (lane >> 2) & 3, dsub = (lane >> 4) & 1;
-    const uint32_t get = lds0 + (4 * half + j4) * S::ROW + (((2 * dsub + (piece >> 1)) ^ S::swizzle(4 * half + j4)) << 4) + (piece & 1) * 8;
+    const uint32_t get = lds0 + (4 * half + j4) * S::ROW + (((2 * dsub + (piece >> 1)) ^ S::swizzle_v(4 * half + j4)) << 4) + (piece & 1) * 8;
 
     const int B = a.B;
     while (unit < unit_end && b < B) {
         // ---- the item: trajectory, key/value head, a team's rows ----
         const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
+        if constexpr (!S::ALONE) {                     // (everyone is done with the item before)
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            group_barrier();
+        }
         if (listed != b) {
             int base = 0;
             for (int u0 = 0; u0 < a.N; u0 += 256) {
@@ -115,18 +134,19 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     const int u = u0 + 64 * k + lane;
                     const bool there = u < a.N && tok[k] >= 0;
                     const unsigned long long bits = __ballot(there);
-                    if (there) list[base + __popcll(bits & ((1ull << lane) - 1))] = (uint16_t)u;
+                    if (wr == 0 && there) list[base + __popcll(bits & ((1ull << lane) - 1))] = (uint16_t)u;
                     base += __popcll(bits);
                 }
             }
             nodes = __builtin_amdgcn_readfirstlane(base);
             listed = b;
-            lanes_agree();
+            if constexpr (S::ALONE) lanes_agree();
+            else __syncthreads();
         }
         if (nodes == 0) { ++b; continue; }             // nothing drafted: no units
         const long long most = (long long)a.width << a.page_shift;
         const int len = __builtin_amdgcn_readfirstlane((int)clamp_length(a.len[b], most));
-        const int cache_units = (len + S::KT - 1) / S::KT, units = cache_units + 1, per_item = units + S::START;
+        const int cache_units = (len + S::KT - 1) / S::KT, units = cache_units + 1, per_item = units + S::START;   // (the first unit is the tree)
         const int all_rows = nodes * a.per_kv;
         const long long per_head = per_item * head_weight(all_rows, S::TM, S::HEAVY, S::LIGHT);
         const int heads_before = (int)quotient(unit - b_start, per_head);
@@ -134,7 +154,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
         const int tile = (int)quotient(unit - head_start, per_item);
         // (the groups of 32 rows in equal numbers for the head's tiles)
         const int row_groups = (all_rows + 31) / 32, tiles = (row_groups + S::WR - 1) / S::WR;
-        const int row0 = tile * row_groups / tiles * 32, rows = min(all_rows, (tile + 1) * row_groups / tiles * 32);
+        const int row0 = 32 * (int)quotient((long long)tile * row_groups, tiles), rows = min(all_rows, 32 * (int)quotient((tile + 1ll) * row_groups, tiles));
         const int hk = (heads_before + b) % a.kv_heads;   // (not the same head of all trajectories at one time)
         const long long item_start = head_start + (long long)tile * per_item, item_end = item_start + per_item;
         const int u0 = (int)units_before(unit - item_start, 1, S::START, units), u1 = (int)units_before(unit_end - item_start, 1, S::START, units);
@@ -150,26 +170,28 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
         const int row = row0 + wr * 32 + col, my_row = row < rows ? row : rows - 1;
         const int node = list[my_row / a.per_kv], head = hk * a.per_kv + my_row % a.per_kv;
 
-        if (row0 + wr * 32 < rows) {                   // this wave has rows
+        const bool busy = row0 + wr * 32 < rows;       // this wave has rows
+        if constexpr (S::ALONE)
+            if (!busy) __builtin_unreachable();
         float16v o[DT];
 #pragma unroll
         for (int i = 0; i < DT; ++i) o[i] = float16v{0};
         float m = -__builtin_huge_valf(), l = 0.0f;    // running maximum of the products with the keys, sum of the weights
-        uint4v q[DC];                                  // in the order of the lanes' halves of keys
+        uint4v q[DC];
         {
-            const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2] + D / 2 * half;
+            const uint16_t *qp = a.q + b * a.qs[0] + node * a.qs[1] + head * a.qs[2];
 #pragma unroll
-            for (int i = 0; i < DC; ++i) q[i] = *(const uint4v *)(qp + 8 * i);
+            for (int i = 0; i < DC; ++i) q[i] = *(const uint4v *)(qp + S::element(half, i));
         }
         // Weights of the scores t of 32 keys, their products with the values in LDS.
-        auto values = [&](float16v &t) {
+        auto values = [&](float16v &t, uint32_t get) {
             uint4v vf[2][DT];
 #pragma unroll
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)((get ^ (d << 6)) + 16 * k * S::ROW));
-                    const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)((get ^ (d << 6) ^ 32) + (16 * k + 8) * S::ROW));
+                    const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)((get ^ (d << 6) ^ S::EIGHT) + (16 * k + 8) * S::ROW));
                     vf[k][d] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
                 }
             float top = t[0];
@@ -190,7 +212,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
         };
 
         // ---- the tree: the nodes that these rows see ----
-        if (u0 == 0) {
+        if (busy && u0 == 0) {
             const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
             const uint32_t *anc = a.anc + (long long)node * a.anc_words;
             int count = 0;
@@ -209,21 +231,30 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     count += __popc(word);
                 }
             }
+            if (half == 0) seen[count + col] = 0;      // (the root, for what is left of the last 32)
             lanes_agree();
             for (int j0 = 0; j0 < count; j0 += 32) {
-                const int v = seen[min(j0 + col, count - 1)];
-                const uint16_t *kp = a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2] + D / 2 * half;
+                const int v = seen[j0 + col];
+                const uint16_t *kp = a.k_new + b * a.ks[0] + v * a.ks[1] + hk * a.ks[2];
                 const uint16_t *vp = a.v_new + b * a.vs[0] + v * a.vs[1] + hk * a.vs[2] + D / 2 * half;
+                // which of them this lane's row sees: bits of its 16 of the 32
+                uint2 ids[4];
+                uint32_t mine = 0, words[16];
+#pragma unroll
+                for (int g = 0; g < 4; ++g) ids[g] = *(const uint2 *)(seen + j0 + 8 * g + 4 * half);
+                auto node_at = [&](int x) { return (x & 2 ? ids[x / 4].y : ids[x / 4].x) >> (16 * (x & 1)) & 0xFFFFu; };
+#pragma unroll
+                for (int x = 0; x < 16; ++x) words[x] = anc[node_at(x) / 32];
                 uint4v kw[DC], vw[DC];
 #pragma unroll
-                for (int x = 0; x < DC; ++x) { kw[x] = *(const uint4v *)(kp + 8 * x); vw[x] = *(const uint4v *)(vp + 8 * x); }
-                // which of them this lane's row sees: bits of its 16 of the 32
-                uint32_t mine = 0;
+                for (int x = 0; x < DC; ++x) kw[x] = *(const uint4v *)(kp + S::element(half, x));
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int x = 0; x < 16; ++x) {
-                    const int j = 8 * (x / 4) + x % 4 + 4 * half, u = seen[min(j0 + j, count - 1)];
-                    mine |= (j0 + j < count ? anc[u / 32] >> (u & 31) & 1u : 0u) << j;
-                }
+                for (int x = 0; x < 16; ++x) mine |= (words[x] >> (node_at(x) & 31) & 1u) << (8 * (x / 4) + x % 4 + 4 * half);
+                if (count - j0 < 32) mine &= (1u << (count - j0)) - 1u;
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int x = 0; x < DC; ++x) vw[x] = *(const uint4v *)(vp + 8 * x);
                 // Values that are no finite numbers, of nodes that a row does not see, would reach it as 0 * infinity: they become
                 // zeros, and the rows that see them get them added below.
                 bool found = false;
@@ -236,7 +267,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                         found |= lo | hi;
                         vw[x][e] &= (lo ? 0u : 0xFFFFu) | (hi ? 0u : 0xFFFF0000u);
                     }
-                    *(lds_uint4v *)(uintptr_t)(put ^ (x << 4)) = vw[x];
+                    *(lds_uint4v *)(uintptr_t)(put ^ (x << 4)) = vw[x];   // (chunks D / 16 half + x)
                 }
                 const unsigned long long wild2 = __ballot(found && j0 + col < count);
                 float16v t = float16v{0};
@@ -244,7 +275,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 for (int x = 0; x < DC; ++x) t = mfma32<F16>(kw[x], q[x], t);
 #pragma unroll
                 for (int x = 0; x < 16; ++x) t[x] = mine >> (8 * (x / 4) + x % 4 + 4 * half) & 1u ? t[x] : -__builtin_huge_valf();
-                values(t);
+                values(t, get);
                 uint32_t wild = __builtin_amdgcn_readfirstlane((uint32_t)wild2 | (uint32_t)(wild2 >> 32));
                 const uint32_t all = mine | (uint32_t)__shfl_xor((int)mine, 32);
                 for (; wild; wild &= wild - 1) {
@@ -265,7 +296,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
 
         // ---- the cached keys of this share: blocks a unit ahead, page numbers two ----
         const int first = max(u0 - 1, 0), n = u1 - 1 - first;   // (the item's first unit is the tree)
-        if (n > 0) {
+        if (S::ALONE && n > 0) {
             const int32_t *table = a.table + (long long)b * a.width;
             const int page_shift = a.page_shift, pages = a.pages;
             const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
@@ -315,14 +346,110 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
 #pragma unroll
                     for (int x = 0; x < 16; ++x) t[x] = 8 * (x / 4) + x % 4 + 4 * half < left ? t[x] : -__builtin_huge_valf();
                 }
-                values(t);
+                values(t, get);
             }
         }
+        if constexpr (!S::ALONE)
+            if (n > 0) {
+                // every thread has MINE blocks of a unit: loaded two units ahead of the products, converted into LDS one
+                const int32_t *table = a.table + (long long)b * a.width;
+                const int page_shift = a.page_shift, pages = a.pages;
+                const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
+                const uint32_t scale_page = (uint32_t)(a.scale_page / S::BLOCKS), scale_slot = (uint32_t)(a.scale_slot / S::BLOCKS);
+                const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4), *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4);
+                const uint8_t *k_scale = a.k_scale + hk * a.scale_head, *v_scale = a.v_scale + hk * a.scale_head;
+                constexpr int HALF = S::KT * S::BLOCKS;          // the first half of a unit's blocks are keys
+                const int mine = (int)threadIdx.x % HALF, my_key = mine / S::BLOCKS, my_piece = mine % S::BLOCKS;
+                const bool mine_v = (int)threadIdx.x >= HALF;    // (MINE 1; with two, one of a key and one of a value)
+                static_assert(S::MINE == 1 ? 2 * HALF == S::THREADS : S::MINE == 2 && HALF == S::THREADS, "who has which block");
+                const uint4v *pool[S::MINE];
+                const uint8_t *scales[S::MINE];
+                uint32_t to[S::MINE];
+#pragma unroll
+                for (int r = 0; r < S::MINE; ++r) {
+                    const bool is_v = S::MINE == 1 ? mine_v : r == 1;
+                    pool[r] = (is_v ? v_pool : k_pool) + my_piece;
+                    scales[r] = (is_v ? v_scale : k_scale) + my_piece;
+                    to[r] = lds_begin + (is_v ? S::KT * S::ROW : 0) + my_key * S::ROW + (((4 * my_piece) ^ (is_v ? S::swizzle_v(my_key) : S::swizzle_k(my_key))) << 4);
+                }
+                constexpr int AHEAD = S::AHEAD;
+                uint4v block[AHEAD][S::MINE];
+                uint32_t scale[AHEAD][S::MINE];
+                auto key_of = [&](int i) { return min((first + i) * S::KT + my_key, len - 1); };   // behind the end: the last key again, weighted with zero
+                auto page_of = [&](int i) { return table[key_of(i) >> page_shift]; };
+                auto load = [&](int i, int page, uint4v *block, uint32_t *scale) {
+                    const int key = key_of(i);
+                    const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
+                    const unsigned long long from = at * pool_page + place * pool_slot;
+                    const unsigned long long sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * S::BLOCKS;
+#pragma unroll
+                    for (int r = 0; r < S::MINE; ++r) {
+                        block[r] = pool[r][from];
+                        scale[r] = scales[r][sfrom];
+                    }
+                };
+                auto store = [&](int i, const uint4v *block, const uint32_t *scale) {
+#pragma unroll
+                    for (int r = 0; r < S::MINE; ++r) {
+                        const float factor = mx4_factor(scale[r]);
+#pragma unroll
+                        for (int x = 0; x < 4; ++x)
+                            *(lds_uint4v *)(uintptr_t)((to[r] ^ (x << 4)) + (i & 1) * S::STAGE) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[r][x], factor));
+                    }
+                };
+                {
+                    int page[AHEAD];
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) page[u] = page_of(u);
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u) load(u, page[u], block[u], scale[u]);
+                }
+                int page = page_of(AHEAD);
+                asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                group_barrier();                                 // (everyone is done with the tree)
+                store(0, block[0], scale[0]);
+                load(AHEAD, page, block[0], scale[0]);
+                page = page_of(AHEAD + 1);
+                const uint32_t k_at = lds_begin + col * S::ROW + ((half ^ S::swizzle_k(col)) << 4), v_at = get - lds0 + lds_begin + S::KT * S::ROW;
+                auto unit_of_keys = [&](int i, uint4v *block, uint32_t *scale) {   // the place of unit i + 1
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    group_barrier();                             // the unit's keys and values are there, those of the one before done with
+                    const uint32_t stage = (i & 1) * S::STAGE;
+                    uint4v kf[DC];
+                    auto read_keys = [&](int t) {
+#pragma unroll
+                        for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)((k_at ^ (x << 5)) + stage + t * 32 * S::ROW);
+                    };
+                    if (busy) read_keys(0);
+                    store(i + 1, block, scale);                  // (past the last unit: that one's last key again)
+                    load(i + 1 + AHEAD, page, block, scale);
+                    page = page_of(i + 2 + AHEAD);
+                    if (busy) {
+#pragma unroll
+                        for (int t = 0; t < S::SUB; ++t) {
+                            if (t > 0) read_keys(t);
+                            float16v s = float16v{0};
+#pragma unroll
+                            for (int x = 0; x < DC; ++x) s = mfma32<F16>(kf[x], q[x], s);
+                            const int left = len - (first + i) * S::KT - 32 * t;
+                            if (left < 32) {
+#pragma unroll
+                                for (int x = 0; x < 16; ++x) s[x] = 8 * (x / 4) + x % 4 + 4 * half < left ? s[x] : -__builtin_huge_valf();
+                            }
+                            if (left > 0) values(s, v_at + stage + t * 32 * S::ROW);
+                        }
+                    }
+                };
+                for (int i0 = 0; i0 < n; i0 += AHEAD)
+#pragma unroll
+                    for (int u = 0; u < AHEAD; ++u)
+                        if (i0 + u < n) unit_of_keys(i0 + u, block[(u + 1) % AHEAD], scale[(u + 1) % AHEAD]);
+            }
 
         // ---- the rows' outputs, or this wave's part of them ----
         l = other_half_sum(l);
         m = fmaxf(m, kLowest);                         // (nothing seen: differences of maxima are numbers)
-        if (row < rows) {
+        if (busy && row < rows) {
             const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
             if (u0 == 0 && u1 == units) {
                 const float r = 1.0f / l;
@@ -344,7 +471,6 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     for (int i = 0; i < 4; ++i) to4[(4 * d + i) * 64] = float4v{o[d][4 * i], o[d][4 * i + 1], o[d][4 * i + 2], o[d][4 * i + 3]};
                 if (leads && half == 0) a.place[w * S::TM + at] = b * a.os[0] + node * a.os[1] + head * a.os[2];
             }
-        }
         }
         if (u1 < units) break;
         unit = item_end;
