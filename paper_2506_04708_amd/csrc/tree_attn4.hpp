@@ -35,15 +35,15 @@ struct Attn4Shape {
     static constexpr int WAVES = ALONE ? 4 : WR, THREADS = 64 * WAVES, MIN_WAVES = 2;
     static constexpr int TEAMS = WAVES / WR, TM = 32 * WR;   // shares of a workgroup, rows of one
     static constexpr int KT = ALONE || D == 128 ? 32 : 64, SUB = KT / 32;   // keys of a unit
-    static constexpr int AHEAD = WR == 4 ? 4 : 2;    // units whose blocks are on their way
+    static constexpr int AHEAD = 2;    // units whose blocks are on their way
     static constexpr int START = 6, HEAVY = 1, LIGHT = 1;
     static constexpr int ROW = 2 * D, CPR = D / 8;   // bytes and 16-byte chunks of a token's key or value
     static constexpr int BLOCKS = D / kMx4Block, MINE = 2 * KT * BLOCKS / THREADS;   // blocks of a key, of a thread in a unit
     static_assert(ALONE || MINE * THREADS == 2 * KT * BLOCKS, "a unit's blocks are shared out evenly");
     static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
-    // LDS: 32 values of each wave, two units' keys and values in their place (unit sums before them) | drafted nodes of each team's
+    // LDS: 32 values of each wave, three units' keys and values in their place (unit sums before them) | drafted nodes of each team's
     // trajectory | nodes that a wave's rows see
-    static constexpr int VALUES = 32 * ROW, STAGE = 2 * KT * ROW, ROWS = ALONE ? WAVES * VALUES : 2 * STAGE;
+    static constexpr int VALUES = 32 * ROW, STAGE = 2 * KT * ROW, ROWS = ALONE ? WAVES * VALUES : 3 * STAGE;
     static_assert(ROWS >= WAVES * VALUES, "a wave's values have room");
     static constexpr int LIST = ROWS > SUMS ? ROWS : SUMS, SEEN = LIST + TEAMS * 2048, SEEN_EACH = 2048 + 64, BYTES = SEEN + WAVES * SEEN_EACH;
     static __device__ __forceinline__ int tree_keys(int) { return 1; }
@@ -183,6 +183,13 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
 #pragma unroll
             for (int i = 0; i < DC; ++i) q[i] = *(const uint4v *)(qp + S::element(half, i));
         }
+        // Scores of keys that are not among the first `left` of 32 count for nothing.
+        auto mask_tail = [&](float16v &t, int left) {
+            int from = left - 4 * half;
+            asm volatile("" : "+v"(from));             // (compared with constants, not sixteen sums kept in registers)
+#pragma unroll
+            for (int x = 0; x < 16; ++x) t[x] = 8 * (x / 4) + x % 4 < from ? t[x] : -__builtin_huge_valf();
+        };
         // Weights of the scores t of 32 keys, their products with the values in LDS.
         auto values = [&](float16v &t, uint32_t get) {
             uint4v vf[2][DT];
@@ -342,10 +349,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     page = table[key_of(i + 2) >> page_shift];
                 }
                 const int left = len - (first + i) * S::KT;
-                if (left < 32) {
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) t[x] = 8 * (x / 4) + x % 4 + 4 * half < left ? t[x] : -__builtin_huge_valf();
-                }
+                if (left < 32) mask_tail(t, left);
                 values(t, get);
             }
         }
@@ -388,62 +392,142 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                         scale[r] = scales[r][sfrom];
                     }
                 };
-                auto store = [&](int i, const uint4v *block, const uint32_t *scale) {
+                auto store_word = [&](const uint4v *block, const uint32_t *scale, uint32_t stage, int x) {
 #pragma unroll
-                    for (int r = 0; r < S::MINE; ++r) {
-                        const float factor = mx4_factor(scale[r]);
-#pragma unroll
-                        for (int x = 0; x < 4; ++x)
-                            *(lds_uint4v *)(uintptr_t)((to[r] ^ (x << 4)) + (i & 1) * S::STAGE) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[r][x], factor));
-                    }
+                    for (int r = 0; r < S::MINE; ++r)
+                        *(lds_uint4v *)(uintptr_t)((to[r] ^ (x << 4)) + stage) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[r][x], mx4_factor(scale[r])));
                 };
-                {
-                    int page[AHEAD];
+                // (page numbers as far ahead of the blocks as those of the conversions: loads come back in order, and a wait for a
+                // page number is one for all blocks before it)
+                int page[AHEAD];
 #pragma unroll
-                    for (int u = 0; u < AHEAD; ++u) page[u] = page_of(u);
+                for (int u = 0; u < AHEAD; ++u) page[u] = page_of(u);
 #pragma unroll
-                    for (int u = 0; u < AHEAD; ++u) load(u, page[u], block[u], scale[u]);
-                }
-                int page = page_of(AHEAD);
+                for (int u = 0; u < AHEAD; ++u) load(u, page[u], block[u], scale[u]);
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) page[u] = page_of(AHEAD + u);
+                __builtin_amdgcn_sched_barrier(0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 group_barrier();                                 // (everyone is done with the tree)
-                store(0, block[0], scale[0]);
-                load(AHEAD, page, block[0], scale[0]);
-                page = page_of(AHEAD + 1);
                 const uint32_t k_at = lds_begin + col * S::ROW + ((half ^ S::swizzle_k(col)) << 4), v_at = get - lds0 + lds_begin + S::KT * S::ROW;
-                auto unit_of_keys = [&](int i, uint4v *block, uint32_t *scale) {   // the place of unit i + 1
-                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-                    group_barrier();                             // the unit's keys and values are there, those of the one before done with
-                    const uint32_t stage = (i & 1) * S::STAGE;
-                    uint4v kf[DC];
-                    auto read_keys = [&](int t) {
+                // Two steps at a time, 32 keys apart: scores of these keys, in whose products' shadow the weights of the keys before are made; then
+                // the products of those with their values, beside the search for these keys' maximum and the next unit's conversion.  A wave
+                // issues in order, so vector instructions between the matrix instructions are what keeps both units busy.
+                float top = -__builtin_huge_valf();
+                auto step = [&](auto have_old, auto have_new, float16v &old, float16v &now, uint32_t k_off, uint32_t v_off, int left, auto fill) {
+                    constexpr bool OLD = decltype(have_old)::value, NEW = decltype(have_new)::value;
+                    constexpr int PER = 16 / DC, READS = 2 * DT / DC;
+                    uint4v kf[DC], vf[2 * DT];
+                    if constexpr (NEW) {
 #pragma unroll
-                        for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)((k_at ^ (x << 5)) + stage + t * 32 * S::ROW);
-                    };
-                    if (busy) read_keys(0);
-                    store(i + 1, block, scale);                  // (past the last unit: that one's last key again)
-                    load(i + 1 + AHEAD, page, block, scale);
-                    page = page_of(i + 2 + AHEAD);
-                    if (busy) {
+                        for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)((k_at ^ (x << 5)) + k_off);
+                        now = float16v{0};
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                    float shift = 0.0f;
+                    float16v *const of[1] = {&old};
+                    if constexpr (OLD) shift = raise_row<F16>(ex, other_half_max(top), m, l, o, of);
+                    uint32_t p[8];
+                    float e[2][PER];
 #pragma unroll
-                        for (int t = 0; t < S::SUB; ++t) {
-                            if (t > 0) read_keys(t);
-                            float16v s = float16v{0};
+                    for (int x = 0; x <= DC; ++x) {
+                        if (x < DC) {
+                            if constexpr (NEW) now = mfma32<F16>(kf[x], q[x], now);
+                            if constexpr (OLD) {
 #pragma unroll
-                            for (int x = 0; x < DC; ++x) s = mfma32<F16>(kf[x], q[x], s);
-                            const int left = len - (first + i) * S::KT - 32 * t;
-                            if (left < 32) {
+                                for (int y = x * READS; y < (x + 1) * READS; ++y) {
+                                    const uint32_t at = ((v_at + v_off) ^ (y % DT << 6)) + 16 * (y / DT) * S::ROW;
+                                    const short4v a0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)at);
+                                    const short4v a1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_short4v *)(uintptr_t)(at + 8 * S::ROW));
+                                    vf[y] = __builtin_bit_cast(uint4v, __builtin_shufflevector(a0, a1, 0, 1, 2, 3, 4, 5, 6, 7));
+                                }
 #pragma unroll
-                                for (int x = 0; x < 16; ++x) s[x] = 8 * (x / 4) + x % 4 + 4 * half < left ? s[x] : -__builtin_huge_valf();
+                                for (int y = 0; y < PER; ++y) e[x & 1][y] = __builtin_amdgcn_exp2f(fmaf(old[x * PER + y], c, shift));
                             }
-                            if (left > 0) values(s, v_at + stage + t * 32 * S::ROW);
                         }
+                        if constexpr (OLD)
+                            if (x > 0) {
+#pragma unroll
+                                for (int y = 0; y < PER; y += 2) {
+                                    const int at = ((x - 1) * PER + y) / 2;
+                                    p[at] = pack2<F16>(e[(x - 1) & 1][y], e[(x - 1) & 1][y + 1]);
+                                    l = add2<F16>(p[at], l);
+                                    asm volatile("" : "+v"(p[at]), "+v"(l));   // (made here, not where they are used)
+                                }
+                            }
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                    if constexpr (NEW) {
+                        if (left < 32) mask_tail(now, left);
+                        top = now[0];
+                    }
+#pragma unroll
+                    for (int y = 0; y < 2 * DT; ++y) {
+                        const int k = y / DT;
+                        if constexpr (OLD) o[y % DT] = mfma32<F16>(vf[y], uint4v{p[4 * k], p[4 * k + 1], p[4 * k + 2], p[4 * k + 3]}, o[y % DT]);
+                        constexpr int EACH = 8 / DT;
+                        if constexpr (NEW) {
+#pragma unroll
+                            for (int x = 0; x < EACH; ++x) top = fmaxf(top, now[y * EACH + x]);
+                        }
+                        fill(y);
+                        __builtin_amdgcn_sched_barrier(0);
                     }
                 };
-                for (int i0 = 0; i0 < n; i0 += AHEAD)
+                using Yes = std::true_type;
+                using No = std::false_type;
+                auto no_fill = [](int) {};
+                float16v even = float16v{0}, odd = float16v{0};
+                #pragma unroll
+                for (int x = 0; x < 4; ++x) store_word(block[0], scale[0], 0, x);
+                load(AHEAD, page[0], block[0], scale[0]);
+                __builtin_amdgcn_sched_barrier(0);
+                page[0] = page_of(2 * AHEAD);
+                __builtin_amdgcn_sched_barrier(0);
+                uint32_t before = 0, here = 0, next = S::STAGE;  // places of the units: the one before, this one, the next
+                auto unit_of_keys = [&](auto have_old, auto is_odd, int i, uint4v *block, uint32_t *scale, int &page) {   // block: of unit i + 1
+                    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+                    group_barrier();                             // the unit's keys and values are there, those of two units before done with
+                    const int left = len - (first + i) * S::KT;
+                    auto fill = [&](int y) {                     // (past the last unit: that one's last key again)
+                        if (y % (2 * DT / 4) == 0) store_word(block, scale, next, y / (2 * DT / 4));
+                    };
+                    if (!busy) {
 #pragma unroll
-                    for (int u = 0; u < AHEAD; ++u)
-                        if (i0 + u < n) unit_of_keys(i0 + u, block[(u + 1) % AHEAD], scale[(u + 1) % AHEAD]);
+                        for (int x = 0; x < 4; ++x) store_word(block, scale, next, x);
+                    } else if constexpr (S::SUB == 1) {
+                        if constexpr (decltype(is_odd)::value) step(have_old, Yes{}, even, odd, here, before, left, fill);
+                        else step(have_old, Yes{}, odd, even, here, before, left, fill);
+                    } else {
+                        step(have_old, Yes{}, odd, even, here, before + 32 * S::ROW, left, fill);
+                        step(Yes{}, Yes{}, even, odd, here + 32 * S::ROW, here, left - 32, no_fill);
+                    }
+                    load(i + 1 + AHEAD, page, block, scale);
+                    __builtin_amdgcn_sched_barrier(0);
+                    page = page_of(i + 1 + 2 * AHEAD);
+                    __builtin_amdgcn_sched_barrier(0);
+                    before = here; here = next; next = next == 2 * S::STAGE ? 0 : next + S::STAGE;
+                };
+                unit_of_keys(No{}, No{}, 0, block[1 % AHEAD], scale[1 % AHEAD], page[1 % AHEAD]);
+                static_assert(AHEAD % 2 == 0, "a place's units are all odd or all even");
+                // (left in the middle, never skipped: the compiler counts the loads on their way along every path it sees)
+                if (n > 1)
+                    for (int i = 1;;) {
+                        bool done = false;
+#pragma unroll
+                        for (int u = 0; u < AHEAD; u += 2) {
+                            unit_of_keys(Yes{}, Yes{}, i, block[(u + 2) % AHEAD], scale[(u + 2) % AHEAD], page[(u + 2) % AHEAD]);
+                            if (++i >= n) { done = true; break; }
+                            unit_of_keys(Yes{}, No{}, i, block[(u + 3) % AHEAD], scale[(u + 3) % AHEAD], page[(u + 3) % AHEAD]);
+                            if (++i >= n) { done = true; break; }
+                        }
+                        if (done) break;
+                    }
+                if (busy) {
+                    if (S::SUB == 1 && (n & 1)) odd = even;
+                    step(Yes{}, No{}, odd, even, 0, before + (S::SUB - 1) * 32 * S::ROW, 0, no_fill);
+                }
             }
 
         // ---- the rows' outputs, or this wave's part of them ----
