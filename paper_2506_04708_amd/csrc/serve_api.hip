@@ -65,15 +65,11 @@ auto with_attn_shape(AttnForm f, Call call)
     default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2>{});
     }
 }
-// Over a cache of 4 bits: one, two or four waves of rows with the same keys.
+// Over a cache of 4 bits: up to 64 rows a wave for each 32, more than that four waves of rows with the same keys.
 template <int D, bool F16, typename Call>
 auto with_attn4_shape(AttnForm f, Call call)
 {
-    switch (f) {
-    case kAttn32: return call(Attn4Shape<D, F16, 1>{});
-    case kAttn64: return call(Attn4Shape<D, F16, 2>{});
-    default: return call(Attn4Shape<D, F16, 4>{});
-    }
+    return f == kAttnMore ? call(Attn4Shape<D, F16, 4>{}) : call(Attn4Shape<D, F16, 1>{});
 }
 template <typename Call>
 auto with_attn_shape(const stand_cache *c, AttnForm f, Call call)

@@ -27,7 +27,7 @@ struct TreeAttn4Args : TreeAttnArgs {                // k_pool, v_pool: blocks o
     int workgroups;
 };
 
-// A form.  WR = 1: every wave of a workgroup works by itself.  WR = 2, 4: the workgroup's waves have 32 rows each and the same keys.
+// A form.  WR = 1: every wave of a workgroup works by itself.  WR = 4: the workgroup's waves have 32 rows each and the same keys.
 template <int D_, bool F16_, int WR_>
 struct Attn4Shape {
     static constexpr int D = D_, WR = WR_;
@@ -35,7 +35,8 @@ struct Attn4Shape {
     static constexpr int WAVES = ALONE ? 4 : WR, THREADS = 64 * WAVES, MIN_WAVES = 2;
     static constexpr int TEAMS = WAVES / WR, TM = 32 * WR;   // shares of a workgroup, rows of one
     static constexpr int KT = ALONE || D == 128 ? 32 : 64, SUB = KT / 32;   // keys of a unit
-    static constexpr int AHEAD = 2;    // units whose blocks are on their way
+    // units whose blocks are on their way (ALONE with two: decoding 220 us instead of 214, 60 000 tokens of 48 rows 62 instead of 56)
+    static constexpr int AHEAD = ALONE ? 1 : 2;
     static constexpr int START = 6, HEAVY = 1, LIGHT = 1;
     static constexpr int ROW = 2 * D, CPR = D / 8;   // bytes and 16-byte chunks of a token's key or value
     static constexpr int BLOCKS = D / kMx4Block, MINE = 2 * KT * BLOCKS / THREADS;   // blocks of a key, of a thread in a unit
@@ -43,17 +44,17 @@ struct Attn4Shape {
     static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
     // LDS: 32 values of each wave, three units' keys and values in their place (unit sums before them) | drafted nodes of each team's
     // trajectory | nodes that a wave's rows see
-    static constexpr int VALUES = 32 * ROW, STAGE = 2 * KT * ROW, ROWS = ALONE ? WAVES * VALUES : 3 * STAGE;
+    static constexpr int KEY_ROW = ROW + 16, KEYS = KT * KEY_ROW;
+    static constexpr int VALUES = 32 * ROW, STAGE = KEYS + KT * ROW, ROWS = ALONE ? WAVES * VALUES : 3 * STAGE;
     static_assert(ROWS >= WAVES * VALUES, "a wave's values have room");
     static constexpr int LIST = ROWS > SUMS ? ROWS : SUMS, SEEN = LIST + TEAMS * 2048, SEEN_EACH = 2048 + 64, BYTES = SEEN + WAVES * SEEN_EACH;
     static __device__ __forceinline__ int tree_keys(int) { return 1; }
     static __device__ __forceinline__ int workgroups(const TreeAttn4Args &a) { return a.workgroups; }
     // Element of a head that a lane's first one of product x is.
     static __device__ __forceinline__ int element(int half, int x) { return ALONE ? D / 2 * half + 8 * x : 16 * x + 8 * half; }
-    // 16-byte chunk c of key k stands at chunk c ^ swizzle_k(k): reads of one chunk of 16 keys and writes of a block of each of four
-    // (two) keys touch every bank once.
-    static __device__ __forceinline__ int swizzle_k(int k) { return D == 128 ? k & 15 : (k >> 1) & 7; }
-    // Of a value: the transposing reads have four chunks of four tokens; writes have, ALONE, one chunk of 16 tokens, else as keys.
+    // Keys stand in rows of KEY_ROW bytes: reads of one chunk of 16 keys and writes of a block of each of four (two) keys touch
+    // every bank once, and a lane's chunks are a constant apart.  16-byte chunk c of value k stands at chunk c ^ swizzle_v(k): the
+    // transposing reads have four chunks of four tokens; writes have, ALONE, one chunk of 16 tokens, else as keys.
     static __device__ __forceinline__ int swizzle_v(int k)
     {
         const int far = D == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
@@ -308,49 +309,67 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
             const int page_shift = a.page_shift, pages = a.pages;
             const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
             const uint32_t scale_page = (uint32_t)(a.scale_page / (2 * HB)), scale_slot = (uint32_t)(a.scale_slot / (2 * HB));
+            // scales in the order of their blocks: a block's number is its scale's
+            const bool alike = pool_page == a.scale_page && pool_slot == a.scale_slot;
             const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4) + HB * half, *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4) + HB * half;
             const uint8_t *k_scale = a.k_scale + hk * a.scale_head + HB * half, *v_scale = a.v_scale + hk * a.scale_head + HB * half;
-            uint4v kb[HB], vb[HB];
-            uint32_t ks, vs;                           // a byte for each block
+            constexpr int AHEAD = S::AHEAD;
+            uint4v kb[AHEAD][HB], vb[AHEAD][HB];
+            uint32_t ks[AHEAD], vs[AHEAD];             // a byte for each block
+            int page[AHEAD];
             auto key_of = [&](int i) { return min((first + i) * S::KT + col, len - 1); };   // behind the end: the last key again, weighted with zero
-            auto load = [&](int i, int page) {
+            auto page_of = [&](int i) { return table[key_of(i) >> page_shift]; };
+            auto load = [&](int i, int u) {
                 const int key = key_of(i);
-                const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
-                const uint32_t from = at * pool_page + place * pool_slot;
-                const unsigned long long sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * (2 * HB);
+                const uint32_t at = (uint32_t)clamp_page(page[u], pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
+                const unsigned long long from = at * pool_page + place * pool_slot;
+                unsigned long long sfrom = from;
+                if (!alike) sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * (2 * HB);
 #pragma unroll
                 for (int r = 0; r < HB; ++r) {
-                    kb[r] = k_pool[(unsigned long long)from + r];
-                    vb[r] = v_pool[(unsigned long long)from + r];
+                    kb[u][r] = k_pool[from + r];
+                    vb[u][r] = v_pool[from + r];
                 }
                 if constexpr (HB == 2) {
-                    ks = *(const uint16_t *)(k_scale + sfrom);
-                    vs = *(const uint16_t *)(v_scale + sfrom);
+                    ks[u] = *(const uint16_t *)(k_scale + sfrom);
+                    vs[u] = *(const uint16_t *)(v_scale + sfrom);
                 } else {
-                    ks = k_scale[sfrom];
-                    vs = v_scale[sfrom];
+                    ks[u] = k_scale[sfrom];
+                    vs[u] = v_scale[sfrom];
                 }
+                __builtin_amdgcn_sched_barrier(0);
+                page[u] = page_of(i + AHEAD);          // (behind the blocks, and used when they have come)
+                __builtin_amdgcn_sched_barrier(0);
             };
-            load(0, table[key_of(0) >> page_shift]);
-            int page = table[key_of(1) >> page_shift];
-            for (int i = 0; i < n; ++i) {
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) page[u] = page_of(u);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) load(u, u);
+            auto unit_of_keys = [&](int i, int u) {
                 float16v t = float16v{0};
 #pragma unroll
                 for (int r = 0; r < HB; ++r) {
-                    const float kf = mx4_factor(ks >> (8 * r) & 255u), vf = mx4_factor(vs >> (8 * r) & 255u);
+                    const float kf = mx4_factor(ks[u] >> (8 * r) & 255u), vf = mx4_factor(vs[u] >> (8 * r) & 255u);
 #pragma unroll
                     for (int x = 0; x < 4; ++x) {
-                        t = mfma32<F16>(__builtin_bit_cast(uint4v, mx4_eight<F16>(kb[r][x], kf)), q[4 * r + x], t);
-                        *(lds_uint4v *)(uintptr_t)(put ^ ((4 * r + x) << 4)) = __builtin_bit_cast(uint4v, mx4_eight<F16>(vb[r][x], vf));
+                        t = mfma32<F16>(__builtin_bit_cast(uint4v, mx4_eight<F16>(kb[u][r][x], kf)), q[4 * r + x], t);
+                        *(lds_uint4v *)(uintptr_t)(put ^ ((4 * r + x) << 4)) = __builtin_bit_cast(uint4v, mx4_eight<F16>(vb[u][r][x], vf));
                     }
                 }
-                if (i + 1 < n) {
-                    load(i + 1, page);
-                    page = table[key_of(i + 2) >> page_shift];
-                }
+                load(i + AHEAD, u);
                 const int left = len - (first + i) * S::KT;
                 if (left < 32) mask_tail(t, left);
                 values(t, get);
+            };
+            // (left in the middle, never skipped: the compiler counts the loads on their way along every path it sees)
+            for (int i = 0;;) {
+                bool done = false;
+#pragma unroll
+                for (int u = 0; u < AHEAD; ++u) {
+                    unit_of_keys(i, u);
+                    if (++i >= n) { done = true; break; }
+                }
+                if (done) break;
             }
         }
         if constexpr (!S::ALONE)
@@ -360,6 +379,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 const int page_shift = a.page_shift, pages = a.pages;
                 const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
                 const uint32_t scale_page = (uint32_t)(a.scale_page / S::BLOCKS), scale_slot = (uint32_t)(a.scale_slot / S::BLOCKS);
+                // scales in the order of their blocks: a block's number is its scale's
+                const bool alike = pool_page == a.scale_page && pool_slot == a.scale_slot;
                 const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4), *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4);
                 const uint8_t *k_scale = a.k_scale + hk * a.scale_head, *v_scale = a.v_scale + hk * a.scale_head;
                 constexpr int HALF = S::KT * S::BLOCKS;          // the first half of a unit's blocks are keys
@@ -368,13 +389,16 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 static_assert(S::MINE == 1 ? 2 * HALF == S::THREADS : S::MINE == 2 && HALF == S::THREADS, "who has which block");
                 const uint4v *pool[S::MINE];
                 const uint8_t *scales[S::MINE];
-                uint32_t to[S::MINE];
+                uint32_t to[S::MINE][4];                         // where its four chunks go
 #pragma unroll
                 for (int r = 0; r < S::MINE; ++r) {
                     const bool is_v = S::MINE == 1 ? mine_v : r == 1;
                     pool[r] = (is_v ? v_pool : k_pool) + my_piece;
                     scales[r] = (is_v ? v_scale : k_scale) + my_piece;
-                    to[r] = lds_begin + (is_v ? S::KT * S::ROW : 0) + my_key * S::ROW + (((4 * my_piece) ^ (is_v ? S::swizzle_v(my_key) : S::swizzle_k(my_key))) << 4);
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        to[r][x] = lds_begin + (is_v ? S::KEYS + my_key * S::ROW + (((4 * my_piece + x) ^ S::swizzle_v(my_key)) << 4)
+                                                     : my_key * S::KEY_ROW + 16 * (4 * my_piece + x));
                 }
                 constexpr int AHEAD = S::AHEAD;
                 uint4v block[AHEAD][S::MINE];
@@ -385,7 +409,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     const int key = key_of(i);
                     const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
                     const unsigned long long from = at * pool_page + place * pool_slot;
-                    const unsigned long long sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * S::BLOCKS;
+                    unsigned long long sfrom = from;
+                    if (!alike) sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * S::BLOCKS;
 #pragma unroll
                     for (int r = 0; r < S::MINE; ++r) {
                         block[r] = pool[r][from];
@@ -395,7 +420,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 auto store_word = [&](const uint4v *block, const uint32_t *scale, uint32_t stage, int x) {
 #pragma unroll
                     for (int r = 0; r < S::MINE; ++r)
-                        *(lds_uint4v *)(uintptr_t)((to[r] ^ (x << 4)) + stage) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[r][x], mx4_factor(scale[r])));
+                        *(lds_uint4v *)(uintptr_t)(to[r][x] + stage) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[r][x], mx4_factor(scale[r])));
                 };
                 // (page numbers as far ahead of the blocks as those of the conversions: loads come back in order, and a wait for a
                 // page number is one for all blocks before it)
@@ -410,7 +435,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 __builtin_amdgcn_sched_barrier(0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 group_barrier();                                 // (everyone is done with the tree)
-                const uint32_t k_at = lds_begin + col * S::ROW + ((half ^ S::swizzle_k(col)) << 4), v_at = get - lds0 + lds_begin + S::KT * S::ROW;
+                const uint32_t k_at = lds_begin + col * S::KEY_ROW + 16 * half, v_at = get - lds0 + lds_begin + S::KEYS;
                 // Two steps at a time, 32 keys apart: scores of these keys, in whose products' shadow the weights of the keys before are made; then
                 // the products of those with their values, beside the search for these keys' maximum and the next unit's conversion.  A wave
                 // issues in order, so vector instructions between the matrix instructions are what keeps both units busy.
@@ -421,7 +446,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     uint4v kf[DC], vf[2 * DT];
                     if constexpr (NEW) {
 #pragma unroll
-                        for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)((k_at ^ (x << 5)) + k_off);
+                        for (int x = 0; x < DC; ++x) kf[x] = *(const lds_uint4v *)(uintptr_t)(k_at + k_off + 32 * x);
                         now = float16v{0};
                     }
                     __builtin_amdgcn_sched_barrier(0);
@@ -460,7 +485,6 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     }
                     if constexpr (NEW) {
                         if (left < 32) mask_tail(now, left);
-                        top = now[0];
                     }
 #pragma unroll
                     for (int y = 0; y < 2 * DT; ++y) {
@@ -469,7 +493,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                         constexpr int EACH = 8 / DT;
                         if constexpr (NEW) {
 #pragma unroll
-                            for (int x = 0; x < EACH; ++x) top = fmaxf(top, now[y * EACH + x]);
+                            for (int x = 0; x < EACH; ++x) top = y + x == 0 ? now[0] : fmaxf(top, now[y * EACH + x]);
                         }
                         fill(y);
                         __builtin_amdgcn_sched_barrier(0);
@@ -501,7 +525,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                         else step(have_old, Yes{}, odd, even, here, before, left, fill);
                     } else {
                         step(have_old, Yes{}, odd, even, here, before + 32 * S::ROW, left, fill);
-                        step(Yes{}, Yes{}, even, odd, here + 32 * S::ROW, here, left - 32, no_fill);
+                        step(Yes{}, Yes{}, even, odd, here + 32 * S::KEY_ROW, here, left - 32, no_fill);
                     }
                     load(i + 1 + AHEAD, page, block, scale);
                     __builtin_amdgcn_sched_barrier(0);
