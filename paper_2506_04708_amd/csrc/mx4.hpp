@@ -70,6 +70,19 @@ __device__ __forceinline__ uint2 mx4_half_block(const float *x, uint32_t &scale)
     return uint2{mx4_pack(x, factor), mx4_pack(x + 8, factor)};
 }
 
+// A quarter of a block, 8 elements, of every lane; four neighbours have a block.
+template <bool F16>
+__device__ __forceinline__ uint32_t mx4_quarter_block(const float *x, uint32_t &scale)
+{
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, mx4_magnitude(x[i]));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
+    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
+    scale = (uint32_t)mx4_scale(top, F16);
+    return mx4_pack(x, mx4_factor(scale));
+}
+
 // Two 16-bit elements of a word as fp32.
 template <bool F16> __device__ __forceinline__ float row_low(uint32_t w)
 {

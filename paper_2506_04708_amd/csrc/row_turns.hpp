@@ -11,6 +11,11 @@
 // A thread has 16 elements of a head, whole pairs of them (two pieces of 8 that lie half a rotation apart, or 16 in a row), so
 // that pairs need no exchange; D / 16 lanes have a head and add up their squares.  Workgroups have queries, keys or values, not a
 // mixture.  For 4 bits a key's elements change lanes through LDS, so that blocks are of neighbours.
+//
+// Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 24 us, 5.8 TB/s).  Trees
+// are bound by how little is on its way at a time: a wave asks for what its row is decided by, then for rows and cosines, and has
+// some 600 instructions for each head of its lanes between them and its stores (128 trees of 128 nodes, 16/8 heads of 128, 85 MB: 28 us; with 132
+// instead of 128 registers, three waves of a SIMD instead of four, 31; one head for a thread, its conversions for each, 34).
 #pragma once
 #include "cache_four.hpp"
 
@@ -23,12 +28,13 @@ struct TurnArgs {
     const float *turns;                              // [positions][2 * half]: cosines, sines
     const uint16_t *q_norm, *k_norm;
     double eps;
-    int positions, half, neighbours;
+    int positions, half;
     const int32_t *start, *count;                    // [B] or NULL (0; all rows)
     const int32_t *tok;                              // a tree's rows: [B][rows], < 0: not drafted; NULL: rows in a line
     const unsigned long long *anc;
     int anc_words;
     int rows, q_heads, kv_heads, q_groups, k_groups; // workgroups of a trajectory's queries, keys; the others have values
+    int q_step, k_step;                              // threads of a row's queries, of its keys (and values), in lots of D / 16
     const int64_t *slots;                            // [B][width]
     int width;
     long long slot_count;
@@ -39,8 +45,15 @@ enum TurnTarget { kTurnRows, kTurnCache16, kTurnCache4 };
 constexpr int kTurnThreads = 256;
 constexpr int turn_heads_of_group(int d) { return kTurnThreads / (d / 16); }
 
-template <int D, bool F16, TurnTarget TO>
-__global__ __launch_bounds__(kTurnThreads) void row_turns_kernel(TurnArgs args)
+// 1 / sqrt(x), off by a few steps of fp64: one step of third order on the instruction's 2^-25 or so.
+__device__ __forceinline__ double inverse_root(double x)
+{
+    const double r = __builtin_amdgcn_rsq(x), e = fma(-x * r, r, 1.0);
+    return x > 0.0 && x < __builtin_huge_val() ? fma(r * e, fma(e, 0.375, 0.5), r) : r;
+}
+
+template <int D, bool F16, TurnTarget TO, bool NEIGHBOURS>
+__global__ __launch_bounds__(kTurnThreads, 4) void row_turns_kernel(TurnArgs args)
 {
     const TurnArgs &a = args;
     constexpr int LANES = D / 16, ITEMS = kTurnThreads / LANES;
@@ -50,17 +63,21 @@ __global__ __launch_bounds__(kTurnThreads) void row_turns_kernel(TurnArgs args)
     if (!is_q) group -= a.q_groups;
     const bool is_k = !is_q && group < a.k_groups;
     if (!is_q && !is_k) group -= a.k_groups;
-    const int heads = is_q ? a.q_heads : a.kv_heads;
+    // heads step, 2 step, ... behind the first one
+    const int heads = is_q ? a.q_heads : a.kv_heads, step = is_q ? a.q_step : a.k_step;
     const unsigned item = (unsigned)group * ITEMS + threadIdx.x / LANES;
-    const int row = (int)(item / (unsigned)heads), head = (int)(item % (unsigned)heads);
-    const int n = a.count ? commit_positions(a.count[b], a.rows) : a.rows;
-    if (row >= n) return;
-    long long pos = (a.start ? a.start[b] : 0) + (long long)row;
-    if (TO == kTurnRows && a.tok) {
-        if (a.tok[(long long)b * a.rows + row] < 0) return;
+    const int row = (int)(item / (unsigned)step), first_head = (int)(item % (unsigned)step);
+    // (what a row is decided and placed by is asked for at once)
+    long long pos = a.start ? a.start[b] : 0;
+    if constexpr (TO == kTurnRows) {
+        const int u = row < a.rows ? row : 0, tok = a.tok[(long long)b * a.rows + u];
         int depth = -1;
-        for (int i = 0; i < a.anc_words; ++i) depth += __popcll(a.anc[row * a.anc_words + i]);
-        pos += depth - row;
+        for (int i = 0; i < a.anc_words; ++i) depth += __popcll(a.anc[u * a.anc_words + i]);
+        if (row >= a.rows || tok < 0) return;
+        pos += depth;
+    } else {
+        if (row >= (a.count ? commit_positions(a.count[b], a.rows) : a.rows)) return;
+        pos += row;
     }
     long long slot = -1;
     if (TO != kTurnRows && !is_q) {
@@ -69,32 +86,39 @@ __global__ __launch_bounds__(kTurnThreads) void row_turns_kernel(TurnArgs args)
         if (slot < 0 && (!is_k || !a.k_out)) return;
     }
     const long long page = slot >> a.to.page_shift, place = slot & ((1ll << a.to.page_shift) - 1);
-    const long long dst = (page * a.to.page + place * a.to.slot + head * a.to.head) * 16;
-    const long long sdst = page * a.to.scale_page + place * a.to.scale_slot + head * a.to.scale_head + t / 2;
+    const long long dst = (page * a.to.page + place * a.to.slot) * 16, dst_head = a.to.head * 16;
+    const long long sdst = page * a.to.scale_page + place * a.to.scale_slot + t / 2;
 
     float y[16];
     if (TO != kTurnRows && !is_q && !is_k) {         // values, as they are
-        const uint4 *from = (const uint4 *)(a.v + b * a.vs[0] + row * a.vs[1] + head * a.vs[2]) + 2 * t;
-        const uint4 v0 = from[0], v1 = from[1];
-        if constexpr (TO == kTurnCache16) {
-            ((uint4 *)(a.to.v + dst))[2 * t] = v0;
-            ((uint4 *)(a.to.v + dst))[2 * t + 1] = v1;
-        } else {
-            row_eight<F16>(v0, y);
-            row_eight<F16>(v1, y + 8);
-            uint32_t s;
-            ((uint2 *)(a.to.v + dst))[t] = mx4_half_block<F16>(y, s);
-            if (!(t & 1)) a.to.v_scale[sdst] = (uint8_t)s;
+        for (int head = first_head; head < heads; head += step) {
+            const uint4 *from = (const uint4 *)(a.v + b * a.vs[0] + row * a.vs[1] + head * a.vs[2]) + 2 * t;
+            const uint4 v0 = from[0], v1 = from[1];
+            char *to = a.to.v + dst + head * dst_head;
+            if constexpr (TO == kTurnCache16) {
+                ((uint4 *)to)[2 * t] = v0;
+                ((uint4 *)to)[2 * t + 1] = v1;
+            } else {
+                row_eight<F16>(v0, y);
+                row_eight<F16>(v1, y + 8);
+                uint32_t s;
+                ((uint2 *)to)[t] = mx4_half_block<F16>(y, s);
+                if (!(t & 1)) a.to.v_scale[sdst + head * a.to.scale_head] = (uint8_t)s;
+            }
         }
         return;
     }
     // this thread's two pieces of eight elements
     const int turned = a.half / 8;                   // threads whose pairs are rotated
-    const bool turns = t < turned, apart = turns && !a.neighbours;
+    const bool turns = t < turned, apart = turns && !NEIGHBOURS;
     const int first = apart ? t : 2 * t, second = apart ? t + turned : 2 * t + 1;
-    const uint16_t *x = is_q ? a.q + b * a.qs[0] + row * a.qs[1] + head * a.qs[2] : a.k + b * a.ks[0] + row * a.ks[1] + head * a.ks[2];
-    const uint4 x0 = ((const uint4 *)x)[first], x1 = ((const uint4 *)x)[second];
-    float cs[16];
+    const long long x_head = is_q ? a.qs[2] : a.ks[2];
+    const uint16_t *x = is_q ? a.q + b * a.qs[0] + row * a.qs[1] : a.k + b * a.ks[0] + row * a.ks[1];
+    uint16_t *out = is_q ? a.q_out + b * a.qos[0] + row * a.qos[1] : a.k_out ? a.k_out + b * a.kos[0] + row * a.kos[1] : nullptr;
+    const long long out_head = is_q ? a.qos[2] : a.kos[2];
+    uint4 x0 = ((const uint4 *)(x + first_head * x_head))[first], x1 = ((const uint4 *)(x + first_head * x_head))[second];
+    // cosines and sines of its pairs, weights of its elements: the same for all heads
+    double cs[16], weight[16];
     if (turns) {
         const bool there = pos >= 0 && pos < a.positions;
         const float4 *c = (const float4 *)(a.turns + (there ? pos : 0) * 2 * a.half + 8 * t), *s = c + a.half / 4;
@@ -103,64 +127,62 @@ __global__ __launch_bounds__(kTurnThreads) void row_turns_kernel(TurnArgs args)
 #pragma unroll
         for (int i = 0; i < 16; ++i) cs[i] = there ? v[i] : __builtin_nanf("");
     }
-    float f[16];
-    row_eight<F16>(x0, f);
-    row_eight<F16>(x1, f + 8);
-    double z[16];
-#pragma unroll
-    for (int i = 0; i < 16; ++i) z[i] = f[i];
     const uint16_t *norm = is_q ? a.q_norm : a.k_norm;
     if (norm) {
         float w[16];
         row_eight<F16>(((const uint4 *)norm)[first], w);
         row_eight<F16>(((const uint4 *)norm)[second], w + 8);
-        double sum = 0.0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) sum = fma(z[i], z[i], sum);
-#pragma unroll
-        for (int off = 1; off < LANES; off <<= 1) sum += __shfl_xor(sum, off);
-        const double r = 1.0 / sqrt(sum * (1.0 / D) + a.eps);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) z[i] *= r * (double)w[i];
+        for (int i = 0; i < 16; ++i) weight[i] = w[i];
     }
-    if (turns) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            // (pairs: element i of both pieces, or two neighbours)
-            const double p = a.neighbours ? z[2 * i] : z[i], q = a.neighbours ? z[2 * i + 1] : z[8 + i];
-            const double c = cs[i], s = cs[8 + i];
-            const double p1 = fma(p, c, -(q * s)), q1 = fma(p, s, q * c);
-            y[i] = (float)p1;
-            y[8 + i] = (float)q1;
+    for (int head = first_head; head < heads; head += step) {
+        float f[16];
+        row_eight<F16>(x0, f);
+        row_eight<F16>(x1, f + 8);
+        if (head + step < heads) {
+            x0 = ((const uint4 *)(x + (head + step) * x_head))[first];
+            x1 = ((const uint4 *)(x + (head + step) * x_head))[second];
         }
-        if (a.neighbours) {
-            float w[16];
+        double z[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) { w[2 * i] = y[i]; w[2 * i + 1] = y[8 + i]; }
+        for (int i = 0; i < 16; ++i) z[i] = f[i];
+        if (norm) {
+            double sum = 0.0;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) y[i] = w[i];
+            for (int i = 0; i < 16; ++i) sum = fma(z[i], z[i], sum);
+#pragma unroll
+            for (int off = 1; off < LANES; off <<= 1) sum += __shfl_xor(sum, off);
+            const double r = inverse_root(fma(sum, 1.0 / D, a.eps));
+#pragma unroll
+            for (int i = 0; i < 16; ++i) z[i] *= r * weight[i];
         }
-    } else {
+        if (turns) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) y[i] = (float)z[i];
-    }
-    const uint4 o0{row_two<F16>(y[0], y[1]), row_two<F16>(y[2], y[3]), row_two<F16>(y[4], y[5]), row_two<F16>(y[6], y[7])};
-    const uint4 o1{row_two<F16>(y[8], y[9]), row_two<F16>(y[10], y[11]), row_two<F16>(y[12], y[13]), row_two<F16>(y[14], y[15])};
-    uint16_t *out = is_q ? a.q_out + b * a.qos[0] + row * a.qos[1] + head * a.qos[2]
-                         : a.k_out ? a.k_out + b * a.kos[0] + row * a.kos[1] + head * a.kos[2] : nullptr;
-    if (out) {
-        ((uint4 *)out)[first] = o0;
-        ((uint4 *)out)[second] = o1;
-    }
-    if constexpr (TO == kTurnCache16) {
-        if (is_k && slot >= 0) {
-            ((uint4 *)(a.to.k + dst))[first] = o0;
-            ((uint4 *)(a.to.k + dst))[second] = o1;
+            for (int i = 0; i < 8; ++i) {
+                // (pairs: element i of both pieces, or two neighbours)
+                constexpr int FAR = NEIGHBOURS ? 1 : 8, BY = NEIGHBOURS ? 2 : 1;
+                const double p = z[BY * i], q = z[BY * i + FAR];
+                y[BY * i] = (float)fma(p, cs[i], -(q * cs[8 + i]));
+                y[BY * i + FAR] = (float)fma(p, cs[8 + i], q * cs[i]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) y[i] = (float)z[i];
         }
-    }
-    if constexpr (TO == kTurnCache4) {
-        __shared__ float4 lines[kTurnThreads * 4];
-        if (is_k && slot >= 0) {
+        const uint4 o0{row_two<F16>(y[0], y[1]), row_two<F16>(y[2], y[3]), row_two<F16>(y[4], y[5]), row_two<F16>(y[6], y[7])};
+        const uint4 o1{row_two<F16>(y[8], y[9]), row_two<F16>(y[10], y[11]), row_two<F16>(y[12], y[13]), row_two<F16>(y[14], y[15])};
+        if (out) {
+            ((uint4 *)(out + head * out_head))[first] = o0;
+            ((uint4 *)(out + head * out_head))[second] = o1;
+        }
+        if (TO == kTurnRows || !is_k || slot < 0) continue;
+        char *to = a.to.k + dst + head * dst_head;
+        if constexpr (TO == kTurnCache16) {
+            ((uint4 *)to)[first] = o0;
+            ((uint4 *)to)[second] = o1;
+        }
+        if constexpr (TO == kTurnCache4) {
+            __shared__ float4 lines[kTurnThreads * 4];
             float4 *line = lines + threadIdx.x / LANES * (D / 4);
             line[2 * first] = float4{y[0], y[1], y[2], y[3]};
             line[2 * first + 1] = float4{y[4], y[5], y[6], y[7]};
@@ -176,8 +198,8 @@ __global__ __launch_bounds__(kTurnThreads) void row_turns_kernel(TurnArgs args)
                 y[4 * i] = l.x; y[4 * i + 1] = l.y; y[4 * i + 2] = l.z; y[4 * i + 3] = l.w;
             }
             uint32_t s;
-            ((uint2 *)(a.to.k + dst))[t] = mx4_half_block<F16>(y, s);
-            if (!(t & 1)) a.to.k_scale[sdst] = (uint8_t)s;
+            ((uint2 *)to)[t] = mx4_half_block<F16>(y, s);
+            if (!(t & 1)) a.to.k_scale[sdst + head * a.to.scale_head] = (uint8_t)s;
         }
     }
 }

@@ -124,7 +124,7 @@ CachePlaces places_of(const stand_cache *c)
 }
 
 // The kernel's view of the rows of stand_tree_rotate and stand_cache_append; -> workgroups of a trajectory.
-unsigned turn_args(TurnArgs &a, const stand_rotation *rotation, const stand_turned_rows *rows, bool values)
+unsigned turn_args(TurnArgs &a, int64_t B, const stand_rotation *rotation, const stand_turned_rows *rows, bool values)
 {
     a.q = (const uint16_t *)rows->d_q; a.k = (const uint16_t *)rows->d_k; a.v = (const uint16_t *)rows->d_v;
     a.q_out = (uint16_t *)rows->d_q_out; a.k_out = (uint16_t *)rows->d_k_out;
@@ -132,31 +132,43 @@ unsigned turn_args(TurnArgs &a, const stand_rotation *rotation, const stand_turn
         a.qs[i] = rows->q_stride[i]; a.ks[i] = rows->k_stride[i]; a.vs[i] = rows->v_stride[i];
         a.qos[i] = rows->q_out_stride[i]; a.kos[i] = rows->k_out_stride[i];
     }
-    a.turns = nullptr; a.q_norm = a.k_norm = nullptr; a.eps = 0.0; a.positions = a.half = a.neighbours = 0;
+    a.turns = nullptr; a.q_norm = a.k_norm = nullptr; a.eps = 0.0; a.positions = a.half = 0;
     if (rotation) {
-        a.turns = rotation->d_turns; a.positions = rotation->positions; a.half = rotation->dims / 2; a.neighbours = rotation->neighbours != 0;
+        a.turns = rotation->d_turns; a.positions = rotation->positions; a.half = rotation->dims / 2;
         a.q_norm = (const uint16_t *)rotation->d_q_norm; a.k_norm = (const uint16_t *)rotation->d_k_norm; a.eps = rotation->eps;
     }
     a.rows = rows->rows; a.q_heads = rows->q_heads; a.kv_heads = rows->kv_heads;
-    a.q_groups = a.q ? (int)turn_groups(rows->rows, rows->q_heads, rows->head_dim) : 0;
-    a.k_groups = (int)turn_groups(rows->rows, rows->kv_heads, rows->head_dim);
+    // A thread has up to four heads of its row, whose cosines and weights it makes once (128 trees of 128, 16/8 heads of 128: 27 us, two heads 30,
+    // one 37; as many heads as leave a wave one row 35); where one head would not make 1024 workgroups, one.
+    const int many = B * turn_groups(rows->rows, rows->q_heads + 2ll * rows->kv_heads, rows->head_dim) >= 1024 ? 4 : 1;
+    a.q_step = (rows->q_heads + many - 1) / many;
+    a.k_step = (rows->kv_heads + many - 1) / many;
+    a.q_groups = a.q ? (int)turn_groups(rows->rows, a.q_step, rows->head_dim) : 0;
+    a.k_groups = (int)turn_groups(rows->rows, a.k_step, rows->head_dim);
     a.tok = nullptr; a.anc = nullptr; a.anc_words = 0; a.start = a.count = nullptr;
     a.slots = nullptr; a.width = 0; a.slot_count = 0;
     return (unsigned)(a.q_groups + (values ? 2 : 1) * a.k_groups);
 }
-template <TurnTarget TO>
-void turn_launch(const TurnArgs &a, const stand_turned_rows *rows, unsigned groups, int B, hipStream_t s)
+template <TurnTarget TO, bool NEIGHBOURS>
+void turn_launch(const TurnArgs &a, const stand_turned_rows *rows, dim3 grid, hipStream_t s)
 {
-    const dim3 grid(groups, (unsigned)B), threads(kTurnThreads);
+    const dim3 threads(kTurnThreads);
     const bool f16 = rows->dtype == STAND_F16;
     static_assert(turn_heads_of_group(64) == 64 && turn_heads_of_group(128) == 32, "turn_groups() counts with these");
     if (rows->head_dim == 64) {
-        if (f16) row_turns_kernel<64, true, TO><<<grid, threads, 0, s>>>(a);
-        else row_turns_kernel<64, false, TO><<<grid, threads, 0, s>>>(a);
+        if (f16) row_turns_kernel<64, true, TO, NEIGHBOURS><<<grid, threads, 0, s>>>(a);
+        else row_turns_kernel<64, false, TO, NEIGHBOURS><<<grid, threads, 0, s>>>(a);
     } else {
-        if (f16) row_turns_kernel<128, true, TO><<<grid, threads, 0, s>>>(a);
-        else row_turns_kernel<128, false, TO><<<grid, threads, 0, s>>>(a);
+        if (f16) row_turns_kernel<128, true, TO, NEIGHBOURS><<<grid, threads, 0, s>>>(a);
+        else row_turns_kernel<128, false, TO, NEIGHBOURS><<<grid, threads, 0, s>>>(a);
     }
+}
+template <TurnTarget TO>
+void turn_launch(const TurnArgs &a, const stand_rotation *rotation, const stand_turned_rows *rows, unsigned groups, int B, hipStream_t s)
+{
+    const dim3 grid(groups, (unsigned)B);
+    if (rotation && rotation->neighbours) turn_launch<TO, true>(a, rows, grid, s);
+    else turn_launch<TO, false>(a, rows, grid, s);
 }
 
 // Workgroups of a launch: as many as the device holds at once, a multiple of its eight XCDs; 0: the device refused.  (Above
@@ -266,9 +278,9 @@ extern "C" int stand_cache_commit(stand_handle *h, const stand_cache *cache, con
     if (refused) return refused;
     if (of_four(cache)) {
         CommitFourArgs a;
-        a.units = cache->head_dim / 16;
+        a.units = cache->head_dim / kFourUnit;
         a.heads = cache->kv_heads;
-        a.per_group = commit_per_group(a.heads * a.units);
+        a.per_group = four_per_group(a.heads * a.units);
         const int64_t groups = commit_groups(width, a.per_group);
         const DeviceScope scope(v.device);
         if (scope.e != hipSuccess) return bad_device(v, scope.e);
@@ -311,9 +323,9 @@ extern "C" int stand_cache_read(stand_handle *h, const stand_cache *cache, int32
     const int refused = check_cache_read(v.B, cache, first_layer, layers, d_table, table_width, rows);
     if (refused) return refused;
     ReadArgs a;
-    a.units = cache->head_dim / 16;
+    a.units = cache->head_dim / kReadUnit;
     a.heads = cache->kv_heads;
-    a.per_group = commit_per_group(a.heads * a.units);
+    a.per_group = four_per_group(a.heads * a.units);
     const int64_t groups = commit_groups(rows->rows, a.per_group);
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
@@ -337,12 +349,12 @@ extern "C" int stand_tree_rotate(stand_handle *h, const stand_rotation *rotation
     const int refused = check_tree_rotate(v.B, v.N, rotation, d_len, d_draft_tok, rows);
     if (refused) return refused;
     TurnArgs a;
-    const unsigned groups = turn_args(a, rotation, rows, false);
+    const unsigned groups = turn_args(a, v.B, rotation, rows, false);
     a.start = d_len; a.tok = d_draft_tok; a.anc = v.anc; a.anc_words = v.anc_words;
     a.to = CachePlaces{};
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
-    turn_launch<kTurnRows>(a, rows, groups, v.B, (hipStream_t)stream);
+    turn_launch<kTurnRows>(a, rotation, rows, groups, v.B, (hipStream_t)stream);
     return launched(v);
 }
 
@@ -355,7 +367,7 @@ extern "C" int stand_cache_append(stand_handle *h, const stand_cache *cache, int
     const int refused = check_cache_append(v.B, cache, layer, rotation, rows, d_slots, width);
     if (refused) return refused;
     TurnArgs a;
-    const unsigned groups = turn_args(a, rotation, rows, true);
+    const unsigned groups = turn_args(a, v.B, rotation, rows, true);
     a.start = d_start; a.count = d_count; a.slots = d_slots; a.width = width;
     a.to = places_of(cache);
     a.to.k += layer * a.to.layer * 16; a.to.v += layer * a.to.layer * 16;
@@ -363,8 +375,8 @@ extern "C" int stand_cache_append(stand_handle *h, const stand_cache *cache, int
     a.slot_count = (long long)cache->pages << a.to.page_shift;
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
-    if (of_four(cache)) turn_launch<kTurnCache4>(a, rows, groups, v.B, (hipStream_t)stream);
-    else turn_launch<kTurnCache16>(a, rows, groups, v.B, (hipStream_t)stream);
+    if (of_four(cache)) turn_launch<kTurnCache4>(a, rotation, rows, groups, v.B, (hipStream_t)stream);
+    else turn_launch<kTurnCache16>(a, rotation, rows, groups, v.B, (hipStream_t)stream);
     return launched(v);
 }
 
