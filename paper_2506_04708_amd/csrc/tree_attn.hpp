@@ -844,6 +844,8 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
     const JoinRecord r = a.join[w];
     const Exponent ex = exponent_of(a.scale);
     if (wr * 32 >= r.rows) return;
+    // (in tiles of one wave, which often have few rows, a lane without one reads what the last row's does: fewer lines)
+    const int from_lane = TM == 32 ? (lane & 32) | min(lane & 31, r.rows - 1) : lane;
     const int turn = w - r.first - 1;                  // 0: the item's second share
     const bool share = r.last - r.first + 1 > kJoinShared;
     if (turn >= (share ? 8 : 1)) return;
@@ -866,7 +868,7 @@ __global__ __launch_bounds__(256) void tree_attn_join_kernel(TreeAttnArgs a)
                 const float *slot = a.part + (2 * g + (g == r.first)) * kSlot;
                 m[k] = slot[at]; x[k] = slot[TM + at];
 #pragma unroll
-                for (int i = 0; i < COUNT; ++i) p[k][i] = ((const float4v *)(slot + 2 * TM))[(wr * GROUPS + group + i) * 64 + lane];
+                for (int i = 0; i < COUNT; ++i) p[k][i] = ((const float4v *)(slot + 2 * TM))[(wr * GROUPS + group + i) * 64 + from_lane];
             }
             float best = top;
 #pragma unroll

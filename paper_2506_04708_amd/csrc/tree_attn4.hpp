@@ -1,20 +1,31 @@
 // tree_attn4.hpp -- attention of the nodes of a drafted tree over a paged cache of 4 bits and over their own ancestors.
 //
 // The mathematics is tree_attn.hpp's: one pass over the keys with a running maximum, S^T = K Q^T and O^T = V^T P^T with 32x32x16
-// products, weights rounded to the rows' type.  What differs is where the time goes: a token's key and value are a quarter of the
-// bytes, so that reading them once for every 32 rows costs less than sharing them out, and making 16-bit numbers of them takes a
-// wave 64 conversions for 32 keys beside 16 matrix instructions.  So every wave works by itself: it has 32 rows of one
-// key/value head and a run of its keys, no barrier and no other wave's pace, and rows are cut into groups of 32 that leave few lanes empty.
+// products, weights rounded to the rows' type, sums in fp32.  A token's key and value are a quarter of the bytes; one instruction makes two numbers
+// of the rows' type of two elements and their block's scale, exactly (mx4.hpp), and a wave needs 64 of them for 32 keys beside its 16 matrix
+// instructions.  Two forms, by the rows that share a key/value head (serve_api.hip):
 //
-// Keys: a lane has half of a key, D / 64 blocks, straight from memory.  A block's four words, converted with its scale (one
-// instruction for two numbers, exact), are the left operand of four products; the queries' elements are held in the same
-// order.  Values: a lane has half of a token's too; converted they go through 32 rows of LDS of the wave's own, from which the
-// transposing reads take them as V^T.  Rows of LDS are swizzled by 16 bytes so that both touch every bank once.
+// Up to 64, every wave works by itself on 32 rows and a run of their keys: no barrier, no other wave's pace.  A lane has half of a key, D / 64
+// blocks, straight from memory: a block's words, converted, are the left operand of four products, and the queries' elements are held in the
+// same order.  Of a token's value a lane has half too; converted, it goes through 32 rows of LDS of the wave's own, from which the
+// transposing reads take V^T.
 //
-// The tree: the nodes that the wave's rows see, ancestors of a few nodes, are collected first, so that most trees take one step
-// of 32 keys.  Their rows have 16 bits and take the same way without the conversions.
+// Above, the four waves of a workgroup have 32 rows each and the same keys (a team; a head's groups of 32 rows are shared out evenly over its
+// teams).  Every thread converts one block of a unit into LDS for all, two units ahead of the products' reads of them in the third place of
+// memory, and a step makes the scores of 32 keys beside the weights of the 32 before.  Two workgroups share a compute unit and do not wait for
+// each other.  (Waves by themselves take 150 us instead of 122 for the trees below: the vector units are the ones that are short, and every wave
+// would convert everything; with all eight waves of a compute unit as one team, at one barrier, 133.)
 //
-// Work is cut as attn_plan.hpp says, a share for every wave that the chip holds; a unit is 32 keys, the whole tree is one.
+// The tree comes first: the nodes that a wave's rows see, ancestors of a few nodes, are collected, so that most trees take one step of 32
+// keys.  Their rows have 16 bits and take the first form's way without the conversions.
+//
+// Work is cut as attn_plan.hpp says, a share for every team that the chip holds; a unit is 32 keys (64 of heads of 64 in a team), the
+// whole tree is one.  Beginnings count as START units (64 single tokens 214 us, with 3 225, with 10 216; 32 trees 122, 128, 123).
+//
+// Bound: decoding by HBM (1.08 GB of cache in 214 us, 5.1 TB/s; a torch copy reaches 5.0 counting both ways).  Trees by what a wave issues between
+// its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128: 122 us for 70 GFLOP, 576 TFLOP/s on rows as
+// they are, where a large matrix product reaches 1253): a unit takes two workgroups about 1 us, of which the matrix units are busy for a
+// half.  Short calls by the chain lengths -> shares -> nodes -> ancestors, page numbers -> keys, each a trip to memory.
 #pragma once
 #include "mx4.hpp"
 #include "tree_attn.hpp"
@@ -39,8 +50,7 @@ struct Attn4Shape {
     static constexpr int AHEAD = ALONE ? 1 : 2;
     static constexpr int START = 6, HEAVY = 1, LIGHT = 1;
     static constexpr int ROW = 2 * D, CPR = D / 8;   // bytes and 16-byte chunks of a token's key or value
-    static constexpr int BLOCKS = D / kMx4Block, MINE = 2 * KT * BLOCKS / THREADS;   // blocks of a key, of a thread in a unit
-    static_assert(ALONE || MINE * THREADS == 2 * KT * BLOCKS, "a unit's blocks are shared out evenly");
+    static constexpr int BLOCKS = D / kMx4Block;     // of a key
     static constexpr int SUMS = (8 * (kAttnMaxBatch + 1) + 255) / 256 * 256;
     // LDS: 32 values of each wave, three units' keys and values in their place (unit sums before them) | drafted nodes of each team's
     // trajectory | nodes that a wave's rows see
@@ -302,7 +312,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
             }
         }
 
-        // ---- the cached keys of this share: blocks a unit ahead, page numbers two ----
+        // ---- the cached keys of this share ----
         const int first = max(u0 - 1, 0), n = u1 - 1 - first;   // (the item's first unit is the tree)
         if (S::ALONE && n > 0) {
             const int32_t *table = a.table + (long long)b * a.width;
@@ -374,7 +384,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
         }
         if constexpr (!S::ALONE)
             if (n > 0) {
-                // every thread has MINE blocks of a unit: loaded two units ahead of the products, converted into LDS one
+                // every thread has a block of a unit: loaded AHEAD units before it is converted into LDS, which is one before the products
                 const int32_t *table = a.table + (long long)b * a.width;
                 const int page_shift = a.page_shift, pages = a.pages;
                 const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
@@ -385,42 +395,31 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 const uint8_t *k_scale = a.k_scale + hk * a.scale_head, *v_scale = a.v_scale + hk * a.scale_head;
                 constexpr int HALF = S::KT * S::BLOCKS;          // the first half of a unit's blocks are keys
                 const int mine = (int)threadIdx.x % HALF, my_key = mine / S::BLOCKS, my_piece = mine % S::BLOCKS;
-                const bool mine_v = (int)threadIdx.x >= HALF;    // (MINE 1; with two, one of a key and one of a value)
-                static_assert(S::MINE == 1 ? 2 * HALF == S::THREADS : S::MINE == 2 && HALF == S::THREADS, "who has which block");
-                const uint4v *pool[S::MINE];
-                const uint8_t *scales[S::MINE];
-                uint32_t to[S::MINE][4];                         // where its four chunks go
+                const bool is_v = (int)threadIdx.x >= HALF;
+                static_assert(2 * HALF == S::THREADS, "who has which block");
+                const uint4v *const pool = (is_v ? v_pool : k_pool) + my_piece;
+                const uint8_t *const scales = (is_v ? v_scale : k_scale) + my_piece;
+                uint32_t to[4];                                  // where its four chunks go
 #pragma unroll
-                for (int r = 0; r < S::MINE; ++r) {
-                    const bool is_v = S::MINE == 1 ? mine_v : r == 1;
-                    pool[r] = (is_v ? v_pool : k_pool) + my_piece;
-                    scales[r] = (is_v ? v_scale : k_scale) + my_piece;
-#pragma unroll
-                    for (int x = 0; x < 4; ++x)
-                        to[r][x] = lds_begin + (is_v ? S::KEYS + my_key * S::ROW + (((4 * my_piece + x) ^ S::swizzle_v(my_key)) << 4)
-                                                     : my_key * S::KEY_ROW + 16 * (4 * my_piece + x));
-                }
+                for (int x = 0; x < 4; ++x)
+                    to[x] = lds_begin + (is_v ? S::KEYS + my_key * S::ROW + (((4 * my_piece + x) ^ S::swizzle_v(my_key)) << 4)
+                                              : my_key * S::KEY_ROW + 16 * (4 * my_piece + x));
                 constexpr int AHEAD = S::AHEAD;
-                uint4v block[AHEAD][S::MINE];
-                uint32_t scale[AHEAD][S::MINE];
+                uint4v block[AHEAD];
+                uint32_t scale[AHEAD];
                 auto key_of = [&](int i) { return min((first + i) * S::KT + my_key, len - 1); };   // behind the end: the last key again, weighted with zero
                 auto page_of = [&](int i) { return table[key_of(i) >> page_shift]; };
-                auto load = [&](int i, int page, uint4v *block, uint32_t *scale) {
+                auto load = [&](int i, int page, uint4v &block, uint32_t &scale) {
                     const int key = key_of(i);
                     const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
                     const unsigned long long from = at * pool_page + place * pool_slot;
                     unsigned long long sfrom = from;
                     if (!alike) sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * S::BLOCKS;
-#pragma unroll
-                    for (int r = 0; r < S::MINE; ++r) {
-                        block[r] = pool[r][from];
-                        scale[r] = scales[r][sfrom];
-                    }
+                    block = pool[from];
+                    scale = scales[sfrom];
                 };
-                auto store_word = [&](const uint4v *block, const uint32_t *scale, uint32_t stage, int x) {
-#pragma unroll
-                    for (int r = 0; r < S::MINE; ++r)
-                        *(lds_uint4v *)(uintptr_t)(to[r][x] + stage) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[r][x], mx4_factor(scale[r])));
+                auto store_word = [&](const uint4v &block, uint32_t scale, uint32_t stage, int x) {
+                    *(lds_uint4v *)(uintptr_t)(to[x] + stage) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[x], mx4_factor(scale)));
                 };
                 // (page numbers as far ahead of the blocks as those of the conversions: loads come back in order, and a wait for a
                 // page number is one for all blocks before it)
@@ -503,14 +502,14 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 using No = std::false_type;
                 auto no_fill = [](int) {};
                 float16v even = float16v{0}, odd = float16v{0};
-                #pragma unroll
+#pragma unroll
                 for (int x = 0; x < 4; ++x) store_word(block[0], scale[0], 0, x);
                 load(AHEAD, page[0], block[0], scale[0]);
                 __builtin_amdgcn_sched_barrier(0);
                 page[0] = page_of(2 * AHEAD);
                 __builtin_amdgcn_sched_barrier(0);
                 uint32_t before = 0, here = 0, next = S::STAGE;  // places of the units: the one before, this one, the next
-                auto unit_of_keys = [&](auto have_old, auto is_odd, int i, uint4v *block, uint32_t *scale, int &page) {   // block: of unit i + 1
+                auto unit_of_keys = [&](auto have_old, auto is_odd, int i, uint4v &block, uint32_t &scale, int &page) {   // block: of unit i + 1
                     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                     group_barrier();                             // the unit's keys and values are there, those of two units before done with
                     const int left = len - (first + i) * S::KT;
