@@ -466,7 +466,7 @@ typedef struct {
 int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots, int32_t width,
                        const int32_t *d_row, const int32_t *d_count, void *stream);
 
-/* Rows for the tokens of a cache, written: as stand_cache_rows. */
+/* Rows for the tokens of a cache, written: as stand_cache_rows, no stride 0 where it would be taken more than once. */
 typedef struct {
     void *d_k, *d_v;
     int32_t rows;
@@ -497,7 +497,8 @@ typedef struct {
 } stand_rotation;
 
 /* Queries, keys and (where a call takes them) values of `rows` rows of each trajectory, strides as in stand_tree_rows.  An output
- * may be its input with the same strides (in place); otherwise outputs overlap no input.  d_q NULL: no queries.  d_k_out NULL: the keys go
+ * may be its input with the same strides (in place); otherwise outputs overlap no input.  A stride of 0 of an output is refused where
+ * it would be taken more than once.  d_q NULL: no queries.  d_k_out NULL: the keys go
  * to the cache alone. */
 typedef struct {
     const void *d_q, *d_k, *d_v;

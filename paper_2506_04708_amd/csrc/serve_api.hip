@@ -137,12 +137,12 @@ unsigned turn_args(TurnArgs &a, int64_t B, const stand_rotation *rotation, const
         a.turns = rotation->d_turns; a.positions = rotation->positions; a.half = rotation->dims / 2;
         a.q_norm = (const uint16_t *)rotation->d_q_norm; a.k_norm = (const uint16_t *)rotation->d_k_norm; a.eps = rotation->eps;
     }
-    a.rows = rows->rows; a.q_heads = rows->q_heads; a.kv_heads = rows->kv_heads;
+    a.rows = rows->rows; a.q_heads = a.q ? rows->q_heads : 0; a.kv_heads = rows->kv_heads;
     // A thread has up to four heads of its row, whose cosines and weights it makes once (128 trees of 128, 16/8 heads of 128: 27 us, two heads 30,
     // one 37; as many heads as leave a wave one row 35); where one head would not make 1024 workgroups, one.
-    const int many = B * turn_groups(rows->rows, rows->q_heads + 2ll * rows->kv_heads, rows->head_dim) >= 1024 ? 4 : 1;
-    a.q_step = (rows->q_heads + many - 1) / many;
-    a.k_step = (rows->kv_heads + many - 1) / many;
+    const int many = B * turn_groups(rows->rows, a.q_heads + 2ll * a.kv_heads, rows->head_dim) >= 1024 ? 4 : 1;
+    a.q_step = (a.q_heads + many - 1) / many;
+    a.k_step = (a.kv_heads + many - 1) / many;
     a.q_groups = a.q ? (int)turn_groups(rows->rows, a.q_step, rows->head_dim) : 0;
     a.k_groups = (int)turn_groups(rows->rows, a.k_step, rows->head_dim);
     a.tok = nullptr; a.anc = nullptr; a.anc_words = 0; a.start = a.count = nullptr;

@@ -92,7 +92,9 @@ inline int check_cache_commit(int64_t B, const stand_cache *cache, const stand_c
     return B > kServeMaxBatch || cache->layers > 65535 ? STAND_ELIMIT : STAND_OK;
 }
 
-// Rows that a layer's or a trajectory's lie side by side in: one element of the next row behind a head's would be another's.
+// Places that are written differ from each other (a view that repeats one, as torch's expand makes them, would be written by many).
+inline bool apart(int64_t stride, int64_t count) { return stride != 0 || count == 1; }
+
 inline int check_cache_read(int64_t B, const stand_cache *cache, int32_t first_layer, int32_t layers, const int32_t *d_table, int32_t table_width,
                             const stand_cache_rows_out *rows)
 {
@@ -101,6 +103,9 @@ inline int check_cache_read(int64_t B, const stand_cache *cache, int32_t first_l
     if (rows->rows < 1 || rows->rows > kServeMaxWidth || (int64_t)table_width * cache->page_size > STAND_MAX_CACHED) return STAND_EINVAL;
     if (!aligned16(rows->d_k) || !aligned16(rows->d_v)) return STAND_EINVAL;
     if (!stride_ok(rows->layer_stride) || !stride_ok(rows->batch_stride) || !stride_ok(rows->row_stride) || !stride_ok(rows->head_stride))
+        return STAND_EINVAL;
+    if (!apart(rows->layer_stride, layers) || !apart(rows->batch_stride, B) || !apart(rows->row_stride, rows->rows) ||
+        !apart(rows->head_stride, cache->kv_heads))
         return STAND_EINVAL;
     return B > kServeMaxBatch || layers > 65535 ? STAND_ELIMIT : STAND_OK;
 }
@@ -112,10 +117,11 @@ inline bool rotation_ok(const stand_rotation *r, int32_t head_dim)
     return !(r->d_q_norm || r->d_k_norm) || (r->eps >= 0.0f && r->eps <= 3.402823466e+38f);
 }
 
-// An output is its input in the same places, or somewhere else.
-inline bool output_ok(const void *out, const int64_t *out_stride, const void *in, const int64_t *in_stride)
+// An output [B][rows][heads] is its input in the same places, or somewhere else.
+inline bool output_ok(const void *out, const int64_t *out_stride, const void *in, const int64_t *in_stride, int64_t B, int64_t rows, int64_t heads)
 {
-    return out && aligned16(out) && strides_ok(out_stride) && (out != in || !memcmp(out_stride, in_stride, 3 * sizeof(int64_t)));
+    return out && aligned16(out) && strides_ok(out_stride) && apart(out_stride[0], B) && apart(out_stride[1], rows) && apart(out_stride[2], heads) &&
+           (out != in || !memcmp(out_stride, in_stride, 3 * sizeof(int64_t)));
 }
 
 constexpr int64_t kTurnMaxGroups = (1 << 24) - 1;      // workgroups of a trajectory: a launch's dimension has threads for so many
@@ -130,9 +136,9 @@ inline int check_turned_rows(int64_t B, const stand_turned_rows *r, bool values,
     if (!r || !r->d_k || !aligned16(r->d_k) || !strides_ok(r->k_stride)) return STAND_EINVAL;
     if ((r->dtype != STAND_BF16 && r->dtype != STAND_F16) || (r->head_dim != 64 && r->head_dim != 128)) return STAND_EINVAL;
     if (r->rows < 1 || r->rows > kServeMaxWidth || r->kv_heads < 1 || r->kv_heads > 4096) return STAND_EINVAL;
-    if (r->d_q && (r->q_heads < 1 || !aligned16(r->d_q) || !strides_ok(r->q_stride) || !output_ok(r->d_q_out, r->q_out_stride, r->d_q, r->q_stride)))
+    if (r->d_q && (r->q_heads < 1 || !aligned16(r->d_q) || !strides_ok(r->q_stride) || !output_ok(r->d_q_out, r->q_out_stride, r->d_q, r->q_stride, B, r->rows, r->q_heads)))
         return STAND_EINVAL;
-    if ((k_out || r->d_k_out) && !output_ok(r->d_k_out, r->k_out_stride, r->d_k, r->k_stride)) return STAND_EINVAL;
+    if ((k_out || r->d_k_out) && !output_ok(r->d_k_out, r->k_out_stride, r->d_k, r->k_stride, B, r->rows, r->kv_heads)) return STAND_EINVAL;
     if (values && (!r->d_v || !aligned16(r->d_v) || !strides_ok(r->v_stride))) return STAND_EINVAL;
     if (B > kServeMaxBatch || (r->d_q && r->q_heads > 65535)) return STAND_ELIMIT;
     const int64_t q = r->d_q ? turn_groups(r->rows, r->q_heads, r->head_dim) : 0, k = turn_groups(r->rows, r->kv_heads, r->head_dim);

@@ -514,6 +514,26 @@ def test_attention_of_large_trees(binding, N, H, G, d, dtype, share):
     Attn4(binding, 260 + N + H, [170, 0], N, H, G, d, 16, dtype, share).check()
 
 
+@pytest.mark.parametrize("d,dtype,N", [(64, BF, 9), (128, HF, 9), (64, HF, 64), (128, BF, 64)])
+def test_scales_in_another_order_than_their_blocks(binding, d, dtype, N):
+    """Blocks as [page, place, head], scales as [page, head, place] with room between pages: one's place is not the other's."""
+    t = Attn4(binding, 280 + N + d, [300, 0, 77], N, 4, 2, d, 16, dtype, 0.8)
+    a = t.on_gpu()
+    c = a["cache"]
+
+    def moved(s):
+        layers, pages, page, G, n = s.shape
+        room = torch.full((layers, pages + 1, G + 1, page, n), 255, dtype=torch.uint8, device="cuda")
+        room[:, :pages, :G] = s.transpose(2, 3)
+        return room[:, :pages, :G].transpose(2, 3)
+
+    other = binding.PagedCache(c.k, c.v, moved(c.k_scale), moved(c.v_scale), dtype)
+    out = t.h.tree_attention(**dict(a, cache=other))
+    t.check(out)
+    drafted = torch.from_numpy(t.tok).cuda() >= 0
+    assert torch.equal(out[drafted], t.h.tree_attention(**a)[drafted])
+
+
 @pytest.mark.parametrize("d,dtype,N", [(64, BF, 1), (128, HF, 16), (128, BF, 64)])
 def test_places_far_into_a_cache(binding, d, dtype, N):
     """Pages 9 GiB apart, their scales nearly 2: places past 2^32 bytes and 2^31 heads' scales, for rows that come and rows that are read."""
@@ -581,6 +601,9 @@ def test_refusals(binding):
     rotate(q=a["q"][:, :, :, :32])
     rotate(q_out=torch.empty((2, 9, 5, 64), dtype=BF, device="cuda"))
     rotate(q_out=torch.empty((2, 9, 4, 64), dtype=HF, device="cuda"))
+    rotate(k=a["k"][:, :, :1].expand(2, 9, 2, 64))           # in place, but one head for both
+    rotate(q_out=torch.empty((2, 1, 4, 64), dtype=BF, device="cuda").expand(2, 9, 4, 64))
+    append(k_out=torch.empty((1, 9, 2, 64), dtype=BF, device="cuda").expand(2, 9, 2, 64))
     append(layer=2)
     append(layer=-1)
     append(k=a["k"].half())

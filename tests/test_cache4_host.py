@@ -162,6 +162,13 @@ def test_refusals_of_the_rotation(lib):
         assert call(r=rotation(**r)) == 0, r
     for r in BAD_ROTATION:
         assert call(r=rotation(**r)) == EINVAL, r
+    # outputs that repeat a place
+    for out in ("q_out_stride", "k_out_stride"):
+        for i in range(3):
+            zero = [0 if i == j else s for j, s in enumerate((4096, 256, 64))]
+            assert call(**{out: zero}) == EINVAL and call(d_q_out=4096, d_k_out=8192, **{out: zero, out.replace("_out", ""): zero}) == EINVAL
+            assert call(**{out.replace("_out", ""): zero}) == 0
+    assert call(B=1, q_out_stride=[0, 256, 64]) == 0 and call(N=1, rows=1, k_out_stride=[4096, 0, 64]) == 0 and call(kv_heads=1, k_out_stride=[4096, 256, 0]) == 0
     for kw in BAD_ROWS + [dict(d_k_out=0), dict(length=0), dict(tok=0), dict(N=8), dict(no_rows=True), dict(no_rotation=True)]:
         assert call(**kw) == EINVAL, kw
     assert call(B=65536) == ELIMIT and call(q_heads=65536) == ELIMIT
@@ -199,6 +206,7 @@ def test_refusals_of_the_read(lib):
         assert call(c=cache(**kw)) == EINVAL, kw
     for kw in (dict(first=-1), dict(first=1), dict(first=2, layers=1), dict(layers=0), dict(layers=3), dict(layers=2 ** 31 - 1, first=1), dict(table=0), dict(width=0), dict(width=(1 << 26) + 1),
                dict(no_rows=True), dict(d_k=0), dict(d_v=0), dict(d_k=8), dict(d_v=8), dict(rows=0), dict(rows=(1 << 30) + 1), dict(layer_stride=4), dict(batch_stride=-8),
-               dict(row_stride=1 << 48), dict(head_stride=12)):
+               dict(row_stride=1 << 48), dict(head_stride=12),
+               dict(layer_stride=0), dict(batch_stride=0), dict(row_stride=0), dict(head_stride=0)):
         assert call(**kw) == EINVAL, kw
     assert call(B=65536) == ELIMIT and call(c=cache(layers=65536), layers=65536) == ELIMIT
