@@ -23,7 +23,7 @@ STAND_BOTH int four_per_group(int row_units) { return (kCommitThreads + row_unit
 // ---- rows into 4 bits ---------------------------------------------------------------------------------------------------
 // As cache_commit_kernel (cache_ops.hpp): row row[b][j] of trajectory b to slot slots[b][j], all layers.  A thread has 8 elements
 // of a key and of a value: 16 bytes in, 4 out, and a block's four threads share its scale.  Bound by HBM with prompts (475 MB, 16 layers x
-// 4 x up to 2100 rows of 8 heads of 128: 114 us, 4.2 TB/s), after a step by its trips to memory: count, slot and row, key and value
+// 4 x up to 2100 rows of 8 heads of 128: 115 us, 4.1 TB/s), after a step by its trips to memory: count, slot and row, key and value
 // (28 layers of 32 short paths: 6 us).
 struct CommitFourArgs {
     const uint4 *k_rows, *v_rows;
@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kCommitThreads) void cache_commit4_kernel(CommitFou
 // ---- tokens out of a cache -----------------------------------------------------------------------------------------------
 // Token start[b] + j of trajectory b, j < count[b], to row j; tokens that no page in the cache has become zeros.  A thread writes 16
 // elements of a key and of a value: of 16 bits it copies them, of 4 it makes them from 8 bytes and a scale.  (8 elements, a word of 4 bytes and
-// a scale each: twice the time.)  Bound by HBM (the prompts above, 475 MB: 84 us, 5.7 TB/s).
+// a scale each: twice the time.)  Bound by HBM (the prompts above, 475 MB: 87 us, 5.5 TB/s).
 struct ReadArgs {
     uint4 *k_rows, *v_rows;
     CachePlaces from;

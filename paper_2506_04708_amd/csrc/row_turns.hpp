@@ -12,7 +12,7 @@
 // that pairs need no exchange; D / 16 lanes have a head and add up their squares.  Workgroups have queries, keys or values, not a
 // mixture.  For 4 bits a key's elements change lanes through LDS, so that blocks are of neighbours.
 //
-// Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 24 us, 5.8 TB/s).  Trees
+// Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 25 us, 5.8 TB/s).  Trees
 // are bound by how little is on its way at a time: a wave asks for what its row is decided by, then for rows and cosines, and has
 // some 600 instructions for each head of its lanes between them and its stores (128 trees of 128 nodes, 16/8 heads of 128, 85 MB: 28 us; with 132
 // instead of 128 registers, three waves of a SIMD instead of four, 31; one head for a thread, its conversions for each, 34).

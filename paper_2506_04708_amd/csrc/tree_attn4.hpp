@@ -22,7 +22,7 @@
 // Work is cut as attn_plan.hpp says, a share for every team that the chip holds; a unit is 32 keys (64 of heads of 64 in a team), the
 // whole tree is one.  Beginnings count as START units (64 single tokens 214 us, with 3 225, with 10 216; 32 trees 122, 128, 123).
 //
-// Bound: decoding by HBM (1.08 GB of cache in 214 us, 5.1 TB/s; a torch copy reaches 5.0 counting both ways).  Trees by what a wave issues between
+// Bound: decoding by HBM (1.08 GB of cache in 213 us, 5.1 TB/s; a torch copy reaches 5.0 counting both ways).  Trees by what a wave issues between
 // its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128: 122 us for 70 GFLOP, 576 TFLOP/s on rows as
 // they are, where a large matrix product reaches 1253): a unit takes two workgroups about 1 us, of which the matrix units are busy for a
 // half.  Short calls by the chain lengths -> shares -> nodes -> ancestors, page numbers -> keys, each a trip to memory.
