@@ -519,32 +519,49 @@ class Stand:
         _check(self._lib.stand_cache_commit(self.h, cache.ref, desc, self._arg(slots, torch.int64), slots.shape[1],
                                             self._arg(row, torch.int32), self._arg(count, torch.int32), self._stream()), self.h)
 
-    def _turned(self, dtype, q, k, v, q_out, k_out):
-        """stand_turned_rows of k [B, rows, kv heads, d] and what goes with it."""
-        B, rows, heads, d = k.shape
-        assert dtype in _HALF and B == self.B and k.get_device() == self._index
-        assert k.dtype is dtype and (v is None or v.shape == k.shape)
-        assert (q is None) == (q_out is None) and (q is None or (q.shape == q_out.shape and q.shape[:2] == (B, rows) and q.shape[3] == d))
-        assert k_out is None or k_out.shape == k.shape
-        ptr, strides = [], []
-        for t in (q, k, v, q_out, k_out):
-            if t is None:
-                ptr.append(0)
-                strides += (0, 0, 0)
-                continue
-            s0, s1, s2, s3 = t.stride()
-            assert s3 == 1 and t.dtype is dtype and t.get_device() == self._index
-            ptr.append(t.data_ptr())
-            strides += (s0, s1, s2)
-        return _TURNED_ROWS.pack(*ptr, _HALF[dtype], rows, 0 if q is None else q.shape[2], heads, d, *strides)
+    def _turned(self, dtype, shape, q, k, v, q_out, k_out):
+        """stand_turned_rows of k, whose shape is [B, rows, kv heads, d], and what goes with it."""
+        B, rows, heads, d = shape
+        index, of_q, zero = self._index, 0, (0, 0, 0)
+        k0, k1, k2, k3 = k.stride()
+        assert dtype in _HALF and B == self.B and k.get_device() == index and k.dtype is dtype and k3 == 1
+        qs = vs = qos = kos = zero
+        pq = pv = pqo = pko = 0
+        if q is None:
+            assert q_out is None
+        else:
+            q_shape = q.shape
+            q_batch, q_rows, of_q, q_dim = q_shape
+            *qs, q3 = q.stride()
+            pq = q.data_ptr()
+            assert q_batch == B and q_rows == rows and q_dim == d and q3 == 1 and q.dtype is dtype and q.get_device() == index
+            if q_out is q:
+                qos, pqo = qs, pq
+            else:
+                *qos, q3 = q_out.stride()
+                pqo = q_out.data_ptr()
+                assert q_out.shape == q_shape and q3 == 1 and q_out.dtype is dtype and q_out.get_device() == index
+        if v is not None:
+            *vs, v3 = v.stride()
+            pv = v.data_ptr()
+            assert v.shape == shape and v3 == 1 and v.dtype is dtype and v.get_device() == index
+        pk = k.data_ptr()
+        if k_out is k:
+            kos, pko = (k0, k1, k2), pk
+        elif k_out is not None:
+            *kos, k3 = k_out.stride()
+            pko = k_out.data_ptr()
+            assert k_out.shape == shape and k3 == 1 and k_out.dtype is dtype and k_out.get_device() == index
+        return _TURNED_ROWS.pack(pq, pk, pv, pqo, pko, _HALF[dtype], rows, of_q, heads, d, *qs, k0, k1, k2, *vs, *qos, *kos)
 
     def tree_rotate(self, rotation, length, draft_tok, q, k, q_out=None, k_out=None):
         """Queries q [B, N, heads, d] and keys k [B, N, kv heads, d] of the drafted nodes normed and rotated by their positions; an
         output that is None is the input."""
+        B, N, _, d = shape = k.shape
+        dtype = k.dtype
+        assert N == self.N and length.shape == (B,) and draft_tok.shape == (B, N) and rotation.fits(dtype, d, self._index)
         q_out, k_out = q if q_out is None else q_out, k if k_out is None else k_out
-        assert k.shape[1] == self.N and length.shape == (self.B,) and draft_tok.shape == (self.B, self.N)
-        assert rotation.fits(k.dtype, k.shape[3], self._index)
-        desc = self._turned(k.dtype, q, k, None, q_out, k_out)
+        desc = self._turned(dtype, shape, q, k, None, q_out, k_out)
         _check(self._lib.stand_tree_rotate(self.h, rotation.ref, self._arg(length, torch.int32), self._arg(draft_tok, torch.int32), desc,
                                            self._stream()), self.h)
         return q_out, k_out
@@ -552,13 +569,16 @@ class Stand:
     def cache_append(self, cache, layer, k, v, slots, start=None, count=None, rotation=None, q=None, q_out=None, k_out=None):
         """Rows k, v [B, rows, kv heads, d] into one layer of the cache: row j < count[b] (None: all) at position start[b] + j, to slot
         slots[b][j], its key normed and rotated; queries q [B, rows, heads, d] along with them into q_out (None: in place)."""
+        B, rows, heads, d = shape = k.shape
+        assert slots.dim() == 2
+        of_slots, width = slots.shape
+        assert of_slots == B and width >= rows and heads == cache.heads and d == cache.dim and self._index == cache.index
+        assert (start is None or start.shape == (B,)) and (count is None or count.shape == (B,))
+        assert rotation is None or rotation.fits(cache.dtype, d, self._index)
         q_out = q if q_out is None else q_out
-        assert slots.dim() == 2 and slots.shape[0] == self.B and slots.shape[1] >= k.shape[1] and k.shape[2] == cache.heads and k.shape[3] == cache.dim
-        assert (start is None or start.shape == (self.B,)) and (count is None or count.shape == (self.B,)) and self._index == cache.index
-        assert rotation is None or rotation.fits(k.dtype, k.shape[3], self._index)
-        desc = self._turned(cache.dtype, q, k, v, q_out, k_out)
+        desc = self._turned(cache.dtype, shape, q, k, v, q_out, k_out)
         _check(self._lib.stand_cache_append(self.h, cache.ref, layer, None if rotation is None else rotation.ref, desc, self._arg(start, torch.int32),
-                                            self._arg(slots, torch.int64), slots.shape[1], self._arg(count, torch.int32), self._stream()), self.h)
+                                            self._arg(slots, torch.int64), width, self._arg(count, torch.int32), self._stream()), self.h)
         return q_out
 
     def cache_read(self, cache, table, k, v, count=None, start=None, layer=0):
