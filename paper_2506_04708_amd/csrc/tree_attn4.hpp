@@ -13,7 +13,7 @@
 // Above, the four waves of a workgroup have 32 rows each and the same keys (a team; a head's groups of 32 rows are shared out evenly over its
 // teams).  Every thread converts one block of a unit into LDS for all, two units ahead of the products' reads of them in the third place of
 // memory, and a step makes the scores of 32 keys beside the weights of the 32 before.  Two workgroups share a compute unit and do not wait for
-// each other.  (Waves by themselves take 150 us instead of 122 for the trees below: the vector units are the ones that are short, and every wave
+// each other.  (Waves by themselves take 150 us instead of 121 for the trees below: the vector units are the ones that are short, and every wave
 // would convert everything; with all eight waves of a compute unit as one team, at one barrier, 133.)
 //
 // The tree comes first: the nodes that a wave's rows see, ancestors of a few nodes, are collected, so that most trees take one step of 32
@@ -23,7 +23,7 @@
 // whole tree is one.  Beginnings count as START units (64 single tokens 214 us, with 3 225, with 10 216; 32 trees 122, 128, 123).
 //
 // Bound: decoding by HBM (1.08 GB of cache in 213 us, 5.1 TB/s; a torch copy reaches 5.0 counting both ways).  Trees by what a wave issues between
-// its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128: 122 us for 70 GFLOP, 576 TFLOP/s on rows as
+// its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128: 121 us for 70 GFLOP, 580 TFLOP/s on rows as
 // they are, where a large matrix product reaches 1253): a unit takes two workgroups about 1 us, of which the matrix units are busy for a
 // half.  Short calls by the chain lengths -> shares -> nodes -> ancestors, page numbers -> keys, each a trip to memory.
 #pragma once
@@ -230,7 +230,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
         };
 
         // ---- the tree: the nodes that these rows see ----
-        if (busy && u0 == 0) {
+        auto tree = [&]() {
+            if (!busy || u0 != 0) return;
             const TreeAttn4Args &a = fresh_args<TreeAttn4Args>();
             const uint32_t *anc = a.anc + (long long)node * a.anc_words;
             int count = 0;
@@ -310,10 +311,11 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                         }
                 }
             }
-        }
+        };
 
         // ---- the cached keys of this share ----
         const int first = max(u0 - 1, 0), n = u1 - 1 - first;   // (the item's first unit is the tree)
+        if constexpr (S::ALONE) tree();
         if (S::ALONE && n > 0) {
             const int32_t *table = a.table + (long long)b * a.width;
             const int page_shift = a.page_shift, pages = a.pages;
@@ -382,56 +384,60 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                 if (done) break;
             }
         }
-        if constexpr (!S::ALONE)
+        if constexpr (!S::ALONE) {
+            // every thread has a block of a unit: loaded AHEAD units before it is converted into LDS, which is one before the products
+            const int32_t *table = a.table + (long long)b * a.width;
+            const int page_shift = a.page_shift, pages = a.pages;
+            const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
+            const uint32_t scale_page = (uint32_t)(a.scale_page / S::BLOCKS), scale_slot = (uint32_t)(a.scale_slot / S::BLOCKS);
+            // scales in the order of their blocks: a block's number is its scale's
+            const bool alike = pool_page == a.scale_page && pool_slot == a.scale_slot;
+            const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4), *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4);
+            const uint8_t *k_scale = a.k_scale + hk * a.scale_head, *v_scale = a.v_scale + hk * a.scale_head;
+            constexpr int HALF = S::KT * S::BLOCKS;          // the first half of a unit's blocks are keys
+            const int mine = (int)threadIdx.x % HALF, my_key = mine / S::BLOCKS, my_piece = mine % S::BLOCKS;
+            const bool is_v = (int)threadIdx.x >= HALF;
+            static_assert(2 * HALF == S::THREADS, "who has which block");
+            const uint4v *const pool = (is_v ? v_pool : k_pool) + my_piece;
+            const uint8_t *const scales = (is_v ? v_scale : k_scale) + my_piece;
+            uint32_t to[4];                                  // where its four chunks go
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+                to[x] = lds_begin + (is_v ? S::KEYS + my_key * S::ROW + (((4 * my_piece + x) ^ S::swizzle_v(my_key)) << 4)
+                                          : my_key * S::KEY_ROW + 16 * (4 * my_piece + x));
+            constexpr int AHEAD = S::AHEAD;
+            uint4v block[AHEAD];
+            uint32_t scale[AHEAD];
+            // the first ones are asked for before the tree, whose trips to memory then are theirs too (128 trees of 128 nodes: 142 us
+            // instead of 144; the other form has no registers for that)
+            const int last = max(len - 1, 0);                // (with no key to come: any place of the cache)
+            auto key_of = [&](int i) { return min((first + i) * S::KT + my_key, last); };   // behind the end: the last key again, weighted with zero
+            auto page_of = [&](int i) { return table[key_of(i) >> page_shift]; };
+            auto load = [&](int i, int page, uint4v &block, uint32_t &scale) {
+                const int key = key_of(i);
+                const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
+                const unsigned long long from = at * pool_page + place * pool_slot;
+                unsigned long long sfrom = from;
+                if (!alike) sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * S::BLOCKS;
+                block = pool[from];
+                scale = scales[sfrom];
+            };
+            auto store_word = [&](const uint4v &block, uint32_t scale, uint32_t stage, int x) {
+                *(lds_uint4v *)(uintptr_t)(to[x] + stage) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[x], mx4_factor(scale)));
+            };
+            // (page numbers as far ahead of the blocks as those of the conversions: loads come back in order, and a wait for a
+            // page number is one for all blocks before it)
+            int page[AHEAD];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) page[u] = page_of(u);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) load(u, page[u], block[u], scale[u]);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) page[u] = page_of(AHEAD + u);
+            __builtin_amdgcn_sched_barrier(0);
+            tree();
             if (n > 0) {
-                // every thread has a block of a unit: loaded AHEAD units before it is converted into LDS, which is one before the products
-                const int32_t *table = a.table + (long long)b * a.width;
-                const int page_shift = a.page_shift, pages = a.pages;
-                const uint32_t pool_page = (uint32_t)(a.pool_page / kMx4Block), pool_slot = (uint32_t)(a.pool_slot / kMx4Block);
-                const uint32_t scale_page = (uint32_t)(a.scale_page / S::BLOCKS), scale_slot = (uint32_t)(a.scale_slot / S::BLOCKS);
-                // scales in the order of their blocks: a block's number is its scale's
-                const bool alike = pool_page == a.scale_page && pool_slot == a.scale_slot;
-                const uint4v *k_pool = (const uint4v *)(a.k_pool + hk * a.pool_head / 4), *v_pool = (const uint4v *)(a.v_pool + hk * a.pool_head / 4);
-                const uint8_t *k_scale = a.k_scale + hk * a.scale_head, *v_scale = a.v_scale + hk * a.scale_head;
-                constexpr int HALF = S::KT * S::BLOCKS;          // the first half of a unit's blocks are keys
-                const int mine = (int)threadIdx.x % HALF, my_key = mine / S::BLOCKS, my_piece = mine % S::BLOCKS;
-                const bool is_v = (int)threadIdx.x >= HALF;
-                static_assert(2 * HALF == S::THREADS, "who has which block");
-                const uint4v *const pool = (is_v ? v_pool : k_pool) + my_piece;
-                const uint8_t *const scales = (is_v ? v_scale : k_scale) + my_piece;
-                uint32_t to[4];                                  // where its four chunks go
-#pragma unroll
-                for (int x = 0; x < 4; ++x)
-                    to[x] = lds_begin + (is_v ? S::KEYS + my_key * S::ROW + (((4 * my_piece + x) ^ S::swizzle_v(my_key)) << 4)
-                                              : my_key * S::KEY_ROW + 16 * (4 * my_piece + x));
-                constexpr int AHEAD = S::AHEAD;
-                uint4v block[AHEAD];
-                uint32_t scale[AHEAD];
-                auto key_of = [&](int i) { return min((first + i) * S::KT + my_key, len - 1); };   // behind the end: the last key again, weighted with zero
-                auto page_of = [&](int i) { return table[key_of(i) >> page_shift]; };
-                auto load = [&](int i, int page, uint4v &block, uint32_t &scale) {
-                    const int key = key_of(i);
-                    const uint32_t at = (uint32_t)clamp_page(page, pages), place = (uint32_t)(key & ((1 << page_shift) - 1));
-                    const unsigned long long from = at * pool_page + place * pool_slot;
-                    unsigned long long sfrom = from;
-                    if (!alike) sfrom = (unsigned long long)(at * scale_page + place * scale_slot) * S::BLOCKS;
-                    block = pool[from];
-                    scale = scales[sfrom];
-                };
-                auto store_word = [&](const uint4v &block, uint32_t scale, uint32_t stage, int x) {
-                    *(lds_uint4v *)(uintptr_t)(to[x] + stage) = __builtin_bit_cast(uint4v, mx4_eight<F16>(block[x], mx4_factor(scale)));
-                };
-                // (page numbers as far ahead of the blocks as those of the conversions: loads come back in order, and a wait for a
-                // page number is one for all blocks before it)
-                int page[AHEAD];
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) page[u] = page_of(u);
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) load(u, page[u], block[u], scale[u]);
-                __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-                for (int u = 0; u < AHEAD; ++u) page[u] = page_of(AHEAD + u);
-                __builtin_amdgcn_sched_barrier(0);
                 asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
                 group_barrier();                                 // (everyone is done with the tree)
                 const uint32_t k_at = lds_begin + col * S::KEY_ROW + 16 * half, v_at = get - lds0 + lds_begin + S::KEYS;
@@ -552,6 +558,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
                     step(Yes{}, No{}, odd, even, 0, before + (S::SUB - 1) * 32 * S::ROW, 0, no_fill);
                 }
             }
+        }
 
         // ---- the rows' outputs, or this wave's part of them ----
         l = other_half_sum(l);
