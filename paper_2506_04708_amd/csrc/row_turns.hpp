@@ -12,10 +12,11 @@
 // that pairs need no exchange; D / 16 lanes have a head and add up their squares.  Workgroups have queries, keys or values, not a
 // mixture.  For 4 bits a key's elements change lanes through LDS, so that blocks are of neighbours.
 //
-// Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 25 us, 5.8 TB/s).  Trees
+// Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 26 us, 5.5 TB/s).  Trees
 // are bound by how little is on its way at a time: a wave asks for what its row is decided by, then for rows and cosines, and has
-// some 600 instructions for each head of its lanes between them and its stores (128 trees of 128 nodes, 16/8 heads of 128, 85 MB: 28 us; with 132
-// instead of 128 registers, three waves of a SIMD instead of four, 31; one head for a thread, its conversions for each, 34).
+// some 600 instructions for each head of its lanes between them and its stores (128 trees of 128 nodes, 16/8 heads of 128, 85 MB: 26 us; with its stores in the L2 and 132
+// instead of 128 registers, three waves of a SIMD instead of four, 31; one head for a thread, its conversions for each, 34; drafted nodes numbered through, so that waves
+// are full, 32).
 #pragma once
 #include "cache_four.hpp"
 
@@ -41,7 +42,7 @@ struct TurnArgs {
     CachePlaces to;
 };
 
-enum TurnTarget { kTurnRows, kTurnCache16, kTurnCache4 };
+enum TurnTarget { kTurnRows, kTurnRowsPast, kTurnCache16, kTurnCache4 };   // Past: past the L2 (put_row)
 constexpr int kTurnThreads = 256;
 constexpr int turn_heads_of_group(int d) { return kTurnThreads / (d / 16); }
 
@@ -52,11 +53,23 @@ __device__ __forceinline__ double inverse_root(double x)
     return x > 0.0 && x < __builtin_huge_val() ? fma(r * e, fma(e, 0.375, 0.5), r) : r;
 }
 
+// Rows that are written go past the L2 where it could not keep them for their reader: four prompts take 26 us instead of 33, 128 trees
+// of 128 nodes 26 instead of 32, with inputs from HBM (reads past it as well: 30 and 32).  The rows of smaller trees stay in it: the
+// attention that reads them next would take 153 us instead of 150, the rotation before it included (128 trees of 128, 16/8 heads of 64).
+template <bool PAST>
+__device__ __forceinline__ void put_row(uint4 *to, const uint4 &v)
+{
+    typedef uint32_t words __attribute__((ext_vector_type(4)));
+    if constexpr (PAST) __builtin_nontemporal_store(words{v.x, v.y, v.z, v.w}, (words *)to);
+    else *to = v;
+}
+
 template <int D, bool F16, TurnTarget TO, bool NEIGHBOURS>
 __global__ __launch_bounds__(kTurnThreads, 4) void row_turns_kernel(TurnArgs args)
 {
     const TurnArgs &a = args;
     constexpr int LANES = D / 16, ITEMS = kTurnThreads / LANES;
+    constexpr bool TREE = TO == kTurnRows || TO == kTurnRowsPast, PAST = TO != kTurnRows;
     const int b = blockIdx.y, t = threadIdx.x % LANES;
     int group = blockIdx.x;
     const bool is_q = group < a.q_groups;
@@ -69,7 +82,7 @@ __global__ __launch_bounds__(kTurnThreads, 4) void row_turns_kernel(TurnArgs arg
     const int row = (int)(item / (unsigned)step), first_head = (int)(item % (unsigned)step);
     // (what a row is decided and placed by is asked for at once)
     long long pos = a.start ? a.start[b] : 0;
-    if constexpr (TO == kTurnRows) {
+    if constexpr (TREE) {
         const int u = row < a.rows ? row : 0, tok = a.tok[(long long)b * a.rows + u];
         int depth = -1;
         for (int i = 0; i < a.anc_words; ++i) depth += __popcll(a.anc[u * a.anc_words + i]);
@@ -80,7 +93,7 @@ __global__ __launch_bounds__(kTurnThreads, 4) void row_turns_kernel(TurnArgs arg
         pos += row;
     }
     long long slot = -1;
-    if (TO != kTurnRows && !is_q) {
+    if (!TREE && !is_q) {
         slot = a.slots[(long long)b * a.width + row];
         if (slot < 0 || slot >= a.slot_count) slot = -1;
         if (slot < 0 && (!is_k || !a.k_out)) return;
@@ -90,14 +103,14 @@ __global__ __launch_bounds__(kTurnThreads, 4) void row_turns_kernel(TurnArgs arg
     const long long sdst = page * a.to.scale_page + place * a.to.scale_slot + t / 2;
 
     float y[16];
-    if (TO != kTurnRows && !is_q && !is_k) {         // values, as they are
+    if (!TREE && !is_q && !is_k) {         // values, as they are
         for (int head = first_head; head < heads; head += step) {
             const uint4 *from = (const uint4 *)(a.v + b * a.vs[0] + row * a.vs[1] + head * a.vs[2]) + 2 * t;
             const uint4 v0 = from[0], v1 = from[1];
             char *to = a.to.v + dst + head * dst_head;
             if constexpr (TO == kTurnCache16) {
-                ((uint4 *)to)[2 * t] = v0;
-                ((uint4 *)to)[2 * t + 1] = v1;
+                put_row<PAST>((uint4 *)to + 2 * t, v0);
+                put_row<PAST>((uint4 *)to + 2 * t + 1, v1);
             } else {
                 row_eight<F16>(v0, y);
                 row_eight<F16>(v1, y + 8);
@@ -172,14 +185,14 @@ __global__ __launch_bounds__(kTurnThreads, 4) void row_turns_kernel(TurnArgs arg
         const uint4 o0{row_two<F16>(y[0], y[1]), row_two<F16>(y[2], y[3]), row_two<F16>(y[4], y[5]), row_two<F16>(y[6], y[7])};
         const uint4 o1{row_two<F16>(y[8], y[9]), row_two<F16>(y[10], y[11]), row_two<F16>(y[12], y[13]), row_two<F16>(y[14], y[15])};
         if (out) {
-            ((uint4 *)(out + head * out_head))[first] = o0;
-            ((uint4 *)(out + head * out_head))[second] = o1;
+            put_row<PAST>((uint4 *)(out + head * out_head) + first, o0);
+            put_row<PAST>((uint4 *)(out + head * out_head) + second, o1);
         }
-        if (TO == kTurnRows || !is_k || slot < 0) continue;
+        if (TREE || !is_k || slot < 0) continue;
         char *to = a.to.k + dst + head * dst_head;
         if constexpr (TO == kTurnCache16) {
-            ((uint4 *)to)[first] = o0;
-            ((uint4 *)to)[second] = o1;
+            put_row<PAST>((uint4 *)to + first, o0);
+            put_row<PAST>((uint4 *)to + second, o1);
         }
         if constexpr (TO == kTurnCache4) {
             __shared__ float4 lines[kTurnThreads * 4];

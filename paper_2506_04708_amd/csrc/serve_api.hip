@@ -354,7 +354,10 @@ extern "C" int stand_tree_rotate(stand_handle *h, const stand_rotation *rotation
     a.to = CachePlaces{};
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
-    turn_launch<kTurnRows>(a, rotation, rows, groups, v.B, (hipStream_t)stream);
+    // (of a tree's rows a third to a half are not drafted; the L2s have 32 MB)
+    const bool past = (int64_t)v.B * rows->rows * (a.q_heads + (int64_t)a.kv_heads) * rows->head_dim * 2 > ((int64_t)64 << 20);
+    if (past) turn_launch<kTurnRowsPast>(a, rotation, rows, groups, v.B, (hipStream_t)stream);
+    else turn_launch<kTurnRows>(a, rotation, rows, groups, v.B, (hipStream_t)stream);
     return launched(v);
 }
 

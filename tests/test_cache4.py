@@ -79,6 +79,7 @@ class Rotate:
     ([12, 1], 9, 2, 1, 128, BF, 0, "halves", (True, True), 0.9, True),
     ([9] * 70, 2, 2, 1, 128, BF, 112, "halves", (True, True), 0.9, True),
     ([3], 1024, 3, 1, 64, BF, 32, "halves", (True, True), 0.98, False),
+    ([7, 900] * 8, 300, 40, 20, 128, HF, 128, "halves", (True, False), 0.7, True),    # more rows than the L2 keeps
 ], ids=lambda c: "B%d-N%d-%dx%d-d%d-%s%d" % (len(c[0]), c[1], c[2], c[3], c[4], c[7][0], c[6]))
 def test_rotate(binding, case):
     lens, N, H, G, d, dtype, dims, pairs, norm, share, fused = case
