@@ -14,7 +14,7 @@
 //
 // Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 26 us, 5.5 TB/s).  Trees
 // are bound by how little is on its way at a time: a wave asks for what its row is decided by, then for rows and cosines, and has
-// some 600 instructions for each head of its lanes between them and its stores (128 trees of 128 nodes, 16/8 heads of 128, 85 MB: 26 us; with its stores in the L2 and 132
+// some 240 instructions for each head of its lanes and 330 for a row between them and its stores (128 trees of 128 nodes, 16/8 heads of 128, 85 MB: 26 us; with its stores in the L2 and 132
 // instead of 128 registers, three waves of a SIMD instead of four, 31; one head for a thread, its conversions for each, 34; drafted nodes numbered through, so that waves
 // are full, 32).
 #pragma once
