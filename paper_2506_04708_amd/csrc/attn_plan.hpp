@@ -64,4 +64,20 @@ STAND_BOTH long long first_group(long long item_start, long long total, long lon
     return group_of(item_start + (long long)(start + 1) * weight - 1, total, W);
 }
 
+// Neighbours in the order of the work share an XCD and so its L2: workgroups go round the eight of them in turn, and each has an
+// eighth of the W shares.  Whether a team (of `teams` in every workgroup) has a share, and its number.
+STAND_BOTH bool share_of_team(unsigned workgroup, int team, int teams, long long W, long long &w)
+{
+    const int per_xcd = (int)((W + 7) / 8), in_xcd = (int)(workgroup / 8) * teams + team;
+    w = (long long)(workgroup % 8) * per_xcd + in_xcd;
+    return in_xcd < per_xcd && w < W;
+}
+// A head's rows over its tiles, groups of 32 in numbers that differ by one at most: the first row of a tile of so many groups at most (of
+// the tile behind the last one: past all rows, or their number).
+STAND_BOTH int tile_row(int tile, int all_rows, int groups_of_tile)
+{
+    const int groups = (all_rows + 31) / 32, tiles = (groups + groups_of_tile - 1) / groups_of_tile;
+    return 32 * (int)quotient((long long)tile * groups, tiles);
+}
+
 }  // namespace stand

@@ -96,10 +96,8 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
     const long long W = attn_groups(total, a.groups, S::START, S::HEAVY);
     const int wr = wave % S::WR, team = wave / S::WR, share_number = (int)blockIdx.x * S::TEAMS + team;
     if (wr == 0 && lane == 0 && share_number >= W) a.join[share_number] = JoinRecord{0, 0, 0, 0};   // (no share has this number)
-    // neighbours in the order of the work share an XCD and so its L2
-    const int per_xcd = (int)((W + 7) / 8), in_xcd = (int)(blockIdx.x / 8) * S::TEAMS + team;
-    const long long w = (long long)(blockIdx.x % 8) * per_xcd + in_xcd;
-    const bool has_share = in_xcd < per_xcd && w < W;
+    long long w;
+    const bool has_share = share_of_team(blockIdx.x, team, S::TEAMS, W, w);
     long long unit = 0, unit_end = 0, b_start = 0;
     int b = 0;
     if (has_share) {
@@ -163,9 +161,7 @@ __global__ __launch_bounds__(S::THREADS, S::MIN_WAVES) void tree_attn4_kernel(Tr
         const int heads_before = (int)quotient(unit - b_start, per_head);
         const long long head_start = b_start + heads_before * per_head;
         const int tile = (int)quotient(unit - head_start, per_item);
-        // (the groups of 32 rows in equal numbers for the head's tiles)
-        const int row_groups = (all_rows + 31) / 32, tiles = (row_groups + S::WR - 1) / S::WR;
-        const int row0 = 32 * (int)quotient((long long)tile * row_groups, tiles), rows = min(all_rows, 32 * (int)quotient((tile + 1ll) * row_groups, tiles));
+        const int row0 = tile_row(tile, all_rows, S::WR), rows = min(all_rows, tile_row(tile + 1, all_rows, S::WR));
         const int hk = (heads_before + b) % a.kv_heads;   // (not the same head of all trajectories at one time)
         const long long item_start = head_start + (long long)tile * per_item, item_end = item_start + per_item;
         const int u0 = (int)units_before(unit - item_start, 1, S::START, units), u1 = (int)units_before(unit_end - item_start, 1, S::START, units);
