@@ -460,7 +460,9 @@ typedef struct {
 
 /* Rows into the cache: for all layers, trajectories b and j < d_count[b], row d_row[b][j] of trajectory b goes to slot
  * d_slots[b][j] (stand_cache_pages).  After a verification d_row is d_out_node and d_count is d_out_len (width = depth + 1); a
- * prompt's rows go in as they stand with d_row NULL (row j).  Into a cache of 4 bits they go as described at stand_cache4.  d_count NULL: `width` each.  A negative slot or row (or one past
+ * prompt's rows go in as they stand with d_row NULL (row j).  Into a cache of 4 bits they go as described at stand_cache4: a drafted node's
+ * key that stand_tree_rotate has rounded to the rows' type is rounded to 4 bits from there, where stand_cache_append rounds the fp32
+ * key once, so that the two may differ next to borders of elements and scales.  d_count NULL: `width` each.  A negative slot or row (or one past
  * the end) is left out.  d_slots, d_row: [B][width].  The slots of a call differ from each other (where they do not, what
  * ends up there is not specified); the rows do not overlap the cache. */
 int stand_cache_commit(stand_handle *h, const stand_cache *cache, const stand_cache_rows *rows, const int64_t *d_slots, int32_t width,

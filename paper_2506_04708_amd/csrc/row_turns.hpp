@@ -4,19 +4,21 @@
 // For a head x of a row at position p:   y = w x / sqrt(mean(x^2) + eps)   (without a norm: y = x), then for each pair i of
 // rotated elements, (a, b) = (y[i], y[i + half]) or (y[2 i], y[2 i + 1]):
 //     a' = a cos(p, i) - b sin(p, i),   b' = a sin(p, i) + b cos(p, i)
-// with cos and sin from the caller's table.  All of it in fp64, rounded to fp32 and from there to the type that is written: the vector
-// units do fp64 at the rate of fp32, sums of squares cannot overflow, and what a key becomes in 4 bits is the nearest value of the formula's whatever
-// the order of the sums.
+// with cos and sin from the caller's table.  All of it in fp64, rounded to fp32 and from there to the type that is written: sums of
+// squares cannot overflow, and what a key becomes in 4 bits is the nearest value of the formula's whatever the order of the sums.  (An
+// fp64 operation takes a SIMD 4.4 clocks where an fp32 one takes 2.6, a conversion 4.5: with four waves on it, eight independent chains each.)
 //
 // A thread has 16 elements of a head, whole pairs of them (two pieces of 8 that lie half a rotation apart, or 16 in a row), so
 // that pairs need no exchange; D / 16 lanes have a head and add up their squares.  Workgroups have queries, keys or values, not a
 // mixture.  For 4 bits a key's elements change lanes through LDS, so that blocks are of neighbours.
 //
-// Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 26 us, 5.5 TB/s).  Trees
-// are bound by how little is on its way at a time: a wave asks for what its row is decided by, then for rows and cosines, and has
-// some 240 instructions for each head of its lanes and 330 for a row between them and its stores (128 trees of 128 nodes, 16/8 heads of 128, 85 MB: 26 us; with its stores in the L2 and 132
-// instead of 128 registers, three waves of a SIMD instead of four, 31; one head for a thread, its conversions for each, 34; drafted nodes numbered through, so that waves
-// are full, 32).
+// Bound by HBM with prompts (142 MB in and out, 4 x up to 2100 rows with 32 heads of queries, 8 of keys and values: 26 us, 5.5 TB/s).
+// Trees are bound by how little is on its way at a time: a wave asks for what its row is decided by, then for rows and cosines, and
+// has some 200 vector instructions for each head of its lanes, 139 of them fp64, and 150 for a row before them (128 trees of 128 nodes,
+// 16/8 heads of 128, 85 MB: 25 .. 27 us; with its stores in the L2 and 132 instead of 128 registers, three waves of a SIMD instead of
+// four, 31; one head for a thread, its conversions for each, 34; drafted nodes numbered through, so that waves are full, 32).
+// 128 registers are too few for most forms: pairs half a rotation apart spill 2, keys into 16 bits 2 or (such pairs) 4, into 4 bits 6
+// or 10, stored once a row and loaded again for every head.  Neighbouring pairs in rows spill none.
 #pragma once
 #include "cache_four.hpp"
 
@@ -42,7 +44,7 @@ struct TurnArgs {
     CachePlaces to;
 };
 
-enum TurnTarget { kTurnRows, kTurnRowsPast, kTurnCache16, kTurnCache4 };   // Past: past the L2 (put_row)
+enum TurnTarget { kTurnRows, kTurnRowsPast, kTurnCache16, kTurnCache4 };   // Past: past the caches (put_row), as the kinds behind it always
 constexpr int kTurnThreads = 256;
 constexpr int turn_heads_of_group(int d) { return kTurnThreads / (d / 16); }
 
@@ -53,9 +55,16 @@ __device__ __forceinline__ double inverse_root(double x)
     return x > 0.0 && x < __builtin_huge_val() ? fma(r * e, fma(e, 0.375, 0.5), r) : r;
 }
 
-// Rows that are written go past the L2 where it could not keep them for their reader: four prompts take 26 us instead of 33, 128 trees
-// of 128 nodes 26 instead of 32, with inputs from HBM (reads past it as well: 30 and 32).  The rows of smaller trees stay in it: the
-// attention that reads them next would take 153 us instead of 150, the rotation before it included (128 trees of 128, 16/8 heads of 64).
+// Rows that are written past the caches.  A tree's are where there are more than 64 MiB of them (stand_tree_rotate): the call by itself, on
+// two sets of inputs in turn, then takes 28 us instead of 34 (128 trees of 128 nodes, 16/8 heads of 128; 62 and 79 for 256 trees); in place it takes
+// 32 instead of 30.5; together with the attention behind it as long either way (322 and 322, 612 and 612; in place 326 and 326).
+// Smaller trees' stay in the caches: past them the rotation and its attention take 153 us instead of 150 (128 trees of 128, 16/8 heads of 64).
+//     Appended rows always are, whatever their number.  By itself an append of 4 prompts of 2100 (32/8 heads of 128) then takes 37 us into
+// 16 bits and 45 into 4, instead of 51 and 60, in turn on two sets of inputs; in place 39 and 49 instead of 38 and 43.  What reads
+// the rows next finds none of them in the caches: with a read of the tokens and a pass over the queries behind it 111 and 116 us instead of 102
+// and 106 (in place 105 and 108 instead of 99 and 102), with a product of 70 GFLOP for that pass 133 and 137 instead of 130 and 137; four chunks of
+// 1024 58 and 60 instead of 53 and 55.  Past 200 MB a call it is the better way behind which reader ever, by 1 .. 3 % (16 prompts of
+// 2100: 378 and 400 us instead of 391 and 412).  For 64 single tokens it makes no difference (with their attention 42 and 30 us both ways).
 template <bool PAST>
 __device__ __forceinline__ void put_row(uint4 *to, const uint4 &v)
 {

@@ -65,7 +65,15 @@ auto with_attn_shape(AttnForm f, Call call)
     default: return call(AttnShape<D, F16, D == 64 ? 4 : 8, 1, 2>{});
     }
 }
-// Over a cache of 4 bits: up to 64 rows a wave for each 32, more than that four waves of rows with the same keys.
+// Over a cache of 4 bits: up to 64 rows a wave for each 32, more than that four waves of rows with the same keys.  Between 33 and 64 rows
+// either may be ahead, as many trajectories or one: four heads of keys, d 128, all nodes drafted, waves by themselves and teams, us:
+//     rows          36           48           56           64
+//     1000 .. 9000 tokens, 32 trees     43, 55       48, 58       53, 57       54, 59       (three quarters drafted, 64 rows: 49, 57)
+//     200 .. 3000, 128 trees, 8 heads   110, 141     145, 146     157, 146     163, 148
+//     60 000, one tree                  55, 40       56, 40       57, 40       59, 41
+//     40, one tree                      15, 16       15, 16       15, 16       15, 17
+// and d 64 likewise (32 trees 31, 40 .. 37, 43; 128 trees 77, 95 .. 119, 98; one long 44, 32 .. 47, 33; one short 14, 12).  Lengths are the GPU's
+// alone, so the rule is by rows, and for batches, of whose trees a part is not drafted.
 template <int D, bool F16, typename Call>
 auto with_attn4_shape(AttnForm f, Call call)
 {
@@ -354,7 +362,7 @@ extern "C" int stand_tree_rotate(stand_handle *h, const stand_rotation *rotation
     a.to = CachePlaces{};
     const DeviceScope scope(v.device);
     if (scope.e != hipSuccess) return bad_device(v, scope.e);
-    // (of a tree's rows a third to a half are not drafted; the L2s have 32 MB)
+    // (what it takes and saves, alone and with its reader: put_row in row_turns.hpp; of a tree's rows a third to a half are not drafted)
     const bool past = (int64_t)v.B * rows->rows * (a.q_heads + (int64_t)a.kv_heads) * rows->head_dim * 2 > ((int64_t)64 << 20);
     if (past) turn_launch<kTurnRowsPast>(a, rotation, rows, groups, v.B, (hipStream_t)stream);
     else turn_launch<kTurnRows>(a, rotation, rows, groups, v.B, (hipStream_t)stream);

@@ -13,7 +13,7 @@
 // Above, the four waves of a workgroup have 32 rows each and the same keys (a team; a head's groups of 32 rows are shared out evenly over its
 // teams).  Every thread converts one block of a unit into LDS for all, two units ahead of the products' reads of them in the third place of
 // memory, and a step makes the scores of 32 keys beside the weights of the 32 before.  Two workgroups share a compute unit and do not wait for
-// each other.  (Waves by themselves take 150 us instead of 121 for the trees below: the vector units are the ones that are short, and every wave
+// each other.  (Waves by themselves took 150 us when teams took 121 for the trees below: the vector units are the ones that are short, and every wave
 // would convert everything; with all eight waves of a compute unit as one team, at one barrier, 133.)
 //
 // The tree comes first: the nodes that a wave's rows see, ancestors of a few nodes, are collected, so that most trees take one step of 32
@@ -22,10 +22,12 @@
 // Work is cut as attn_plan.hpp says, a share for every team that the chip holds; a unit is 32 keys (64 of heads of 64 in a team), the
 // whole tree is one.  Beginnings count as START units (64 single tokens 214 us, with 3 225, with 10 216; 32 trees 122, 128, 123).
 //
-// Bound: decoding by HBM (1.08 GB of cache in 213 us, 5.1 TB/s; a torch copy reaches 5.0 counting both ways).  Trees by what a wave issues between
-// its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128: 121 us for 70 GFLOP, 580 TFLOP/s on rows as
-// they are, where a large matrix product reaches 1253): a unit takes two workgroups about 1 us, of which the matrix units are busy for a
-// half.  Short calls by the chain lengths -> shares -> nodes -> ancestors, page numbers -> keys, each a trip to memory.
+// Bound: decoding by HBM (1.08 GB of cache in 211 .. 217 us, 5.0 .. 5.1 TB/s; a torch copy reaches 5.0 counting both ways).  Trees by what a wave
+// issues between its matrix instructions (32 trees of 64 nodes over 1000 .. 9000 tokens, 28 heads over 4, d 128: 125 .. 129 us for 70 GFLOP in passes one
+// behind the other, 545 .. 560 TFLOP/s on rows as they are, where a large matrix product reaches 1253; over 16 bits, in turn with
+// it, 132 and 126): a unit takes two workgroups about 1 us, of which the matrix units are busy for a half; of all clocks that compute units are at
+// work, with waves that have no rows, beginnings and ends, for a third.  Short calls by the chain lengths -> shares -> nodes -> ancestors, page numbers -> keys, each
+// a trip to memory.  Teams with d 128 have two registers too few: they are stored once an item and loaded behind its last key.
 #pragma once
 #include "mx4.hpp"
 #include "tree_attn.hpp"
@@ -62,9 +64,11 @@ struct Attn4Shape {
     static __device__ __forceinline__ int workgroups(const TreeAttn4Args &a) { return a.workgroups; }
     // Element of a head that a lane's first one of product x is.
     static __device__ __forceinline__ int element(int half, int x) { return ALONE ? D / 2 * half + 8 * x : 16 * x + 8 * half; }
-    // Keys stand in rows of KEY_ROW bytes: reads of one chunk of 16 keys and writes of a block of each of four (two) keys touch
-    // every bank once, and a lane's chunks are a constant apart.  16-byte chunk c of value k stands at chunk c ^ swizzle_v(k): the
-    // transposing reads have four chunks of four tokens; writes have, ALONE, one chunk of 16 tokens, else as keys.
+    // Keys stand in rows of KEY_ROW bytes, so that a lane's chunks are a constant apart, and 16-byte chunk c of value k stands at chunk
+    // c ^ swizzle_v(k): reads of one chunk of 16 keys, and the transposing ones of four chunks of four tokens, touch every one of 64 banks
+    // once, and so do the places of 16 lanes' writes (a block of each of four or two keys; ALONE one chunk of 16 tokens).  But writes of 16 bytes go
+    // eight lanes at a time to half of the banks, and of eight neighbours two meet in each: 16 clocks a write instead of 8, a quarter of what
+    // LDS is busy for in teams (d 64: a sixth), two fifths ALONE.
     static __device__ __forceinline__ int swizzle_v(int k)
     {
         const int far = D == 128 ? (k & 3) << 2 : ((k >> 1) & 1) << 2;
