@@ -406,3 +406,119 @@ def test_append_of_many_rows(binding, bits, G, d, dtype, R):
                     slots[b, n], slots[b, R - 1] = 4, 6      # behind the counts: these may not go in
         h.cache_append(c.cache, 0, *dev, slots, torch.tensor(start, **I32), None if counts is None else torch.tensor(counts, **I32), rot)
         c.check(near=True)
+
+
+# ---- rows that no 4 bits hold -------------------------------------------------------------------------------------------------------
+
+def held(c, i):
+    """The numbers that the cache's keys (0) or values (1) stand for."""
+    return serveref4.unpack(c.gpu[i].cpu(), c.gpu[i + 2].cpu(), c.dtype)
+
+
+@pytest.mark.parametrize("dtype,d,pairs,dims,norm", [(BF, 64, "halves", 64, True), (HF, 64, "neighbours", 32, False), (BF, 128, "neighbours", 128, False), (HF, 128, "halves", 96, True)])
+def test_appended_rows_that_are_no_finite_numbers(binding, dtype, d, pairs, dims, norm):
+    """A block with an infinity or a NaN, whether it was in the row, came of its turn or of a position without one, is NaN as a whole; the
+    others are as they would be without it.  Keys past what a scale reaches are held as its largest number."""
+    gen = torch.Generator().manual_seed(d + dims)
+    B, R, G, pages, page, positions = 3, 12, 2, 4, 16, 40
+    k, v = (torch.randn((B, R, G, d), generator=gen).to(dtype) for _ in range(2))
+    inf, nan, top = float("inf"), float("nan"), torch.finfo(dtype).max
+    k[0, 0, 0, 3], k[0, 1, 1, d - 1], k[0, 2, 0, 17] = inf, nan, -inf
+    v[0, 0, 1, 40], v[0, 1, 0, 0], v[0, 2, 1, 63] = nan, -inf, inf
+    k[0, 3], v[0, 3] = 0.0, -0.0
+    k[0, 4, 0], v[0, 4, 0] = top, -top
+    k[0, 5, 0, 5], v[0, 5, 0, 5] = top, top
+    smallest = 2.0 ** -133 if dtype is BF else 2.0 ** -24
+    k[0, 6, 0], v[0, 6, 0] = smallest, smallest
+    table = serveref4.turns(positions, dims)
+    w = (1 + 0.3 * torch.randn(d, generator=gen)).to(dtype) if norm else None
+    start = [5, positions - 6, -4]                           # the second one's last rows and the third one's first have no position
+    slots = torch.randperm(pages * page, generator=gen)[:B * R].reshape(B, R)
+    c = Cached(binding, gen, 1, pages, page, G, d, dtype, 4, "nhd")
+    before = [held(c, i) for i in range(2)]
+    h = handle(binding, B, tree(1))
+    rot = binding.Rotation(table.cuda(), pairs, None, None if w is None else w.cuda(), 0.0 if not norm else 1e-6)
+    h.cache_append(c.cache, 0, k.cuda(), v.cuda(), slots.cuda(), torch.tensor(start, **I32), None, rot)
+    pos = torch.tensor(start)[:, None].long() + torch.arange(R)
+    want = [serveref4.turned(k, pos, table, pairs, w, 1e-6).float(), v.float()]
+    for i in range(2):
+        x = before[i].clone()
+        flat = x.reshape(pages * page, G, d)
+        flat[slots] = serveref4.unpack(*serveref4.pack(want[i], dtype), dtype)
+        got = held(c, i)
+        assert torch.equal(torch.isnan(got), torch.isnan(x)), (torch.isnan(got) != torch.isnan(x)).nonzero()[:4]
+        assert torch.equal(torch.nan_to_num(got), torch.nan_to_num(x))
+        assert not bool(torch.isinf(got).any())
+    nans = torch.isnan(held(c, 0).reshape(-1, G, d)[slots])
+    assert bool(nans[1, 6:, :, :dims // 32 * 32].all()) and bool(nans[2, :4, :, :dims // 32 * 32].all())
+
+
+# ---- many trajectories, long texts ----------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("N,H,G,d,dtype,most", [(1, 2, 1, 64, BF, 40), (2, 40, 1, 64, HF, 40), (1, 1, 1, 128, HF, 40)])
+def test_as_many_trajectories_as_it_takes(binding, N, H, G, d, dtype, most):
+    lens = [int(x) for x in np.random.default_rng(3).integers(0, most, 4096)]
+    Attn4(binding, 97, lens, N, H, G, d, 16, dtype, 1.0).check()
+
+
+def test_more_trajectories_are_refused(binding):
+    t = Attn4(binding, 98, [3] * 4097, 1, 2, 1, 64, 16, BF, 1.0)
+    with pytest.raises(binding.StandError):
+        t.h.tree_attention(**t.on_gpu())
+
+
+@pytest.mark.parametrize("N,H,d,dtype,page", [(1, 4, 64, BF, 16), (9, 8, 64, HF, 8), (9, 4, 128, BF, 64), (9, 10, 128, BF, 4096)])
+def test_long_texts(binding, N, H, d, dtype, page):
+    """Two hundred thousand tokens, many times the same pages: a table may name a page as often as it likes."""
+    t = Attn4(binding, 600 + N + d, [16 * page, 33], N, H, 1, d, page, dtype, 1.0)
+    n = 200003
+    t.width = -(-n // page)
+    t.table = np.random.default_rng(5).integers(0, t.pages, (2, t.width)).astype(np.int32)
+    t.lens = [n, 33]
+    t.check()
+
+
+@pytest.mark.parametrize("N,H", [(9, 4), (64, 6)])
+def test_graphs_on_two_streams(binding, N, H):
+    """Two graphs, each with its own buffers and workspaces, replayed on two streams without waiting for each other, rotations and appends
+    in them; eager calls in between."""
+    d, dtype, B = 128, BF, 2
+    ts = [Attn4(binding, 700 + i, [900, 70], N, H, 2, d, 16, dtype, 0.9) for i in range(2)]
+    turns = serveref4.turns(1000, d)
+    rot = binding.Rotation(turns.cuda())
+    sides, graphs, all_args, q_in = [torch.cuda.Stream() for _ in ts], [], [], []
+    for t, s in zip(ts, sides):
+        a = t.on_gpu()
+        x = [a["q"].clone(), a["k"].clone()]
+        a["out"] = torch.empty_like(a["q"])
+
+        def call(a=a, x=x, t=t):
+            t.h.tree_rotate(rot, a["length"], a["draft_tok"], x[0], x[1], a["q"], a["k"])
+            t.h.tree_attention(**a)
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            call()
+        s.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=s):
+            call()
+        graphs.append(g)
+        all_args.append(a)
+        q_in.append(x)
+    torch.cuda.synchronize()
+    for rep in range(5):
+        for a in all_args:
+            a["out"].fill_(3.0)
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, sides):
+            with torch.cuda.stream(s):
+                g.replay()
+                g.replay()
+        torch.cuda.synchronize()
+        for t, a in zip(ts, all_args):
+            if rep == 0:                                     # what the attention saw: the rotated rows as they are
+                t.q, t.k = a["q"].cpu(), a["k"].cpu()
+            t.check(a["out"])
+            eager = t.h.tree_attention(**dict(a, out=None))
+            torch.cuda.synchronize()
+            assert torch.equal(eager, a["out"])
